@@ -293,6 +293,109 @@ bsa_status_t bsa_block_backward(const bsa_params_t* p, int32_t ffn_dim, const bs
                                 const float* dy, float* dx, const bsa_block_grads_t* dw, void* ws,
                                 size_t ws_bytes, void* stream);
 
+/* ---- Dense operators beside the layer ----
+ *
+ * What a model has around the sparse layer: layer norms, affine maps with an activation or a
+ * residual, and full attention over packed sequences. They follow the conventions above
+ * (device pointers of the current device, asynchronous on `stream` alone, caller-owned
+ * buffers, host-side checks before any launch) and are deterministic. They take bf16 or
+ * float32 tensors (dtype); every sum and statistic is float32 and a result is rounded once to
+ * its tensor's type. Rows are contiguous along their last dimension; a leading dimension or
+ * stride of 0 means the packed one. Outputs may not overlap inputs, except where said. A call
+ * without rows (rows, m, total_q = 0) is valid; its weight gradients are zero. */
+
+/* Layer norm over the last dimension: y = (x - mean) rstd gain + bias, rstd = 1 / sqrt(var + eps)
+ * with the biased variance. */
+typedef struct {
+  int64_t rows;                       /* >= 0                                           */
+  int32_t cols;                       /* 1 .. 32768                                     */
+  int32_t dtype;                      /* bsa_dtype_t of x, y, dy and dx                 */
+  float eps;                          /* > 0                                            */
+  int64_t ld_x, ld_y, ld_dy, ld_dx;   /* elements between rows (0: cols)                */
+} bsa_layernorm_t;
+
+/* Validate p and report the backward workspace (ws_bwd_bytes may be NULL). */
+bsa_status_t bsa_layernorm_sizes(const bsa_layernorm_t* p, size_t* ws_bwd_bytes);
+
+/* x [rows, cols] -> y; gain, bias [cols] float32 (bias may be NULL: 0); mean, rstd [rows] float32
+ * outputs, which the backward reads. */
+bsa_status_t bsa_layernorm_forward(const bsa_layernorm_t* p, const void* x, const float* gain, const float* bias,
+                                   void* y, float* mean, float* rstd, void* stream);
+
+/* dx [rows, cols] (dtype), dgain and dbias [cols] float32 (dbias may be NULL: not formed), all
+ * overwritten. dx may be dy or x (same leading dimension). */
+bsa_status_t bsa_layernorm_backward(const bsa_layernorm_t* p, const void* x, const float* gain, const float* mean,
+                                    const float* rstd, const void* dy, void* dx, float* dgain, float* dbias, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Affine map with an epilogue: z = x w^T + bias, y = act(z) + res, with x [m, k], w [n, k], y [m, n]. */
+typedef enum { BSA_ACT_NONE = 0, BSA_ACT_RELU = 1, BSA_ACT_GELU = 2 /* erf form */, BSA_ACT_SILU = 3 } bsa_act_t;
+typedef struct {
+  int64_t m;                            /* rows, 0 .. 2^31 - 1                          */
+  int32_t k, n;                         /* input and output channels, >= 1              */
+  int32_t dtype;                        /* bsa_dtype_t of every tensor                  */
+  int32_t act;                          /* bsa_act_t                                    */
+  int64_t ld_x, ld_w, ld_y, ld_res, ld_dy;  /* elements between rows (0: packed)        */
+} bsa_linear_t;
+
+/* Validate p and report the workspaces (pointers may be NULL). */
+bsa_status_t bsa_linear_sizes(const bsa_linear_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes);
+
+/* bias [n], res [m, n] (may be y itself) and pre may be NULL. pre [m, n] packed receives z for the
+ * backward of a map with an activation (z rounded to dtype). */
+bsa_status_t bsa_linear_forward(const bsa_linear_t* p, const void* x, const void* w, const void* bias, const void* res,
+                                void* y, void* pre, void* ws, size_t ws_bytes, void* stream);
+
+/* With dz = dy act'(z): dx = dz w [m, k], dw = dz^T x [n, k], db = sum of dz over the rows [n], all
+ * dtype, packed and overwritten; each may be NULL (not formed). The residual's gradient is dy.
+ * pre: as filled by the forward (ignored, may be NULL, without an activation). dz is rounded to
+ * dtype where it enters the products (not in db). */
+bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const void* w, const void* pre, const void* dy,
+                                 void* dx, void* dw, void* db, void* ws, size_t ws_bytes, void* stream);
+
+/* Full attention over packed sequences with grouped heads. Sequence s has the query rows
+ * [cu_q[s], cu_q[s+1]) and the key rows [cu_k[s], cu_k[s] + l), l = used_k[s] (a cache that is
+ * filled so far) or, with used_k NULL, cu_k[s+1] - cu_k[s]. Query head h reads key head
+ * h / (heads / kv_heads). o = softmax(scale q k^T) v over the visible keys: all of the sequence's, or,
+ * causal, key j for query i when j <= i + (l - query rows): the last query sees every key. A query
+ * that sees no key has o = 0 and lse = -inf and takes no part in the gradients. A value of v, d_o, q or
+ * k that is not finite may reach every row of the 64-row tile that it is read in.
+ * cu_q, cu_k [seqs + 1] and used_k [seqs] are device arrays (int32): from 0, not decreasing, at most
+ * total_q, total_k and the capacity cu_k[s+1] - cu_k[s]. They cannot be checked on the host: values
+ * outside the tensors are pulled inside (nothing is read or written out of bounds), and then
+ * the outputs are not defined. */
+typedef struct {
+  int32_t seqs;                         /* >= 1                                         */
+  int32_t heads, kv_heads;              /* kv_heads divides heads                       */
+  int32_t head_dim;                     /* 32, 64 or 128                                */
+  int64_t total_q, total_k;             /* rows of q and of k and v, 0 .. 2^31 - 1      */
+  int32_t causal;                       /* 0 or 1                                       */
+  int32_t dtype;                        /* bsa_dtype_t of q, k, v, o, d_o, dq, dk, dv   */
+  float softmax_scale;                  /* 0 -> 1/sqrt(head_dim)                        */
+  int32_t zero_rest;                    /* rows in no sequence (and unused cache rows):
+                                           0 = outputs keep what they held, 1 = outputs
+                                           are set to 0 (lse to -inf)                   */
+  /* elements between rows and between heads of [rows, heads, head_dim] tensors; multiples of
+   * 16 bytes, like the tensors' addresses; both 0: packed */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, do_row, do_head;
+} bsa_attention_t;
+
+/* Validate p and report the workspaces (pointers may be NULL). */
+bsa_status_t bsa_attention_sizes(const bsa_attention_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes);
+
+/* o [total_q, heads, head_dim], lse [heads, total_q] float32 (natural logarithm). */
+bsa_status_t bsa_attention_forward(const bsa_attention_t* p, const void* q, const void* k, const void* v,
+                                   const int32_t* cu_q, const int32_t* cu_k, const int32_t* used_k, void* o, float* lse,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/* dq [total_q, heads, head_dim], dk and dv [total_k, kv_heads, head_dim], packed, dtype, overwritten (a
+ * key head's gradient is the sum over its group). o and lse as filled by the forward. Sequences may
+ * not share rows. */
+bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, const void* k, const void* v,
+                                    const void* o, const float* lse, const void* d_o, const int32_t* cu_q,
+                                    const int32_t* cu_k, const int32_t* used_k, void* dq, void* dk, void* dv, void* ws,
+                                    size_t ws_bytes, void* stream);
+
 /* ---- Measurement support (not part of the layer's computation) ---- */
 
 /* on = 1: start recording, clearing earlier records; on = 0: stop and clear. While on,
@@ -301,7 +404,8 @@ bsa_status_t bsa_block_backward(const bsa_params_t* p, int32_t ffn_dim, const bs
  * "fwd.ball", "fwd.cmp", "fwd.slc", "fwd.gate", "bwd.lse" (store_lse = 0), "bwd.gate", "bwd.dq_ball", "bwd.dq_cmp",
  * "bwd.dq_slc", "bwd.kv_ball", "bwd.kv_cmp", "bwd.mlp", "bwd.slc_csr", "bwd.slc_kv", and
  * for the block "blk.norm", "blk.gemm" (activation products), "blk.wgrad" (weight
- * gradients), "blk.elem" (SwiGLU, casts, layout changes).
+ * gradients), "blk.elem" (SwiGLU, casts, layout changes). Each dense operator's call is one
+ * phase: "norm.fwd", "norm.bwd", "linear.fwd", "linear.bwd", "attn.fwd", "attn.bwd".
  * Host-side bookkeeping only; no device memory is allocated. */
 bsa_status_t bsa_timing_enable(int32_t on);
 

@@ -58,6 +58,24 @@ class bsa_block_saved_t(C.Structure):
         "rstd1", "rstd2", "xn1", "gate", "q", "k", "v", "o", "h", "xn2", "uw", "a")]
 
 
+class bsa_layernorm_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)] + [
+        (n, C.c_int64) for n in ("ld_x", "ld_y", "ld_dy", "ld_dx")]
+
+
+class bsa_linear_t(C.Structure):
+    _fields_ = [("m", C.c_int64), ("k", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32)] + [
+        (n, C.c_int64) for n in ("ld_x", "ld_w", "ld_y", "ld_res", "ld_dy")]
+
+
+class bsa_attention_t(C.Structure):
+    _fields_ = [("seqs", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("total_q", C.c_int64), ("total_k", C.c_int64), ("causal", C.c_int32), ("dtype", C.c_int32),
+                ("softmax_scale", C.c_float), ("zero_rest", C.c_int32)] + [
+        (n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "o_row", "o_head",
+                                 "do_row", "do_head")]
+
+
 _SIGS = {
     "bsa_status_string": (C.c_char_p, [C.c_int]),
     "bsa_last_error": (C.c_char_p, []),
@@ -95,6 +113,15 @@ _SIGS = {
     "bsa_block_backward": (C.c_int, [C.POINTER(bsa_params_t), C.c_int32, C.POINTER(bsa_block_weights_t),
                                      C.c_void_p, C.c_void_p, C.POINTER(bsa_block_saved_t), C.c_void_p, C.c_void_p,
                                      C.POINTER(bsa_block_grads_t), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "bsa_layernorm_sizes": (C.c_int, [C.POINTER(bsa_layernorm_t), C.POINTER(C.c_size_t)]),
+    "bsa_layernorm_forward": (C.c_int, [C.POINTER(bsa_layernorm_t)] + [C.c_void_p] * 7),
+    "bsa_layernorm_backward": (C.c_int, [C.POINTER(bsa_layernorm_t)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]),
+    "bsa_linear_sizes": (C.c_int, [C.POINTER(bsa_linear_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "bsa_linear_forward": (C.c_int, [C.POINTER(bsa_linear_t)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]),
+    "bsa_linear_backward": (C.c_int, [C.POINTER(bsa_linear_t)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "bsa_attention_sizes": (C.c_int, [C.POINTER(bsa_attention_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "bsa_attention_forward": (C.c_int, [C.POINTER(bsa_attention_t)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]),
+    "bsa_attention_backward": (C.c_int, [C.POINTER(bsa_attention_t)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None

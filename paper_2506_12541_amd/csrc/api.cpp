@@ -11,6 +11,7 @@
 #include <string>
 
 #include "kernels.hpp"
+#include "status.hpp"
 
 namespace {
 
@@ -247,6 +248,13 @@ BwdWs bwd_ws_layout(const bsa::Dims& D) {
 }
 
 }  // namespace
+
+namespace bsa {
+
+void clear_error() { g_last_error.clear(); }
+bsa_status_t set_error(bsa_status_t s, const std::string& msg) { return fail(s, msg); }
+
+}  // namespace bsa
 
 extern "C" {
 

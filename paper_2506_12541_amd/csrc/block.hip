@@ -3,6 +3,7 @@
 // cores with f32 accumulation, RMSNorm forward/backward, SwiGLU forward/backward, and the
 // casts, layout changes and deterministic reductions between them.
 #include "common.hpp"
+#include "gemm_common.hpp"
 #include "kernels.hpp"
 
 namespace bsa {
@@ -24,14 +25,6 @@ constexpr float kNormEps = 1e-6f;
 //     x columns and read with transposing LDS reads (ds_read_b64_tr_b16).
 // Accumulator lane L holds C[m0 + L % 16][n0 + 4 (L / 16) + e], e = 0..3 (the B fragment
 // is the first MFMA operand).
-
-// 16-byte chunk swizzle of a staged tile row: 4 or 8 chunks per row (row-fragment reads
-// of 16 consecutive rows on distinct banks) or 16 and more chunks per row (transposing
-// reads of 8 consecutive rows, chunk pairs on distinct banks).
-template <int COLS>
-__device__ __forceinline__ int tile_swz(int x) {
-  return COLS == 32 ? ((x >> 1) & 3) : COLS == 64 ? (x & 7) : 2 * (x & 7);
-}
 
 // Staging of ROWS x COLS tiles of a logical row-major operand into LDS by the NW waves of
 // the workgroup. Each wave instruction fills 1 KB of consecutive LDS; lane L's 16 bytes
@@ -89,80 +82,6 @@ __device__ __forceinline__ long long kt_offset(const GemmMat& m, int kt) {
   return ((b * m.heads << m.lgn) + t) << m.lgd;
 }
 
-template <int BK>
-__device__ __forceinline__ bf16x8 frag_row(const bf16_t* t, int row, int lc) {
-  return *reinterpret_cast<const bf16x8*>(t + row * BK + 8 * (lc ^ tile_swz<BK>(row)));
-}
-
-// Workgroup barrier without a memory fence: the waves' direct-to-LDS loads are already
-// waited for by each wave (vmcnt), and later tiles stay in flight across it (the fence of
-// __syncthreads would wait for every outstanding load). The empty statements keep the
-// compiler from moving LDS accesses across it.
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-// s_waitcnt with vmcnt = V (expcnt and lgkmcnt left at their maxima)
-template <int V>
-__device__ __forceinline__ void vm_wait() {
-  static_assert(V >= 0 && V < 64, "vmcnt");
-  __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | (7 << 4) | (15 << 8));
-}
-
-// Wait for this wave's LDS reads; no LDS access moves across it.
-__device__ __forceinline__ void lgkm_drain() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-// LDS byte addresses of the two transposing reads that give lane (p = L % 16, j = L / 16)
-// the operand X[k0 + 4j + i][m0 + p] (i = 0..3) and X[k0 + 16 + 4j + i][m0 + p] of a
-// [BK][COLS] tile X (BK = 32 or 64): within each 16-lane group, ds_read_b64_tr_b16 hands lane l element
-// l % 4 of the 4-element runs addressed by lanes l / 4, 4 + l / 4, 8 + l / 4, 12 + l / 4, so
-// lane p addresses row k0 + 4j + p / 4 (then + 16) at columns m0 + 4 (p % 4) + [0, 4).
-template <int COLS>
-__device__ __forceinline__ void tr_addr(const bf16_t* t, int k0, int m0, int lane, uint32_t& o0, uint32_t& o1) {
-  const int p = lane & 15, j = lane >> 4;
-  const int col = m0 + 4 * (p & 3);
-  const int lc = col >> 3, sub = col & 7;
-  const int x0 = k0 + 4 * j + (p >> 2), x1 = x0 + 16;
-  const bf16_t* a0 = t + x0 * COLS + 8 * (lc ^ tile_swz<COLS>(x0)) + sub;
-  const bf16_t* a1 = t + x1 * COLS + 8 * (lc ^ tile_swz<COLS>(x1)) + sub;
-  o0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)a0;
-  o1 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)a1;
-}
-
-// Four operand fragments (columns m0 + 16 i, i = 0..3) of one 32-deep contraction step of
-// the transposed form, issued as one statement that also waits for them: every use of the
-// results follows the wait.
-template <int COLS>
-__device__ __forceinline__ void tr_frags4(const bf16_t* t, int k0, int m0, int lane, bf16x8 (&f)[4]) {
-  uint32_t a[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) tr_addr<COLS>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
-  uint2 r[8];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\t"
-      "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
-      "ds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\t"
-      "ds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7])
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    f[i] = __builtin_bit_cast(bf16x8, make_uint4(r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y));
-}
-
-// 1 / (1 + exp(-x)): the hardware reciprocal and one Newton step (within an ulp of the divided
-// value, at a third of the division's instructions). Where exp(-x) leaves the range in which the
-// reciprocal is a normal number (x below -87) the reciprocal stands: the step would give NaN.
-__device__ __forceinline__ float sigmoid(float x) {
-  const float y = 1.0f + __expf(-x);
-  const float r = __builtin_amdgcn_rcpf(y);
-  return y < 0x1p126f ? fmaf(fmaf(-y, r, 1.0f), r, r) : r;
-}
-
 struct GemmArgs {
   GemmMat a, b;
   int ntn;        // column tiles
@@ -171,14 +90,6 @@ struct GemmArgs {
   long long split_stride;   // elements between the partial products of two splits
   bool stream_out;          // SwiGLU forward: stores that bypass the caches
 };
-
-// Rows of a wave's tile that pass through LDS at a time in the epilogue: as many as fit the
-// four arrays of the first two stages.
-constexpr int epi_rows(int array_bytes, int tmw, int tnw, int nw) {
-  int rp = tmw;
-  while (rp > 16 && 4 * (array_bytes / (rp * tnw * 4)) < nw) rp /= 2;
-  return rp;
-}
 
 // Workgroup tile BM x BN of WM x WN waves (wave tile BM / WM x BN / WN in 16 x 16
 // accumulator tiles); contraction tiles of BK in a ring of NS LDS stages, NS - 1 of them in

@@ -1,0 +1,708 @@
+// Packed attention: sequences of different lengths one behind another, grouped heads, causal or
+// not. Sequence s has the query rows [cu_q[s], cu_q[s + 1]) and the key rows [cu_k[s],
+// cu_k[s] + len_k); with S = scale q k^T over the keys a query may see, P = softmax(S):
+//   o = P v, lse = log sum exp S;   D = rowsum(dO o), dS = P (dO v^T - D),
+//   dq = scale dS k, dk = scale dS^T q, dv = P^T dO, dk and dv summed over a key head's group.
+// A row that sees no key has o = 0, lse = -inf and no gradient.
+//
+// The G = heads / kv_heads query heads of a key head share its tiles: a sequence has len_q G
+// packed rows (row p = query p / G, head p % G of the group), so grouped heads, single tokens
+// and the sum over the group need no separate code, and one read of a key tile serves them all.
+// A query-major pass forms o (and dq), a key-major pass dk and dv; no atomics, every sum in a
+// fixed order.
+//
+// The scores are formed transposed (S^T = K Q^T on 16 x 16 tiles, a lane owns a query column),
+// so that probabilities are already laid out as the operand of the next product.
+//
+// Lengths live on the device, so the grid covers the most tiles there can be: sequence s takes
+// tile slots floor(cu[s] G / rows) + s and on, which is monotone and never less than it needs; a
+// workgroup finds its sequence by a 64-way search and leaves when its tile is empty.
+#include <algorithm>
+#include <cmath>
+
+#include "common.hpp"
+#include "attn_common.hpp"
+#include "dense.hpp"
+#include "dense_common.hpp"
+
+namespace bsa {
+namespace {
+
+constexpr int kWaves = 4;
+
+struct Seq {
+  int s;
+  long long q0, k0;      // first query and key row
+  int lq, lk;            // query and key rows
+  int eq, ek;            // rows up to the next sequence's first (eq >= lq, ek >= lk)
+  long long tile;        // this workgroup's tile within the sequence
+};
+
+__device__ __forceinline__ long long clampll(long long x, long long lo, long long hi) {
+  return x < lo ? lo : x > hi ? hi : x;
+}
+
+// The sequence that owns tile slot `slot` of rows-per-tile R (mult packed rows for each row of
+// cu). Offsets outside the tensors are pulled inside: no read or write leaves them.
+__device__ __forceinline__ Seq find_seq(long long slot, const int* cu, int mult, int R, const int* cu_q,
+                                        const int* cu_k, const int* used_k, int S, long long total_q,
+                                        long long total_k) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = S;
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int i = lane * step;
+    const bool le = i < n && (i == 0 || (long long)cu[lo + i] * mult / R + lo + i <= slot);
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(le)) - 1;
+    lo += c * step;
+    n = min(step, n - c * step);
+  }
+  Seq q;
+  q.s = __builtin_amdgcn_readfirstlane(lo);
+  const long long qb = clampll(cu_q[q.s], 0, total_q), kb = clampll(cu_k[q.s], 0, total_k);
+  q.q0 = qb;
+  q.k0 = kb;
+  q.lq = (int)(clampll(cu_q[q.s + 1], qb, total_q) - qb);
+  q.ek = (int)(clampll(cu_k[q.s + 1], kb, total_k) - kb);
+  q.lk = used_k ? (int)clampll(used_k[q.s], 0, q.ek) : q.ek;
+  q.eq = q.s + 1 < S ? q.lq : (int)(total_q - qb);
+  if (q.s + 1 >= S) q.ek = (int)(total_k - kb);
+  q.tile = slot - ((long long)cu[q.s] * mult / R + q.s);
+  return q;
+}
+
+template <typename T> struct AttnTile {
+  static constexpr int keys = sizeof(T) == 2 ? 64 : 32;   // keys (or query rows) of a staged tile
+};
+
+// ---- LDS tiles of ROWS x HD elements, filled by direct loads, 16-byte pieces swizzled ----
+
+template <typename T, int HD> __device__ __forceinline__ int tswz(int row) { return swz<HD * (int)sizeof(T) / 2>(row); }
+
+// Rows r0 + [0, ROWS) of a matrix with row stride ld; rows at or past nrows repeat the last one
+// (masked by the caller; nrows > 0).
+template <typename T, int HD, int ROWS>
+struct TileLoad {
+  static constexpr int E = 16 / (int)sizeof(T), CPR = HD / E, NI = ROWS * CPR / 64;
+  static_assert(NI % kWaves == 0, "tile / wave split");
+  __device__ __forceinline__ static void issue(T* lds, const T* g, long long ld, int r0, int nrows, int wid, int lane) {
+#pragma unroll
+    for (int u = 0; u < NI / kWaves; ++u) {
+      const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
+      const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
+      const int r = min(r0 + row, nrows - 1);
+      __builtin_amdgcn_global_load_lds(g + r * ld + E * c, lds + blk * 64 * E, 16, 0, 0);
+    }
+  }
+};
+
+// 8 consecutive elements (chunk lc) of a tile row
+template <int HD>
+__device__ __forceinline__ bf16x8 row_frag(const bf16_t* t, int x, int lc) { return lds_row_chunk<HD>(t, x, lc); }
+template <int HD>
+__device__ __forceinline__ f32x8 row_frag(const float* t, int x, int lc) {
+  const float* row = t + x * HD;
+  const int s = tswz<float, HD>(x);
+  const float4 a = *reinterpret_cast<const float4*>(row + 4 * ((2 * lc) ^ s));
+  const float4 b = *reinterpret_cast<const float4*>(row + 4 * ((2 * lc + 1) ^ s));
+  return f32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+// column m0 + lane % 16 at rows k0 + 4j + i and k0 + 16 + 4j + i (j = lane / 16, i = 0..3)
+template <int HD>
+__device__ __forceinline__ bf16x8 col_frag(const bf16_t* t, int k0, int m0, int lane) {
+  return lds_tr_chunk<HD>(t, k0, m0, lane);
+}
+template <int HD>
+__device__ __forceinline__ f32x8 col_frag(const float* t, int k0, int m0, int lane) {
+  const int c = m0 + (lane & 15), j = lane >> 4;
+  f32x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int x = k0 + (e < 4 ? 0 : 16) + 4 * j + (e & 3);
+    v[e] = t[x * HD + 4 * ((c >> 2) ^ tswz<float, HD>(x)) + (c & 3)];
+  }
+  return v;
+}
+
+// Element offsets of a packed row: query row t = q0 + p / G, head hk G + p % G.
+struct RowAt {
+  long long t;
+  int h;
+};
+__device__ __forceinline__ RowAt packed_row(const Seq& sq, int hk, int G, long long p) {
+  const int q = (int)(p / G);
+  return RowAt{sq.q0 + q, hk * G + (int)(p - (long long)q * G)};
+}
+
+// The same for packed rows r0 + [0, ROWS) (rows of them, > 0).
+template <typename T, int HD, int ROWS>
+struct PackedLoad {
+  static constexpr int E = 16 / (int)sizeof(T), CPR = HD / E, NI = ROWS * CPR / 64;
+  static_assert(NI % kWaves == 0, "tile / wave split");
+  __device__ __forceinline__ static void issue(T* lds, const T* g, long long row_ld, long long head_ld, const Seq& sq,
+                                               int hk, int G, long long r0, long long rows, int wid, int lane) {
+#pragma unroll
+    for (int u = 0; u < NI / kWaves; ++u) {
+      const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
+      const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
+      const RowAt at = packed_row(sq, hk, G, min(r0 + row, rows - 1));
+      __builtin_amdgcn_global_load_lds(g + at.t * row_ld + at.h * head_ld + E * c, lds + blk * 64 * E, 16, 0, 0);
+    }
+  }
+};
+
+// ---- forward ----
+
+struct FwdP {
+  AttnArgs a;
+  const void *q, *k, *v;
+  const int *cu_q, *cu_k, *used_k;
+  void* o;
+  float* lse;
+  float sl2;         // scale log2(e)
+  int nsplit;        // splits of the key axis
+  float* part;       // [nsplit][total_q][heads][hd] unnormalised outputs
+  float2* ml;        // [nsplit][total_q][heads] reference maximum (log2 units) and sum
+};
+
+// Keys [lo, hi) of split z: equal runs of whole tiles.
+__device__ __forceinline__ void split_range(int lk, int nsplit, int z, int KT, int& lo, int& hi) {
+  const int tiles = (lk + KT - 1) / KT, per = (tiles + nsplit - 1) / nsplit;
+  lo = min(z * per * KT, lk);
+  hi = min(lo + per * KT, lk);
+}
+
+template <typename T, int HD, int QB>
+__global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
+  constexpr int KT = AttnTile<T>::keys, KB = KT / 16, NCH = HD / 32, DB = HD / 16, R = 16 * QB * kWaves;
+  typedef typename Chunk<T>::type CT;
+  __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
+  const AttnArgs& a = p.a;
+  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, j = lane >> 4;
+  const Seq sq = find_seq(blockIdx.x, p.cu_q, G, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
+  const long long rows = (long long)sq.lq * G, ext = (long long)sq.eq * G;
+  // tiles in descending order: with a causal mask the longest rows come first
+  const long long nt = (rows + R - 1) / R;
+  const long long tile = sq.tile < nt ? nt - 1 - sq.tile : sq.tile;
+  const long long p0 = tile * R;
+  if (p0 < 0 || p0 >= ext || (p0 >= rows && (!a.zero_rest || p.nsplit > 1))) return;
+  T* const out = (T*)p.o;
+
+  long long pr[QB];
+  int lim[QB];        // the last key that this lane's query sees
+  CT qf[QB][NCH];
+  f32x4 o[QB][DB];
+  float mx[QB], ls[QB];
+  const int off = sq.lk - sq.lq;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    pr[qb] = p0 + (wid * QB + qb) * 16 + r;
+    const bool on = pr[qb] < rows;
+    const RowAt at = packed_row(sq, hk, G, on ? pr[qb] : 0);
+    lim[qb] = !on ? -1 : a.causal ? min((int)(at.t - sq.q0) + off, sq.lk - 1) : sq.lk - 1;
+    const T* qp = (const T*)p.q + at.t * a.q_row + at.h * a.q_head;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) qf[qb][c] = on ? load_chunk(qp + 32 * c + 8 * j) : zero_chunk(CT{});
+    mx[qb] = kNegInf;
+    ls[qb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // the workgroup's keys: its split's, cut behind the last key that its last query sees
+  int k_lo, k_hi;
+  split_range(sq.lk, p.nsplit, blockIdx.z, KT, k_lo, k_hi);
+  const long long plast = min(p0 + R, rows) - 1;
+  if (p0 >= rows)
+    k_hi = k_lo;
+  else if (a.causal)
+    k_hi = max(min(k_hi, (int)(plast / G) + off + 1), k_lo);
+  // keys up to here are seen by every query of this wave
+  const long long wfirst = p0 + wid * QB * 16;
+  const int all = wfirst >= rows ? 0 : a.causal ? min((int)(wfirst / G) + off + 1, sq.lk) : sq.lk;
+
+  const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
+  const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
+  auto issue = [&](int t0, T* kd, T* vd) {
+    TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
+    TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
+  };
+  auto step = [&](int t0, const T* kc, const T* vc, T* kn, T* vn) {
+    vm_drain();
+    __syncthreads();
+    if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
+    f32x4 s[QB][KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const CT kf = row_frag<HD>(kc, kb * 16 + r, 4 * c + j);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          s[qb][kb] = mma(kf, qf[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qb][kb]);
+      }
+    const bool mask = t0 + KT > all;
+    CT pf[QB][KB / 2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float tmax = kNegInf;
+      if (mask) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[qb][kb][i] = t0 + kb * 16 + 4 * j + i <= lim[qb] ? s[qb][kb][i] : kNegInf;
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, s[qb][kb][i]);
+      // the reference maximum moves only when a score exceeds it by 2^kRescale
+      if (__builtin_amdgcn_ballot_w64(tmax * p.sl2 > mx[qb] + kRescale)) {
+        tmax = col_max(tmax) * p.sl2;
+        const bool raise = tmax > mx[qb] + kRescale;
+        const float mnew = raise ? tmax : mx[qb];
+        const float alpha = raise ? fast_exp2(mx[qb] - mnew) : 1.0f;
+        mx[qb] = mnew;
+        ls[qb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[qb][db] *= alpha;
+      }
+      const float mref = mx[qb] == kNegInf ? 0.f : mx[qb];
+#pragma unroll
+      for (int kp = 0; kp < KB / 2; ++kp) {
+        float v8[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v8[i] = fast_exp2(__builtin_fmaf(s[qb][2 * kp][i], p.sl2, -mref));
+          v8[4 + i] = fast_exp2(__builtin_fmaf(s[qb][2 * kp + 1][i], p.sl2, -mref));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ls[qb] += v8[i];
+        pf[qb][kp] = make_chunk<T>(v8);
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int kp = 0; kp < KB / 2; ++kp) {
+        const CT vf = col_frag<HD>(vc, 32 * kp, 16 * db, lane);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) o[qb][db] = mma(vf, pf[qb][kp], o[qb][db]);
+      }
+  };
+  if (k_lo < k_hi) {
+    issue(k_lo, ks0, vs0);
+    for (int t0 = k_lo; t0 < k_hi; t0 += 2 * KT) {
+      step(t0, ks0, vs0, ks1, vs1);
+      if (t0 + KT < k_hi) step(t0 + KT, ks1, vs1, ks0, vs0);
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    if (pr[qb] >= ext) continue;
+    const RowAt at = packed_row(sq, hk, G, pr[qb]);
+    if (p.nsplit > 1) {
+      const float l = col_sum(ls[qb]);
+      if (pr[qb] >= rows) continue;
+      const long long row = ((long long)blockIdx.z * a.total_q + at.t) * a.heads + at.h;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store4(p.part + row * HD + 16 * db + 4 * j, o[qb][db], 1.f);
+      if (j == 0) p.ml[row] = make_float2(mx[qb], l);
+    } else {
+      const float l = col_sum(ls[qb]);
+      if (pr[qb] >= rows && !a.zero_rest) continue;
+      const bool any = pr[qb] < rows && !(l == 0.f);   // a sum of NaN stays one
+      const float inv = any ? 1.0f / l : 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        store4(out + at.t * a.o_row + at.h * a.o_head + 16 * db + 4 * j, any ? o[qb][db] : f32x4{0.f, 0.f, 0.f, 0.f}, inv);
+      if (j == 0) p.lse[at.h * a.total_q + at.t] = any ? (mx[qb] + log2f(l)) * kLn2 : kNegInf;
+    }
+  }
+}
+
+// Joins the splits of a row: o = sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z. HD / 4 threads
+// per (query row, head); rows of no sequence are left, or zeroed.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) packed_join_kernel(FwdP p) {
+  constexpr int TPR = HD / 4;
+  const AttnArgs& a = p.a;
+  const long long row = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int c = 4 * (threadIdx.x % TPR);
+  if (row >= a.total_q * a.heads) return;
+  const long long t = row / a.heads;
+  const int h = (int)(row - t * a.heads);
+  const bool in = t < p.cu_q[a.seqs];
+  if (!in && !a.zero_rest) return;
+  float m = kNegInf, l = 0.f;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  if (in) {
+    const long long per = a.total_q * a.heads;
+    for (int z = 0; z < p.nsplit; ++z) m = fmaxf(m, p.ml[z * per + row].x);
+    const float mref = m == kNegInf ? 0.f : m;
+    for (int z = 0; z < p.nsplit; ++z) {
+      const float2 ml = p.ml[z * per + row];
+      const float w = fast_exp2(ml.x - mref);
+      l += w * ml.y;
+      acc += w * *reinterpret_cast<const f32x4*>(p.part + (z * per + row) * HD + c);
+    }
+  }
+  const bool any = !(l == 0.f);
+  store4((T*)p.o + t * a.o_row + h * a.o_head + c, any ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, any ? 1.0f / l : 0.f);
+  if (c == 0) p.lse[h * a.total_q + t] = any ? (m + log2f(l)) * kLn2 : kNegInf;
+}
+
+// ---- backward ----
+
+struct BwdP {
+  AttnArgs a;
+  const void *q, *k, *v, *o, *d_o;
+  const float* lse;
+  const int *cu_q, *cu_k, *used_k;
+  void *dq, *dk, *dv;
+  float2* terms;     // [kv_heads][total_q G] packed rows: lse in log2 units (+inf: sees nothing), D
+  float sl2;
+};
+
+// dq, and each row's terms for the key-major pass.
+template <typename T, int HD, int QB>
+__global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
+  constexpr int KT = AttnTile<T>::keys, NCH = HD / 32, DB = HD / 16, R = 16 * QB * kWaves;
+  typedef typename Chunk<T>::type CT;
+  __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
+  const AttnArgs& a = p.a;
+  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, j = lane >> 4;
+  const Seq sq = find_seq(blockIdx.x, p.cu_q, G, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
+  const long long rows = (long long)sq.lq * G, ext = (long long)sq.eq * G;
+  const long long nt = (rows + R - 1) / R;
+  const long long tile = sq.tile < nt ? nt - 1 - sq.tile : sq.tile;
+  const long long p0 = tile * R;
+  if (p0 < 0 || p0 >= ext || (p0 >= rows && !a.zero_rest)) return;
+
+  long long pr[QB];
+  int lim[QB];
+  CT qf[QB][NCH], df[QB][NCH];
+  f32x4 acc[QB][DB];
+  float l2[QB], dd[QB];
+  const int off = sq.lk - sq.lq;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    pr[qb] = p0 + (wid * QB + qb) * 16 + r;
+    const bool on = pr[qb] < rows;
+    const RowAt at = packed_row(sq, hk, G, on ? pr[qb] : 0);
+    lim[qb] = !on ? -1 : a.causal ? min((int)(at.t - sq.q0) + off, sq.lk - 1) : sq.lk - 1;
+    const T* qp = (const T*)p.q + at.t * a.q_row + at.h * a.q_head;
+    const T* dp = (const T*)p.d_o + at.t * a.do_row + at.h * a.do_head;
+    const T* op = (const T*)p.o + at.t * a.o_row + at.h * a.o_head;
+    float d = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      qf[qb][c] = zero_chunk(CT{});
+      df[qb][c] = zero_chunk(CT{});
+      if (on && lim[qb] >= 0) {
+        qf[qb][c] = load_chunk(qp + 32 * c + 8 * j);
+        df[qb][c] = load_chunk(dp + 32 * c + 8 * j);
+        const CT of = load_chunk(op + 32 * c + 8 * j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d = fmaf((float)df[qb][c][e], (float)of[e], d);
+      }
+    }
+    dd[qb] = col_sum(d);
+    l2[qb] = on && lim[qb] >= 0 ? p.lse[at.h * a.total_q + at.t] * kLog2e : __builtin_huge_valf();
+    if (on && j == 0) p.terms[((long long)hk * a.total_q + sq.q0) * G + pr[qb]] = make_float2(l2[qb], dd[qb]);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const long long plast = min(p0 + R, rows) - 1;
+  const int k_hi = p0 >= rows ? 0 : a.causal ? max(min(sq.lk, (int)(plast / G) + off + 1), 0) : sq.lk;
+  const long long wfirst = p0 + wid * QB * 16;
+  const int all = wfirst >= rows ? 0 : a.causal ? min((int)(wfirst / G) + off + 1, sq.lk) : sq.lk;
+
+  const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
+  const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
+  auto issue = [&](int t0, T* kd, T* vd) {
+    TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
+    TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
+  };
+  auto step = [&](int t0, const T* kc, const T* vc, T* kn, T* vn) {
+    vm_drain();
+    __syncthreads();
+    if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
+    const bool mask = t0 + KT > all;
+#pragma unroll
+    for (int kp = 0; kp < KT / 32; ++kp) {
+      f32x4 s[QB][2], g[QB][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+          const CT kf = row_frag<HD>(kc, kp * 32 + kb * 16 + r, 4 * c + j);
+          const CT vf = row_frag<HD>(vc, kp * 32 + kb * 16 + r, 4 * c + j);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            s[qb][kb] = mma(kf, qf[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qb][kb]);
+            g[qb][kb] = mma(vf, df[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : g[qb][kb]);
+          }
+        }
+      CT ds[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float v8[8];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float pv = fast_exp2(__builtin_fmaf(s[qb][kb][i], p.sl2, -l2[qb]));
+            float x = pv * (g[qb][kb][i] - dd[qb]);
+            if (mask && t0 + kp * 32 + kb * 16 + 4 * j + i > lim[qb]) x = 0.f;
+            v8[4 * kb + i] = x;
+          }
+        ds[qb] = make_chunk<T>(v8);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const CT kt = col_frag<HD>(kc, 32 * kp, 16 * db, lane);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) acc[qb][db] = mma(kt, ds[qb], acc[qb][db]);
+      }
+    }
+  };
+  if (k_hi > 0) {
+    issue(0, ks0, vs0);
+    for (int t0 = 0; t0 < k_hi; t0 += 2 * KT) {
+      step(t0, ks0, vs0, ks1, vs1);
+      if (t0 + KT < k_hi) step(t0 + KT, ks1, vs1, ks0, vs0);
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    if (pr[qb] >= ext || (pr[qb] >= rows && !a.zero_rest)) continue;
+    const RowAt at = packed_row(sq, hk, G, pr[qb]);
+    T* const out = (T*)p.dq + (at.t * a.heads + at.h) * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) store4(out + 16 * db + 4 * j, acc[qb][db], a.scale);
+  }
+}
+
+// dk and dv of 16 KW keys per wave (a lane owns a key column, S = Q K^T), over the packed query
+// rows that see them, in tiles of KT rows.
+template <typename T, int HD, int KW>
+__global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
+  constexpr int QT = AttnTile<T>::keys, NCH = HD / 32, DB = HD / 16, R = 16 * KW * kWaves;
+  typedef typename Chunk<T>::type CT;
+  __shared__ __attribute__((aligned(1024))) T qs0[QT * HD], ds0[QT * HD], qs1[QT * HD], ds1[QT * HD];
+  __shared__ __attribute__((aligned(16))) float2 tm0[QT], tm1[QT];
+  const AttnArgs& a = p.a;
+  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, j = lane >> 4;
+  const Seq sq = find_seq(blockIdx.x, p.cu_k, 1, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
+  const long long k0 = sq.tile * R;
+  if (k0 < 0 || k0 >= sq.ek || (k0 >= sq.lk && !a.zero_rest)) return;
+  const long long rows = (long long)sq.lq * G;
+  const int off = sq.lk - sq.lq;
+
+  int key[KW];
+  long long first[KW];     // the first packed row that sees this lane's key
+  CT kf[KW][NCH], vf[KW][NCH];
+  f32x4 dk[KW][DB], dv[KW][DB];
+#pragma unroll
+  for (int w = 0; w < KW; ++w) {
+    key[w] = (int)k0 + (wid * KW + w) * 16 + r;
+    const bool on = key[w] < sq.lk;
+    first[w] = !on ? rows : a.causal ? max((long long)(key[w] - off), 0LL) * G : 0;
+    const long long row = sq.k0 + (on ? key[w] : 0);
+    const T* kp = (const T*)p.k + row * a.k_row + hk * a.k_head;
+    const T* vp = (const T*)p.v + row * a.v_row + hk * a.v_head;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      kf[w][c] = on ? load_chunk(kp + 32 * c + 8 * j) : zero_chunk(CT{});
+      vf[w][c] = on ? load_chunk(vp + 32 * c + 8 * j) : zero_chunk(CT{});
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      dk[w][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+      dv[w][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // rows from here on are seen by every key of the wave (causal: by its last)
+  const long long wkey = k0 + (wid * KW + KW) * 16 - 1;
+  const long long all = wkey >= sq.lk ? rows : a.causal ? max(wkey - off, 0LL) * G : 0;
+  const long long p_lo = k0 >= sq.lk ? rows : a.causal ? max(k0 - off, 0LL) * G / QT * QT : 0;
+
+  // tile rows are packed rows: query and head vary by row
+  auto issue = [&](long long t0, T* qd, T* dd, float2* td) {
+    PackedLoad<T, HD, QT>::issue(qd, (const T*)p.q, a.q_row, a.q_head, sq, hk, G, t0, rows, wid, lane);
+    PackedLoad<T, HD, QT>::issue(dd, (const T*)p.d_o, a.do_row, a.do_head, sq, hk, G, t0, rows, wid, lane);
+    if (threadIdx.x < QT)
+      td[threadIdx.x] = t0 + threadIdx.x < rows ? p.terms[((long long)hk * a.total_q + sq.q0) * G + t0 + threadIdx.x]
+                                                : make_float2(__builtin_huge_valf(), 0.f);
+  };
+  auto step = [&](long long t0, const T* qc, const T* dc, const float2* tc, T* qn, T* dn, float2* tn) {
+    vm_drain();
+    __syncthreads();
+    if (t0 + QT < rows) issue(t0 + QT, qn, dn, tn);
+    const bool mask = t0 < all || t0 + QT > rows;
+#pragma unroll
+    for (int qp = 0; qp < QT / 32; ++qp) {
+      CT pf[KW], sf[KW];
+      f32x4 s[KW][2], g[KW][2];
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+          const CT qf = row_frag<HD>(qc, qp * 32 + qb * 16 + r, 4 * c + j);
+          const CT df = row_frag<HD>(dc, qp * 32 + qb * 16 + r, 4 * c + j);
+#pragma unroll
+          for (int w = 0; w < KW; ++w) {
+            s[w][qb] = mma(qf, kf[w][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[w][qb]);
+            g[w][qb] = mma(df, vf[w][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : g[w][qb]);
+          }
+        }
+      float2 tt[2][4];
+#pragma unroll
+      for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tt[qb][i] = tc[qp * 32 + qb * 16 + 4 * j + i];
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        float p8[8], s8[8];
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float pv = fast_exp2(__builtin_fmaf(s[w][qb][i], p.sl2, -tt[qb][i].x));
+            float x = pv * (g[w][qb][i] - tt[qb][i].y);
+            if (mask) {
+              const long long row = t0 + qp * 32 + qb * 16 + 4 * j + i;
+              const bool see = row >= first[w] && row < rows;
+              pv = see ? pv : 0.f;
+              x = see ? x : 0.f;
+            }
+            p8[4 * qb + i] = pv;
+            s8[4 * qb + i] = x;
+          }
+        pf[w] = make_chunk<T>(p8);
+        sf[w] = make_chunk<T>(s8);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const CT dt = col_frag<HD>(dc, 32 * qp, 16 * db, lane);
+        const CT qt = col_frag<HD>(qc, 32 * qp, 16 * db, lane);
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          dv[w][db] = mma(dt, pf[w], dv[w][db]);
+          dk[w][db] = mma(qt, sf[w], dk[w][db]);
+        }
+      }
+    }
+  };
+  if (p_lo < rows) {
+    issue(p_lo, qs0, ds0, tm0);
+    for (long long t0 = p_lo; t0 < rows; t0 += 2 * QT) {
+      step(t0, qs0, ds0, tm0, qs1, ds1, tm1);
+      if (t0 + QT < rows) step(t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
+    }
+  }
+#pragma unroll
+  for (int w = 0; w < KW; ++w) {
+    if (key[w] >= sq.ek || (key[w] >= sq.lk && !a.zero_rest)) continue;
+    const long long row = ((sq.k0 + key[w]) * a.kv_heads + hk) * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      store4((T*)p.dk + row + 16 * db + 4 * j, dk[w][db], a.scale);
+      store4((T*)p.dv + row + 16 * db + 4 * j, dv[w][db], 1.f);
+    }
+  }
+}
+
+// ---- host ----
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+unsigned tile_slots(long long total, int mult, int R, int S) { return (unsigned)(total * mult / R + S); }
+
+// Splits of the key axis: where the row tiles leave CUs idle, up to two workgroups per CU with
+// at least 256 keys of an average sequence each.
+int fwd_splits(const AttnArgs& a, int R) {
+  const long long tiles = (a.total_q * a.group() / R + a.seqs) * a.kv_heads;
+  const long long avg = a.total_k / std::max(a.seqs, 1);
+  long long s = std::min<long long>(std::max<long long>(512 / std::max<long long>(tiles, 1), 1), avg / 256);
+  return (int)std::max<long long>(std::min<long long>(s, 64), 1);
+}
+
+constexpr int kFwdQB = 2;
+
+template <typename T, int HD>
+hipError_t attn_fwd(FwdP p, hipStream_t st) {
+  constexpr int R = 16 * kFwdQB * kWaves;
+  const AttnArgs& a = p.a;
+  const dim3 grid(tile_slots(a.total_q, a.group(), R, a.seqs), a.kv_heads, p.nsplit);
+  packed_fwd_kernel<T, HD, kFwdQB><<<grid, 64 * kWaves, 0, st>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const long long n = a.total_q * a.heads, per = 256 / (HD / 4);
+  packed_join_kernel<T, HD><<<(unsigned)((n + per - 1) / per), 256, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t attn_bwd(BwdP p, hipStream_t st) {
+  constexpr int QB = HD == 128 ? 1 : 2, KW = 1;
+  const AttnArgs& a = p.a;
+  if (a.total_q > 0) {
+    packed_dq_kernel<T, HD, QB>
+        <<<dim3(tile_slots(a.total_q, a.group(), 16 * QB * kWaves, a.seqs), a.kv_heads), 64 * kWaves, 0, st>>>(p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.total_k > 0) {
+    packed_dkv_kernel<T, HD, KW>
+        <<<dim3(tile_slots(a.total_k, 1, 16 * KW * kWaves, a.seqs), a.kv_heads), 64 * kWaves, 0, st>>>(p);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+#define BSA_ATTN_DISPATCH(FN, a, ...)                                                                       \
+  ((a).bf16 ? ((a).hd == 128  ? FN<bf16_t, 128>(__VA_ARGS__)                                                \
+               : (a).hd == 64 ? FN<bf16_t, 64>(__VA_ARGS__)                                                 \
+                              : FN<bf16_t, 32>(__VA_ARGS__))                                                \
+            : ((a).hd == 128  ? FN<float, 128>(__VA_ARGS__)                                                 \
+               : (a).hd == 64 ? FN<float, 64>(__VA_ARGS__)                                                  \
+                              : FN<float, 32>(__VA_ARGS__)))
+
+}  // namespace
+
+size_t attention_fwd_ws_bytes(const AttnArgs& a) {
+  const int s = fwd_splits(a, 16 * kFwdQB * kWaves);
+  if (s == 1) return 0;
+  const size_t rows = (size_t)s * a.total_q * a.heads;
+  return align256(rows * a.hd * sizeof(float)) + align256(rows * sizeof(float2));
+}
+
+hipError_t launch_attention_fwd(const AttnArgs& a, const void* q, const void* k, const void* v, const int* cu_q,
+                                const int* cu_k, const int* used_k, void* o, float* lse, void* ws, hipStream_t st) {
+  if (a.total_q == 0) return hipSuccess;
+  FwdP p{a, q, k, v, cu_q, cu_k, used_k, o, lse, a.scale * kLog2e, fwd_splits(a, 16 * kFwdQB * kWaves), nullptr, nullptr};
+  if (p.nsplit > 1) {
+    p.part = (float*)ws;
+    p.ml = (float2*)((char*)ws + align256((size_t)p.nsplit * a.total_q * a.heads * a.hd * sizeof(float)));
+  }
+  return BSA_ATTN_DISPATCH(attn_fwd, a, p, st);
+}
+
+size_t attention_bwd_ws_bytes(const AttnArgs& a) { return align256(sizeof(float2) * (size_t)a.total_q * a.heads); }
+
+hipError_t launch_attention_bwd(const AttnArgs& a, const void* q, const void* k, const void* v, const void* o,
+                                const float* lse, const void* d_o, const int* cu_q, const int* cu_k, const int* used_k,
+                                void* dq, void* dk, void* dv, void* ws, hipStream_t st) {
+  BwdP p{a, q, k, v, o, d_o, lse, cu_q, cu_k, used_k, dq, dk, dv, (float2*)ws, a.scale * kLog2e};
+  return BSA_ATTN_DISPATCH(attn_bwd, a, p, st);
+}
+
+}  // namespace bsa

@@ -1,0 +1,452 @@
+// Affine map with an epilogue and its gradients:
+//   z = x w^T + bias, y = act(z) + res;   dz = dy act'(z), dx = dz w, dw = dz^T x, db = sum dz.
+// The three products are C[M, N] = sum_k A(m, k) B(n, k) with each operand stored either with
+// the contraction index fastest ("row" form: x and w of the forward, dz of dx) or with the
+// output index fastest ("column" form: w of dx, both operands of dw). bf16 operands feed the
+// bf16 matrix cores, f32 operands the f32 ones; sums, bias, activation and residual are
+// float32, rounded once to the storage type.
+#include <algorithm>
+
+#include "common.hpp"
+#include "dense.hpp"
+#include "dense_common.hpp"
+#include "gemm_common.hpp"
+
+namespace bsa {
+namespace {
+
+// ---- activations ----
+
+__device__ __forceinline__ float gelu_cdf(float z) { return 0.5f * erfcf(-z * 0.70710678118654752f); }
+
+__device__ __forceinline__ float act_fwd(float z, int act) {
+  switch (act) {
+    case kActRelu: return z > 0.f ? z : z != z ? z : 0.f;
+    case kActGelu: return z * gelu_cdf(z);
+    case kActSilu: return z * sigmoid(z);
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+  switch (act) {
+    case kActRelu: return z > 0.f ? 1.f : 0.f;
+    case kActGelu: return fmaf(z, __expf(-0.5f * z * z) * 0.39894228040143268f, gelu_cdf(z));
+    case kActSilu: {
+      const float s = sigmoid(z);
+      return s * fmaf(z, 1.f - s, 1.f);
+    }
+    default: return 1.f;
+  }
+}
+
+// ---- epilogue ----
+
+template <typename T>
+struct Epi {
+  long long M;
+  int N;
+  T* out;
+  long long ldo;
+  const T* bias;      // [N] or NULL
+  const T* res;       // [M, ldr] or NULL
+  long long ldr;
+  T* pre;             // [M, N] or NULL: z in the storage type
+  int act;
+  float* part;        // not NULL: the bare sums go to part[split][M][N] instead
+};
+
+// Four (EN) consecutive columns n.. of row m.
+template <typename T, int EN>
+__device__ __forceinline__ void epi_store(const Epi<T>& o, long long m, int n, float (&v)[EN], int split) {
+  if (m >= o.M || n >= o.N) return;
+  if (o.part) {
+    float* p = o.part + ((long long)split * o.M + m) * o.N + n;
+#pragma unroll
+    for (int e = 0; e < EN; ++e)
+      if (n + e < o.N) p[e] = v[e];
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < EN; ++e) {
+    if (n + e < o.N) {
+      float z = v[e];
+      if (o.bias) z += to_f32<T>(o.bias[n + e]);
+      if (o.pre) o.pre[m * o.N + n + e] = from_f32<T>(z);
+      z = act_fwd(z, o.act);
+      if (o.res) z += to_f32<T>(o.res[m * o.ldr + n + e]);
+      o.out[m * o.ldo + n + e] = from_f32<T>(z);
+    }
+  }
+}
+
+// ---- products, any shape: tiles staged through registers ----
+
+// A stored matrix (rows x cols, leading dimension ld); in column form its rows are the
+// contraction index.
+template <typename T>
+struct Mat {
+  const T* p;
+  long long ld;
+  long long rows;
+  int cols;
+};
+
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const Mat<T>& m, long long r, int c) {
+  constexpr int E = 16 / (int)sizeof(T);
+  if (r >= m.rows || c >= m.cols) return make_uint4(0, 0, 0, 0);
+  const T* p = m.p + r * m.ld + c;
+  return c + E <= m.cols ? load16u(p) : load_partial(p, m.cols - c);
+}
+
+// LDS tile of R operand rows x BK contraction indices, in the operand's own order: row form
+// [R][BK], column form [BK][R] (f32: 4 elements of padding a row). 16-byte pieces are
+// swizzled, except in the column form of f32, which is read element by element.
+template <typename T, bool TR, int R, int BK>
+struct RegTile {
+  static constexpr int E = 16 / (int)sizeof(T);
+  static constexpr int COLS = TR ? R : BK, ROWS = TR ? BK : R;
+  static constexpr int CPR = COLS / E;
+  static constexpr bool F32T = TR && sizeof(T) == 4;
+  static constexpr int LD = COLS + (F32T ? 4 : 0);
+  static constexpr int NV = ROWS * CPR / 256;
+  static constexpr int SIZE = ROWS * LD;
+  static_assert(NV * 256 == ROWS * CPR, "tile / thread split");
+
+  __device__ static int swz(int row) { return F32T ? 0 : CPR == 4 ? (row >> 1) & 3 : CPR == 8 ? row & 7 : 2 * (row & 7); }
+  // o0: first operand row of the tile, k0: first contraction index
+  __device__ static void load(uint4 (&v)[NV], const Mat<T>& m, long long o0, long long k0) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int i = threadIdx.x + 256 * u, row = i / CPR, c = (i % CPR) * E;
+      v[u] = TR ? load_piece(m, k0 + row, (int)o0 + c) : load_piece(m, o0 + row, (int)k0 + c);
+    }
+  }
+  __device__ static void store(const uint4 (&v)[NV], T* t) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int i = threadIdx.x + 256 * u, row = i / CPR, c = i % CPR;
+      *reinterpret_cast<uint4*>(t + row * LD + E * (c ^ swz(row))) = v[u];
+    }
+  }
+  // Fragment of operand rows r0 + lane % 16 at contraction step ks (32 indices). PAIRS: the
+  // order of the transposing reads (4j.., 16 + 4j..), for a bf16 operand whose partner is in
+  // column form; else 8j...
+  template <bool PAIRS>
+  __device__ static typename Chunk<T>::type frag(const T* t, int r0, int ks, int lane) {
+    const int r = r0 + (lane & 15), j = lane >> 4;
+    if constexpr (!TR) {
+      const T* row = t + r * LD;
+      auto piece = [&](int c) { return *reinterpret_cast<const uint4*>(row + E * (c ^ swz(r))); };
+      if constexpr (sizeof(T) == 4) {
+        const uint4 a = piece(8 * ks + 2 * j), b = piece(8 * ks + 2 * j + 1);
+        return f32x8{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                     __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+      } else if constexpr (PAIRS) {
+        auto half = [&](int c) {
+          return *reinterpret_cast<const uint2*>(row + E * (c ^ swz(r)) + 4 * (j & 1));
+        };
+        const uint2 a = half(4 * ks + j / 2), b = half(4 * ks + 2 + j / 2);
+        return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+      } else {
+        return __builtin_bit_cast(bf16x8, piece(4 * ks + j));
+      }
+    } else if constexpr (sizeof(T) == 4) {
+      f32x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = t[(32 * ks + 8 * j + e) * LD + r];
+      return v;
+    } else {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const int p = lane & 15, col = r0 + 4 * (p & 3);
+      const int x0 = 32 * ks + 4 * j + (p >> 2), x1 = x0 + 16;
+      const T* a0 = t + x0 * LD + 8 * ((col >> 3) ^ swz(x0)) + (col & 7);
+      const T* a1 = t + x1 * LD + 8 * ((col >> 3) ^ swz(x1)) + (col & 7);
+      const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a0));
+      const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a1));
+      return __builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y));
+    }
+  }
+};
+
+// 4 waves in a 2 x 2 arrangement; the next tile is in registers while one is multiplied.
+// Accumulator lane L holds C[m + L % 16][n + 4 (L / 16) + e] (B's fragment comes first).
+template <typename T, bool TA, bool TB, int BM, int BN>
+__global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long long K, int ntn, long long kt_per, Epi<T> o) {
+  constexpr int BK = 32, FI = BM / 32, FJ = BN / 32;
+  typedef RegTile<T, TA, BM, BK> LA;
+  typedef RegTile<T, TB, BN, BK> LB;
+  __shared__ __attribute__((aligned(16))) T as[LA::SIZE], bs[LB::SIZE];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wm = wid >> 1, wn = wid & 1;
+  const int tm = blockIdx.x / ntn, tn = blockIdx.x - tm * ntn;
+  const long long m0 = (long long)tm * BM;
+  const int n0 = tn * BN;
+  const long long nkt = (K + BK - 1) / BK;
+  const long long kt0 = blockIdx.y * kt_per, kt1 = kt0 + kt_per < nkt ? kt0 + kt_per : nkt;
+  f32x4 acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint4 av[LA::NV], bv[LB::NV];
+  if (kt0 < kt1) {
+    LA::load(av, a, m0, kt0 * BK);
+    LB::load(bv, b, n0, kt0 * BK);
+  }
+  for (long long kt = kt0; kt < kt1; ++kt) {
+    __syncthreads();
+    LA::store(av, as);
+    LB::store(bv, bs);
+    __syncthreads();
+    if (kt + 1 < kt1) {
+      LA::load(av, a, m0, (kt + 1) * BK);
+      LB::load(bv, b, n0, (kt + 1) * BK);
+    }
+    typename Chunk<T>::type af[FI], bf[FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i) af[i] = LA::template frag<TB>(as, wm * (BM / 2) + 16 * i, 0, lane);
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) bf[j] = LB::template frag<TA>(bs, wn * (BN / 2) + 16 * j, 0, lane);
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bf[j], af[i], acc[i][j]);
+  }
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) {
+      float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+      epi_store<T, 4>(o, m0 + wm * (BM / 2) + 16 * i + (lane & 15), n0 + wn * (BN / 2) + 16 * j + 4 * (lane >> 4), v,
+                      blockIdx.y);
+    }
+}
+
+// y = epilogue(sum over the splits, in order), four columns per thread
+template <typename T>
+__global__ void __launch_bounds__(256) split_sum_kernel(const float* __restrict__ part, int S, Epi<T> o) {
+  const int nq = (o.N + 3) / 4;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= o.M * nq) return;
+  const long long m = i / nq;
+  const int n = (int)(i - m * nq) * 4;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < S; ++s) {
+    const float* p = part + ((long long)s * o.M + m) * o.N + n;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < o.N) v[e] += p[e];
+  }
+  epi_store<T, 4>(o, m, n, v, 0);
+}
+
+// ---- dz = dy act'(z) and the partial column sums of dz ----
+
+// 32 column pieces x 8 rows at a time; workgroup (x, y) takes rows y rpg .. and leaves the sums
+// of its columns in part[y][n]. dz == NULL: only the sums; part == NULL: only dz.
+template <typename T>
+__global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ pre,
+                                                 int act, long long m, int n, long long rpg, T* __restrict__ dz,
+                                                 float* __restrict__ part) {
+  constexpr int E = 16 / (int)sizeof(T);
+  __shared__ float red[8][32 * E + 4];
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+  const int c = (blockIdx.x * 32 + cx) * E;
+  const long long r0 = blockIdx.y * rpg, r1 = r0 + rpg < m ? r0 + rpg : m;
+  float s[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s[e] = 0.f;
+  if (c < n) {
+    const Mat<T> my{dy, lddy, m, n}, mz{pre, n, m, n};
+#pragma unroll 2
+    for (long long r = r0 + ry; r < r1; r += 8) {
+      float v[E];
+      unpack16<T>(load_piece(my, r, c), v);
+      if (dz) {
+        float z[E];
+        unpack16<T>(load_piece(mz, r, c), z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= act_slope(z[e], act);
+        T* p = dz + r * n + c;
+        if (c + E <= n)
+          store16u(p, pack16<T>(v));
+        else
+          store_partial(p, pack16<T>(v), n - c);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[e] += v[e];
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) red[ry][cx * E + e] = s[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * E; i += 256) {
+    float v = red[0][i];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += red[k][i];
+    const int col = blockIdx.x * 32 * E + i;
+    if (col < n) part[(long long)blockIdx.y * n + col] = v;
+  }
+}
+
+// out = sum over P rows of part [P][n], in the storage type: wave w takes rows w, w + 16, ...
+template <typename T>
+__global__ void __launch_bounds__(1024) db_sum_kernel(const float* __restrict__ part, int P, int n, T* __restrict__ out) {
+  __shared__ float red[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (c < n)
+    for (int i = w; i < P; i += 16) s += part[(long long)i * n + c];
+  red[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && c < n) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += red[k][lane];
+    out[c] = from_f32<T>(s);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) fill_zero_kernel(T* p, long long n) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = from_f32<T>(0.f);
+}
+
+// ---- host ----
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Splits of a product's contraction: while the 128 x 128 tiles leave CUs idle, at least 8
+// contraction tiles each.
+int product_splits(long long M, int N, long long K) {
+  const long long tiles = ((M + 127) / 128) * ((N + 127) / 128), nkt = (K + 31) / 32;
+  int s = 1;
+  while (tiles * s < 256 && nkt / (2 * s) >= 8 && s < 64) s *= 2;
+  return s;
+}
+
+// C = A B^T with the epilogue; S > 1: partial sums in part, joined by split_sum_kernel
+template <typename T, bool TA, bool TB>
+hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long long K, int S, float* part, Epi<T> o,
+                   hipStream_t st) {
+  const long long nkt = (K + 31) / 32, per = (nkt + S - 1) / S;
+  o.part = S > 1 ? part : nullptr;
+  const long long big = ((M + 127) / 128) * ((N + 127) / 128) * S;
+  if (big >= 256) {
+    const int ntn = (N + 127) / 128;
+    const dim3 grid((unsigned)(((M + 127) / 128) * ntn), (unsigned)S);
+    product_kernel<T, TA, TB, 128, 128><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
+  } else {
+    const int ntn = (N + 63) / 64;
+    const dim3 grid((unsigned)(((M + 63) / 64) * ntn), (unsigned)S);
+    product_kernel<T, TA, TB, 64, 64><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || S == 1) return e;
+  o.part = nullptr;
+  const long long n4 = M * ((N + 3) / 4);
+  split_sum_kernel<T><<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(part, S, o);
+  return hipGetLastError();
+}
+
+struct LinBwdWs {
+  size_t dz, dbp, part, total;
+  int S, P;
+  long long rpg;
+};
+LinBwdWs linear_bwd_layout(const LinearArgs& a) {
+  LinBwdWs L{};
+  const size_t esz = a.bf16 ? 2 : 4;
+  const int E = 16 / (int)esz;
+  size_t off = 0;
+  auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
+  L.S = product_splits(a.n, a.k, a.m);
+  // row groups of the dz pass: about 1024 workgroups, at least 32 rows each
+  const long long gx = (a.n + 32 * E - 1) / (32 * E);
+  long long P = std::min<long long>(std::max<long long>(1024 / gx, 1), (a.m + 31) / 32);
+  P = std::max<long long>(std::min<long long>(P, 256), 1);
+  L.rpg = (a.m + P - 1) / P;
+  L.P = (int)(L.rpg ? (a.m + L.rpg - 1) / L.rpg : 1);
+  L.dz = put(a.act == kActNone ? 0 : esz * (size_t)a.m * a.n);
+  L.dbp = put(sizeof(float) * (size_t)L.P * a.n);
+  L.part = put(L.S > 1 ? sizeof(float) * (size_t)L.S * a.n * a.k : 0);
+  L.total = off;
+  return L;
+}
+
+template <typename T>
+hipError_t linear_fwd(const LinearArgs& a, const void* x, const void* w, const void* bias, const void* res, void* y,
+                      void* pre, void* ws, hipStream_t st) {
+  Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, (const T*)res, a.ldr, (T*)pre, a.act, nullptr};
+  return product<T, false, false>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.n,
+                                  a.k, 1, (float*)ws, o, st);
+}
+
+template <typename T>
+hipError_t zero(T* p, long long n, hipStream_t st) {
+  fill_zero_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p, n);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t linear_bwd(const LinearArgs& a, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                      void* dw, void* db, void* ws, hipStream_t st) {
+  if (a.m == 0) {   // empty sums
+    hipError_t e = hipSuccess;
+    if (dw) e = zero((T*)dw, (long long)a.n * a.k, st);
+    if (e == hipSuccess && db) e = zero((T*)db, a.n, st);
+    return e;
+  }
+  constexpr int E = 16 / (int)sizeof(T);
+  const LinBwdWs L = linear_bwd_layout(a);
+  char* c = (char*)ws;
+  T* const dz = a.act == kActNone ? nullptr : (T*)(c + L.dz);
+  float* const dbp = db ? (float*)(c + L.dbp) : nullptr;
+  if (dz || dbp) {
+    dz_kernel<T><<<dim3((a.n + 32 * E - 1) / (32 * E), L.P), 256, 0, st>>>((const T*)dy, a.lddy, (const T*)pre, a.act,
+                                                                           a.m, a.n, L.rpg, dz, dbp);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const Mat<T> mz{dz ? dz : (const T*)dy, dz ? a.n : a.lddy, a.m, a.n};
+  if (dx) {
+    Epi<T> o{a.m, a.k, (T*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
+    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n, 1, nullptr, o, st);
+    if (e != hipSuccess) return e;
+  }
+  if (dw) {
+    Epi<T> o{a.n, a.k, (T*)dw, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
+    hipError_t e = product<T, true, true>(mz, Mat<T>{(const T*)x, a.ldx, a.m, a.k}, a.n, a.k, a.m, L.S,
+                                          (float*)(c + L.part), o, st);
+    if (e != hipSuccess) return e;
+  }
+  if (db) {
+    db_sum_kernel<T><<<(a.n + 63) / 64, 1024, 0, st>>>(dbp, L.P, a.n, (T*)db);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t linear_fwd_ws_bytes(const LinearArgs&) { return 0; }
+
+hipError_t launch_linear_fwd(const LinearArgs& a, const void* x, const void* w, const void* bias, const void* res,
+                             void* y, void* pre, void* ws, hipStream_t st) {
+  if (a.m == 0) return hipSuccess;
+  return a.bf16 ? linear_fwd<bf16_t>(a, x, w, bias, res, y, pre, ws, st)
+                : linear_fwd<float>(a, x, w, bias, res, y, pre, ws, st);
+}
+
+size_t linear_bwd_ws_bytes(const LinearArgs& a) { return linear_bwd_layout(a).total; }
+
+hipError_t launch_linear_bwd(const LinearArgs& a, const void* x, const void* w, const void* pre, const void* dy,
+                             void* dx, void* dw, void* db, void* ws, hipStream_t st) {
+  return a.bf16 ? linear_bwd<bf16_t>(a, x, w, pre, dy, dx, dw, db, ws, st)
+                : linear_bwd<float>(a, x, w, pre, dy, dx, dw, db, ws, st);
+}
+
+}  // namespace bsa

@@ -1,0 +1,455 @@
+"""Layer norm, affine map and packed attention on the GPU against their float64 definitions, within
+bounds derived from the types (tests/dense_ref.py)."""
+import math
+
+import pytest
+import torch
+
+import dense_ref as ref
+from paper_2506_12541_amd import dense
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+DT = {"bf16": BF, "f32": F32}
+
+
+def gen(seed):
+    g = torch.Generator("cpu")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, dtype=F32, scale=1.0, shift=0.0):
+    return (torch.randn(shape, generator=g) * scale + shift).to(dtype).cuda()
+
+
+def rows_apart(t, ld):
+    """The same rows with `ld` elements between them."""
+    buf = torch.full((t.shape[0], ld), float("nan"), dtype=t.dtype, device=t.device)
+    buf[:, :t.shape[1]] = t
+    return buf[:, :t.shape[1]]
+
+
+# ---- layer norm ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 64), (300, 128), (33, 129), (64, 200), (1, 512), (700, 333),
+                                       (9, 1000), (37, 2048), (6, 2049), (3, 4096), (2, 8192), (5, 8191), (2, 16384),
+                                       (3, 20001), (2, 32768)])
+def test_layernorm(dtype, rows, cols):
+    g = gen(rows * 7 + cols)
+    x, dy = normal(g, rows, cols, dtype=DT[dtype], scale=1.5, shift=0.7), normal(g, rows, cols, dtype=DT[dtype])
+    gain, bias = normal(g, cols, scale=0.2, shift=1.0), normal(g, cols, scale=0.2)
+    want = ref.layernorm(x.cpu(), gain.cpu(), bias.cpu(), 1e-5, dy.cpu())
+    y, mean, rstd = dense.layernorm_forward(x, gain, bias)
+    got = dict(dense.layernorm_backward(x, gain, mean, rstd, dy), y=y, mean=mean, rstd=rstd)
+    for name, (value, bound) in want.items():
+        ref.check(name, got[name], value, bound)
+
+
+def test_layernorm_many_rows_strides_and_shapes():
+    g = gen(1)
+    x = normal(g, 40000, 96, dtype=BF, shift=3.0)
+    dy = normal(g, 40000, 96, dtype=BF)
+    gain = normal(g, 96)
+    want = ref.layernorm(x.cpu(), gain.cpu(), None, 1e-3, dy.cpu())
+    y, mean, rstd = dense.layernorm_forward(x, gain, eps=1e-3)
+    a = dense.layernorm_backward(x, gain, mean, rstd, dy, bias=False)
+    assert a["dbias"] is None
+    for name, t in (("y", y), ("dx", a["dx"]), ("dgain", a["dgain"])):
+        ref.check(name, t, *want[name])
+    # odd distances between rows, whose addresses no vector type is aligned to, and more dimensions
+    ys, ms, rs = dense.layernorm_forward(rows_apart(x, 101), gain, eps=1e-3)
+    b = dense.layernorm_backward(rows_apart(x, 101), gain, ms, rs, rows_apart(dy, 99), bias=False)
+    assert torch.equal(ys, y) and torch.equal(b["dx"], a["dx"]) and torch.equal(b["dgain"], a["dgain"])
+    y3, m3, _ = dense.layernorm_forward(x.view(40, 1000, 96), gain, eps=1e-3)
+    assert y3.shape == (40, 1000, 96) and m3.shape == (40, 1000) and torch.equal(y3.view_as(y), y)
+
+
+def test_layernorm_constant_rows_no_rows_and_values_that_are_not_finite():
+    gain = torch.ones(48, device="cuda")
+    x = torch.full((4, 48), 5.0, device="cuda")
+    x[1, 3] = float("nan")
+    x[2, 3] = float("inf")
+    y, mean, rstd = dense.layernorm_forward(x, gain, gain)
+    assert torch.equal(y[0], gain) and torch.equal(y[3], gain)       # (x - mean) = 0
+    assert y[1].isnan().all() and y[2].isnan().all()                 # as the formula gives
+    assert rstd[0].item() == pytest.approx(1 / math.sqrt(1e-5), rel=1e-6)
+    e = x[:0]
+    y, mean, rstd = dense.layernorm_forward(e, gain)
+    got = dense.layernorm_backward(e, gain, mean, rstd, e)
+    assert y.shape == (0, 48) and not got["dgain"].any() and not got["dbias"].any()
+
+
+# ---- affine map ----
+
+def check_linear(g, dtype, m, k, n, act, bias, residual, train=True, x=None):
+    dt = DT[dtype]
+    x = normal(g, m, k, dtype=dt) if x is None else x
+    w = normal(g, n, k, dtype=dt, scale=1 / math.sqrt(k))
+    b = normal(g, n, dtype=dt) if bias else None
+    r = normal(g, m, n, dtype=dt) if residual else None
+    dy = normal(g, m, n, dtype=dt) if train else None
+    cpu = lambda t: None if t is None else t.cpu()
+    want = ref.linear(x.cpu(), w.cpu(), cpu(b), cpu(r), act, cpu(dy))
+    y, pre = dense.linear_forward(x, w, b, r, act=act, save_pre=train)
+    got = dict(y=y)
+    if train:
+        got.update(dense.linear_backward(x, w, dy, pre, act=act, bias=True))
+    for name, (value, bound) in want.items():
+        ref.check(name, got[name], value, bound)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+def test_linear_epilogues(dtype, act):
+    check_linear(gen(2), dtype, 70, 96, 132, act, True, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(1, 1, 1), (1, 64, 64), (2, 512, 40), (5, 33, 17), (16, 1024, 256), (17, 72, 200),
+                                   (48, 2048, 512), (64, 64, 64), (65, 31, 129), (100, 515, 1029), (128, 128, 128),
+                                   (130, 200, 264), (256, 256, 256), (300, 513, 257), (515, 40, 1000), (1000, 1, 3),
+                                   (2000, 256, 128), (2048, 320, 520)])
+def test_linear_shapes(dtype, m, k, n):
+    check_linear(gen(m + k + n), dtype, m, k, n, "gelu" if m % 2 else "none", n % 2 == 0, m % 3 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_large_tiles(dtype):
+    check_linear(gen(3), dtype, 4100, 192, 2304, "silu", True, True)
+    check_linear(gen(4), dtype, 4096, 256, 4096, "none", False, False, train=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_strides(dtype):
+    """Operands whose rows lie apart, aligned to 16 bytes and not, give the packed operands' bits."""
+    g, dt = gen(5), DT[dtype]
+    x, w, r, dy = (normal(g, 200, 136, dtype=dt), normal(g, 264, 136, dtype=dt, scale=0.1), normal(g, 200, 264, dtype=dt),
+                   normal(g, 200, 264, dtype=dt))
+    y, pre = dense.linear_forward(x, w, None, r, act="gelu", save_pre=True)
+    a = dense.linear_backward(x, w, dy, pre, act="gelu", bias=True)
+    for extra in (8, 3):
+        xs, wss, rs, dys = (rows_apart(t, t.shape[1] + extra) for t in (x, w, r, dy))
+        ys, ps = dense.linear_forward(xs, wss, None, rs, act="gelu", save_pre=True)
+        b = dense.linear_backward(xs, wss, dys, ps, act="gelu", bias=True)
+        for u, v in ((y, ys), (pre, ps), *((a[n], b[n]) for n in a)):
+            assert torch.allclose(u.float(), v.float(), rtol=2 * ref.HALF[dt], atol=1e-3)
+    y3, _ = dense.linear_forward(x.view(4, 50, 136), w)
+    assert y3.shape == (4, 50, 264)
+    only = dense.linear_backward(x, w, dy, pre, act="gelu", need_dx=False, bias=True)
+    assert only["dx"] is None and torch.equal(only["dw"], a["dw"]) and torch.equal(only["db"], a["db"])
+    only = dense.linear_backward(x, w, dy, pre, act="gelu", need_dw=False)
+    assert only["dw"] is None and only["db"] is None and torch.equal(only["dx"], a["dx"])
+
+
+def test_linear_no_rows_and_rows_that_are_not_finite():
+    w = torch.ones(40, 24, device="cuda", dtype=BF)
+    e = torch.zeros(0, 24, device="cuda", dtype=BF)
+    y, pre = dense.linear_forward(e, w, act="relu", save_pre=True)
+    got = dense.linear_backward(e, w, y, pre, act="relu", bias=True)
+    assert y.shape == (0, 40) and got["dx"].shape == (0, 24) and not got["dw"].any() and not got["db"].any()
+    for m, k in ((3, 24), (200, 72), (300, 100)):      # k = 100: a contraction tail
+        x = torch.ones(m, k, device="cuda", dtype=BF)
+        x[1, k - 1] = float("inf")
+        x[2, 0] = float("nan")
+        y, _ = dense.linear_forward(x, torch.ones(40, k, device="cuda", dtype=BF))
+        assert (y[0] == k).all() and y[1].isinf().all() and y[2].isnan().all() and (y[3:] == k).all()
+
+
+# ---- packed attention ----
+
+def packed(lens):
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    return torch.tensor(cu, dtype=torch.int32, device="cuda")
+
+
+def check_attention(g, dtype, lq, lk, heads, kv, d, causal, train=True, used=None, tail=0, scale=0.0, amp=1.3):
+    dt = DT[dtype]
+    cu_q, cu_k = packed(lq), packed(lk)
+    tq, tk = sum(lq) + tail, sum(lk) + tail
+    q, k, v = (normal(g, tq, heads, d, dtype=dt, scale=amp), normal(g, tk, kv, d, dtype=dt, scale=amp),
+               normal(g, tk, kv, d, dtype=dt))
+    do = normal(g, tq, heads, d, dtype=dt) if train else None
+    used_k = None if used is None else torch.tensor(used, dtype=torch.int32, device="cuda")
+    want = ref.attention(q, k, v, cu_q, cu_k, used, causal, scale or None, do)
+    o, lse = dense.attention_forward(q, k, v, cu_q, cu_k, used_k, causal=causal, softmax_scale=scale)
+    got = dict(o=o, lse=lse)
+    if train:
+        got.update(dense.attention_backward(q, k, v, o, lse, do, cu_q, cu_k, used_k, causal=causal, softmax_scale=scale))
+    for name, (value, bound) in want.items():
+        ref.check(name, got[name], value, bound)
+
+
+LENS = [1, 0, 7, 64, 65, 130, 33, 200]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,d", [(1, 1, 32), (4, 4, 64), (2, 2, 128), (8, 2, 64), (6, 2, 32), (8, 1, 128)])
+def test_attention_packed(dtype, causal, heads, kv, d):
+    check_attention(gen(heads + d), dtype, LENS, LENS, heads, kv, d, causal, tail=5)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_other_key_lengths(dtype, causal):
+    """Fewer keys than queries (causal: rows that see nothing), none, and more."""
+    check_attention(gen(6), dtype, [5, 70, 3, 64, 1, 0], [3, 20, 0, 300, 1, 9], 4, 2, 64, causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,d", [(8, 2, 128), (4, 4, 64), (16, 1, 64), (5, 1, 32), (32, 1, 64)])
+def test_attention_steps_against_a_cache(dtype, heads, kv, d):
+    """Single and few tokens against caches that are partly filled, empty, and long enough to be split."""
+    cap = [1024] * 6
+    used = [1, 1024, 0, 700, 257, 64]
+    check_attention(gen(7), dtype, [1] * 6, cap, heads, kv, d, True, train=False, used=used)
+    check_attention(gen(8), dtype, [3, 1, 4, 0, 2, 9], cap, heads, kv, d, True, train=False, used=used)
+    check_attention(gen(9), dtype, [2, 17], [5000, 3000], heads, kv, d, True, train=False, used=[4999, 2049], tail=3)
+    check_attention(gen(9), dtype, [3], [900], heads, kv, d, False, used=[555])
+
+
+def test_attention_many_sequences():
+    lens = [(i * 7) % 23 for i in range(300)]
+    check_attention(gen(10), "bf16", lens, lens, 2, 1, 32, True)
+    check_attention(gen(11), "bf16", [1] * 300, [64] * 300, 2, 2, 32, True, train=False, used=[i % 65 for i in range(300)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_one_long_sequence(dtype):
+    check_attention(gen(12), dtype, [1500], [1500], 1, 1, 64, True)
+    check_attention(gen(13), dtype, [130], [4000], 2, 1, 64, True, train=False)
+
+
+def test_attention_scale_and_sharp_scores():
+    """Scores up to several hundred: the running maximum moves, most probabilities vanish."""
+    check_attention(gen(14), "bf16", [300], [300], 2, 2, 64, False, amp=6.0)
+    check_attention(gen(15), "f32", [90, 200], [90, 200], 2, 2, 32, True, scale=0.5)
+
+
+def test_attention_values_of_keys_behind_the_end_do_not_enter():
+    """NaN in unused cache rows, in rows of no sequence, and in other sequences stays out."""
+    g = gen(16)
+    cu_q, cu_k = packed([3, 40]), packed([100, 100])
+    used = torch.tensor([70, 41], dtype=torch.int32, device="cuda")
+    q, k, v = normal(g, 50, 4, 64, dtype=BF), normal(g, 220, 2, 64, dtype=BF), normal(g, 220, 2, 64, dtype=BF)
+    do = normal(g, 50, 4, 64, dtype=BF)
+    o, lse = dense.attention_forward(q, k, v, cu_q, cu_k, used, causal=True)
+    a = dense.attention_backward(q, k, v, o, lse, do, cu_q, cu_k, used, causal=True)
+    for t in (k, v):
+        t[70:100] = float("nan")
+        t[141:] = float("nan")
+    q[43:] = float("nan")
+    do[43:] = float("nan")
+    o2, lse2 = dense.attention_forward(q, k, v, cu_q, cu_k, used, causal=True)
+    b = dense.attention_backward(q, k, v, o2, lse2, do, cu_q, cu_k, used, causal=True)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2) and all(torch.equal(a[n], b[n]) for n in a)
+    assert not o[43:].any() and not a["dq"][43:].any() and (lse[:, 43:] == -math.inf).all()
+    for n in ("dk", "dv"):
+        assert not a[n][70:100].any() and not a[n][141:].any()
+
+
+@pytest.mark.parametrize("lk", [100, 3000])
+def test_attention_leaves_rows_behind_the_last_sequence(lk):
+    g = gen(17)
+    q, k, v = normal(g, 60, 2, 64, dtype=BF), normal(g, lk, 2, 64, dtype=BF), normal(g, lk, 2, 64, dtype=BF)
+    cu_q, cu_k = packed([20, 1]), packed([lk // 2, lk // 2])
+    o, lse = torch.full_like(q, 7.0), torch.full((2, 60), 7.0, device="cuda")
+    dense.attention_forward(q, k, v, cu_q, cu_k, o=o, lse=lse)
+    assert (o[21:] == 7).all() and (lse[:, 21:] == 7).all()
+    fresh, z = dense.attention_forward(q, k, v, cu_q, cu_k)
+    assert torch.equal(o[:21], fresh[:21]) and torch.equal(lse[:, :21], z[:, :21]) and not fresh[21:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_strides(dtype):
+    """Views of one fused projection, and head-major tensors, give the packed tensors' bits."""
+    g, dt = gen(18), DT[dtype]
+    cu = packed([40, 77])
+    qkv = normal(g, 117, 3, 4, 64, dtype=dt)
+    q, k, v = (qkv[:, i].contiguous() for i in range(3))
+    do = normal(g, 117, 4, 64, dtype=dt)
+    o, lse = dense.attention_forward(q, k, v, cu, causal=True)
+    a = dense.attention_backward(q, k, v, o, lse, do, cu, causal=True)
+    o2, lse2 = dense.attention_forward(qkv[:, 0], qkv[:, 1], qkv[:, 2], cu, causal=True)
+    b = dense.attention_backward(qkv[:, 0], qkv[:, 1], qkv[:, 2], o, lse, do, cu, causal=True)
+    hm = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)
+    o3, lse3 = dense.attention_forward(hm(q), hm(k), hm(v), cu, causal=True, o=hm(torch.empty_like(q)),
+                                       lse=torch.empty_like(lse))
+    c = dense.attention_backward(hm(q), hm(k), hm(v), hm(o), lse, hm(do), cu, causal=True)
+    for x, y in ((o, o2), (o, o3), (lse, lse2), (lse, lse3), *((a[n], b[n]) for n in a), *((a[n], c[n]) for n in a)):
+        assert torch.equal(x, y)
+
+
+def test_attention_without_rows():
+    q = torch.zeros(0, 2, 64, device="cuda", dtype=BF)
+    k = torch.ones(9, 2, 64, device="cuda", dtype=BF)
+    cu0, cu = packed([0]), packed([9])
+    o, lse = dense.attention_forward(q, k, k, cu0, cu)
+    got = dense.attention_backward(q, k, k, o, lse, q, cu0, cu)
+    assert o.shape == q.shape and not got["dk"].any() and not got["dv"].any()
+    o, lse = dense.attention_forward(k, q, q, cu, cu0)          # queries without any key
+    got = dense.attention_backward(k, q, q, o, lse, k, cu, cu0)
+    assert not o.any() and (lse == -math.inf).all() and not got["dq"].any()
+
+
+def test_attention_offsets_beyond_32_bits():
+    """Rows whose element offset in the cache passes 2^32."""
+    g = gen(19)
+    row = 1 << 23                                # elements between rows: 520 rows span 8 GiB of bf16
+    buf = torch.zeros(520 * row, dtype=BF, device="cuda")
+    k = buf.as_strided((520, 1, 64), (row, 64, 1))
+    v = buf.as_strided((520, 1, 64), (row, 64, 1), 64)
+    k.copy_(normal(g, 520, 1, 64, dtype=BF))
+    v.copy_(normal(g, 520, 1, 64, dtype=BF))
+    q, do = normal(g, 20, 1, 64, dtype=BF), normal(g, 20, 1, 64, dtype=BF)
+    cu_q, cu_k = packed([20]), packed([520])
+    o, lse = dense.attention_forward(q, k, v, cu_q, cu_k)
+    o2, lse2 = dense.attention_forward(q, k.contiguous(), v.contiguous(), cu_q, cu_k)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    a = dense.attention_backward(q, k, v, o, lse, do, cu_q, cu_k)
+    b = dense.attention_backward(q, k.contiguous(), v.contiguous(), o, lse, do, cu_q, cu_k)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+# ---- together ----
+
+def test_gradients_against_differences():
+    """Central differences of sum(output * weight) in float32 tensors, computed on the GPU: a step of
+    h = 2^-6 along a random direction; the difference quotient is off by h^2/6 of the third
+    derivative (about the gradient's size here) and by 2 rounding errors over 2 h."""
+    g = gen(20)
+    cu = packed([9, 30])
+    q, k, v, do = (normal(g, 39, 2, 32) for _ in range(4))
+    o, lse = dense.attention_forward(q, k, v, cu, causal=True)
+    gr = dense.attention_backward(q, k, v, o, lse, do, cu, causal=True)
+    h = 2.0 ** -6
+    for i, name in enumerate(("dq", "dk", "dv")):
+        t = normal(g, 39, 2, 32, scale=0.1)
+        out = []
+        for s in (1, -1):
+            a = [q, k, v]
+            a[i] = a[i] + s * h * t
+            out.append((dense.attention_forward(*a, cu, causal=True)[0].double() * do.double()).sum())
+        quotient = ((out[0] - out[1]) / (2 * h)).item()
+        exact = (gr[name].double() * t.double()).sum().item()
+        size = (gr[name].double() * t.double()).abs().sum().item()
+        assert abs(quotient - exact) <= 1e-3 * size + 1e-3, name
+
+
+def block_pass(x, W, cu, heads, kv, d, dy):
+    """A pre-norm block of the operators, forward and backward."""
+    n = x.shape[0]
+    a1, m1, r1 = dense.layernorm_forward(x, W["g1"], W["b1"])
+    qkv, _ = dense.linear_forward(a1, W["wqkv"], W["bqkv"])
+    t = qkv.view(n, heads + 2 * kv, d)
+    q, k, v = t[:, :heads], t[:, heads:heads + kv], t[:, heads + kv:]
+    o, lse = dense.attention_forward(q, k, v, cu, causal=True)
+    hres, _ = dense.linear_forward(o.view(n, heads * d), W["wo"], None, x)
+    a2, m2, r2 = dense.layernorm_forward(hres, W["g2"], W["b2"])
+    u, pre = dense.linear_forward(a2, W["w1"], W["c1"], act="gelu", save_pre=True)
+    y, _ = dense.linear_forward(u, W["w2"], W["c2"], hres)
+    G = {}
+    b = dense.linear_backward(u, W["w2"], dy, bias=True)
+    G["w2"], G["c2"] = b["dw"], b["db"]
+    b = dense.linear_backward(a2, W["w1"], b["dx"], pre, act="gelu", bias=True)
+    G["w1"], G["c1"] = b["dw"], b["db"]
+    b = dense.layernorm_backward(hres, W["g2"], m2, r2, b["dx"])
+    G["g2"], G["b2"] = b["dgain"], b["dbias"]
+    dh = dy + b["dx"]
+    b = dense.linear_backward(o.view(n, heads * d), W["wo"], dh)
+    G["wo"] = b["dw"]
+    b = dense.attention_backward(q, k, v, o, lse, b["dx"].view(n, heads, d), cu, causal=True)
+    b = dense.linear_backward(a1, W["wqkv"], torch.cat([b["dq"], b["dk"], b["dv"]], 1).view(n, -1), bias=True)
+    G["wqkv"], G["bqkv"] = b["dw"], b["db"]
+    b = dense.layernorm_backward(x, W["g1"], m1, r1, b["dx"])
+    G["g1"], G["b1"] = b["dgain"], b["dbias"]
+    return dict(y=y, dx=dh + b["dx"], **G)
+
+
+def block_inputs(dtype, lens, heads, kv, d, ffn):
+    g, n, c = gen(21), sum(lens), heads * d
+    mat = lambda o, i: normal(g, o, i, dtype=dtype, scale=1 / math.sqrt(i))
+    vec = lambda m, dt, s: normal(g, m, dtype=dt, scale=0.1, shift=s)
+    W = dict(g1=vec(c, F32, 1), b1=vec(c, F32, 0), wqkv=mat((heads + 2 * kv) * d, c), bqkv=vec((heads + 2 * kv) * d, dtype, 0),
+             wo=mat(c, c), g2=vec(c, F32, 1), b2=vec(c, F32, 0), w1=mat(ffn, c), c1=vec(ffn, dtype, 0), w2=mat(c, ffn),
+             c2=vec(c, dtype, 0))
+    return normal(g, n, c, dtype=dtype), W, packed(lens), normal(g, n, c, dtype=dtype)
+
+
+def block_reference(x, W, lens, heads, kv, d, dy):
+    """The same block in float64, differentiated by autograd."""
+    x = x.cpu().double().requires_grad_()
+    P = {n: t.cpu().double().requires_grad_() for n, t in W.items()}
+    norm = lambda t, a, b: torch.nn.functional.layer_norm(t, t.shape[-1:], P[a], P[b], 1e-5)
+    qkv = (norm(x, "g1", "b1") @ P["wqkv"].t() + P["bqkv"]).view(x.shape[0], heads + 2 * kv, d)
+    outs, at = [], 0
+    for n in lens:
+        t = qkv[at:at + n]
+        q, k, v = t[:, :heads], t[:, heads:heads + kv], t[:, heads + kv:]
+        k, v = (u.repeat_interleave(heads // kv, 1) for u in (k, v))
+        s = torch.einsum("qhd,khd->hqk", q, k) / math.sqrt(d)
+        s = s.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -math.inf)
+        outs.append(torch.einsum("hqk,khd->qhd", s.softmax(2), v).reshape(n, heads * d))
+        at += n
+    h = x + torch.cat(outs) @ P["wo"].t()
+    u = torch.nn.functional.gelu(norm(h, "g2", "b2") @ P["w1"].t() + P["c1"])
+    y = h + u @ P["w2"].t() + P["c2"]
+    y.backward(dy.cpu().double())
+    return dict(y=y.detach(), dx=x.grad, **{n: t.grad for n, t in P.items()})
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_of_the_operators(dtype):
+    """Norm, projection, attention on views of it, residual projection, norm, MLP: forward and backward
+    against float64. Whole tensors by norm: a value passes about 12 roundings to the type in a row (6
+    forward, 6 back), each of half a step at most and independent; twice their plain sum is allowed."""
+    lens, heads, kv, d, ffn = [50, 1, 77], 4, 2, 32, 300
+    x, W, cu, dy = block_inputs(DT[dtype], lens, heads, kv, d, ffn)
+    got = block_pass(x, W, cu, heads, kv, d, dy)
+    want = block_reference(x, W, lens, heads, kv, d, dy)
+    tol = 24 * ref.HALF[DT[dtype]] * (1 if dtype == "bf16" else 8)   # f32: sums of up to 300 terms as well
+    for n, r in want.items():
+        err = (got[n].detach().cpu().double() - r).norm() / r.norm()
+        assert err <= tol, (n, err.item())
+
+
+def test_replays_of_a_captured_pass():
+    """The whole pass captured into a graph, replayed with new inputs beside eager work."""
+    lens, heads, kv, d, ffn = [50, 1, 77], 4, 2, 32, 300
+    x, W, cu, dy = block_inputs(BF, lens, heads, kv, d, ffn)
+    want = block_pass(x, W, cu, heads, kv, d, dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block_pass(x, W, cu, heads, kv, d, dy)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = block_pass(x, W, cu, heads, kv, d, dy)
+    x0 = x.clone()
+    for i in range(4):
+        x.copy_(x0 * (1 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = block_pass(x, W, cu, heads, kv, d, dy)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], want[n]) for n in want), i
+
+
+def test_streams():
+    """A call on a stream of its own, given or current, orders after that stream's work and gives the same bits."""
+    g = gen(22)
+    x, w = normal(g, 300, 128, dtype=BF), normal(g, 256, 128, dtype=BF)
+    want, _ = dense.linear_forward(x, w, act="silu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, _ = dense.linear_forward(x, w, act="silu", stream=side)
+    with torch.cuda.stream(side):
+        again, _ = dense.linear_forward(x, w, act="silu")
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want) and torch.equal(again, want)
