@@ -151,6 +151,13 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Direct global->LDS load of 16 bytes per lane: lane L's bytes land at lds + 16 L (lds uniform).
+// Not a template: the host pass rejects a kernel template that reaches the builtin through a
+// template function instantiated before, and leaves its launch stub out without an error.
+__device__ __forceinline__ void load_lds16(const void* g, void* lds) {
+  __builtin_amdgcn_global_load_lds(g, lds, 16, 0, 0);
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float fast_log2(float x) { return __builtin_amdgcn_logf(x); }
 

@@ -91,7 +91,7 @@ struct TileLoad {
       const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
       const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
       const int r = min(r0 + row, nrows - 1);
-      __builtin_amdgcn_global_load_lds(g + r * ld + E * c, lds + blk * 64 * E, 16, 0, 0);
+      load_lds16(g + r * ld + E * c, lds + blk * 64 * E);
     }
   }
 };
@@ -146,7 +146,7 @@ struct PackedLoad {
       const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
       const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
       const RowAt at = packed_row(sq, hk, G, min(r0 + row, rows - 1));
-      __builtin_amdgcn_global_load_lds(g + at.t * row_ld + at.h * head_ld + E * c, lds + blk * 64 * E, 16, 0, 0);
+      load_lds16(g + at.t * row_ld + at.h * head_ld + E * c, lds + blk * 64 * E);
     }
   }
 };

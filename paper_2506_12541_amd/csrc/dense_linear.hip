@@ -6,6 +6,7 @@
 // bf16 matrix cores, f32 operands the f32 ones; sums, bias, activation and residual are
 // float32, rounded once to the storage type.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "dense.hpp"
@@ -223,6 +224,267 @@ __global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long l
     }
 }
 
+// ---- bf16 products of aligned operands: tiles loaded straight into LDS ----
+
+// Loads of a ROWS x COLS tile of a stored matrix (row form: operand rows x contraction; column
+// form: contraction x operand rows) by NW waves: a wave instruction fills 1 KB of consecutive
+// LDS, and each lane fetches the 16-byte piece that the swizzle puts there. Operand rows behind
+// the matrix repeat its last ones (their products are not stored); the contraction's last,
+// partial tile is staged through registers (tail), zeros behind its end.
+template <bool TR, int ROWS, int COLS, int NW>
+struct DmaTile {
+  static constexpr int CPR = COLS / 8, NU = ROWS * CPR / (64 * NW);
+  static_assert(NU * 64 * NW == ROWS * CPR, "tile / wave split");
+  const char* base;       // the operand block's first element (uniform)
+  uint32_t off[NU];       // bytes from there at contraction index 0 (the launcher bounds ld)
+
+  __device__ __forceinline__ void init(const Mat<bf16_t>& m, long long o0, int wid, int lane) {
+    base = reinterpret_cast<const char*>(m.p + (TR ? o0 : o0 * m.ld));
+    const int last = (int)((TR ? m.cols - 8 : m.rows - 1) - o0 < (1 << 20) ? (TR ? m.cols - 8 : m.rows - 1) - o0 : 1 << 20);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int i = (wid * NU + u) * 64 + lane, row = i / CPR;
+      const int c = 8 * ((i % CPR) ^ tile_swz<COLS>(row));
+      off[u] = 2u * (TR ? (uint32_t)row * (uint32_t)m.ld + min(c, last) : (uint32_t)min(row, last) * (uint32_t)m.ld + c);
+    }
+  }
+  __device__ __forceinline__ void issue(bf16_t* lds, const Mat<bf16_t>& m, long long k0, int wid) const {
+    const char* p = base + 2 * (TR ? k0 * m.ld : k0);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) load_lds16(p + off[u], lds + (wid * NU + u) * 512);
+  }
+  __device__ __forceinline__ void tail(bf16_t* lds, const Mat<bf16_t>& m, long long o0, long long k0, int wid,
+                                       int lane) const {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int i = (wid * NU + u) * 64 + lane, row = i / CPR;
+      const int c = 8 * ((i % CPR) ^ tile_swz<COLS>(row));
+      *reinterpret_cast<uint4*>(lds + 8 * i) = TR ? load_piece(m, k0 + row, (int)o0 + c) : load_piece(m, o0 + row, (int)k0 + c);
+    }
+  }
+};
+
+// Row-form fragment in the order of the transposing reads (4j.., 16 + 4j..).
+template <int BK>
+__device__ __forceinline__ bf16x8 frag_pairs(const bf16_t* t, int row, int ks, int j) {
+  auto half = [&](int c) {
+    return *reinterpret_cast<const uint2*>(t + row * BK + 8 * (c ^ tile_swz<BK>(row)) + 4 * (j & 1));
+  };
+  const uint2 a = half(4 * ks + j / 2), b = half(4 * ks + 2 + j / 2);
+  return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+}
+
+// The NF fragments of operand rows r0 + 16 i of a staged tile at contraction step ks; TR: the tile
+// is in column form (COLS operand rows wide), PAIRS: its partner is.
+template <bool TR, bool PAIRS, int BK, int COLS, int NF>
+struct Frags {
+  __device__ __forceinline__ static void read(const bf16_t* t, int r0, int ks, int lane, bf16x8 (&f)[NF]) {
+    if constexpr (!TR) {
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+        f[i] = PAIRS ? frag_pairs<BK>(t, r0 + 16 * i + (lane & 15), ks, lane >> 4)
+                     : frag_row<BK>(t, r0 + 16 * i + (lane & 15), 4 * ks + (lane >> 4));
+    } else if constexpr (NF % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < NF; i += 4)
+        tr_frags4<COLS>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[4]>(&f[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NF; i += 2)
+        tr_frags2<COLS>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[2]>(&f[i]));
+    }
+  }
+};
+
+// Eight consecutive columns of a row: whole 16-byte pieces unless the row ends inside.
+__device__ __forceinline__ void epi_store8(const Epi<bf16_t>& o, long long m, int n, float (&v)[8], int split) {
+  if (n + 8 > o.N || o.part) {
+    epi_store<bf16_t, 8>(o, m, n, v, split);
+    return;
+  }
+  if (m >= o.M) return;
+  if (o.bias) {
+    float b[8];
+    unpack16<bf16_t>(load16u(o.bias + n), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += b[e];
+  }
+  if (o.pre) store16u(o.pre + m * o.N + n, pack16<bf16_t>(v));
+  if (o.act != kActNone) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_fwd(v[e], o.act);
+  }
+  if (o.res) {
+    float r[8];
+    unpack16<bf16_t>(load16u(o.res + m * o.ldr + n), r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += r[e];
+  }
+  store16u(o.out + m * o.ldo + n, pack16<bf16_t>(v));
+}
+
+// Workgroup tile BM x BN of WM x WN waves, contraction tiles of BK in a ring of NS LDS stages,
+// NS - 1 of them in flight while one feeds the matrix cores.
+template <bool TA, bool TB, int BM, int BN, int WM, int WN, int BK, int NS>
+__global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a, Mat<bf16_t> b, long long K, int ntm,
+                                                                   int ntn, int kt_per, Epi<bf16_t> o) {
+  constexpr int NW = WM * WN, TMW = BM / WM, TNW = BN / WN, FI = TMW / 16, FJ = TNW / 16;
+  static_assert(NS >= 2 && NS <= 4 && (BK == 32 || BK == 64), "pipeline");
+  constexpr int AE = BM * BK, BE = BN * BK;
+  __shared__ __attribute__((aligned(1024))) bf16_t as0[AE], bs0[BE], as1[AE], bs1[BE];
+  __shared__ __attribute__((aligned(1024))) bf16_t as2[NS > 2 ? AE : 8], bs2[NS > 2 ? BE : 8];
+  __shared__ __attribute__((aligned(1024))) bf16_t as3[NS > 3 ? AE : 8], bs3[NS > 3 ? BE : 8];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int wm = wid / WN, wn = wid % WN;
+  // workgroups are dealt to the 8 XCDs round-robin; each XCD gets a contiguous run of tiles, in
+  // bands of 8 tile rows walked column by column, so the tiles it holds at a time share operands
+  const int nt = ntm * ntn;
+  int id = blockIdx.x;
+  if ((nt & 7) == 0) id = (id & 7) * (nt >> 3) + (id >> 3);
+  const int band = id / (8 * ntn), in = id - band * 8 * ntn, bh = min(8, ntm - 8 * band);
+  const int tm = 8 * band + in % bh, tn = in / bh;
+  const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
+  const int nkt = (int)(K / BK);     // whole tiles
+  const int kt0 = min((int)blockIdx.y * kt_per, nkt), kt1 = min(kt0 + kt_per, nkt);
+  const bool tail = (blockIdx.y == gridDim.y - 1) && K > (long long)nkt * BK;
+
+  DmaTile<TA, TA ? BK : BM, TA ? BM : BK, NW> la;
+  DmaTile<TB, TB ? BK : BN, TB ? BN : BK, NW> lb;
+  la.init(a, m0, wid, lane);
+  lb.init(b, n0, wid, lane);
+  constexpr int PER = decltype(la)::NU + decltype(lb)::NU;   // wave load instructions per tile
+  bf16_t* const AS[4] = {as0, as1, as2, as3};
+  bf16_t* const BS[4] = {bs0, bs1, bs2, bs3};
+  auto issue = [&](int kt, int st) {
+    la.issue(AS[st], a, (long long)kt * BK, wid);
+    lb.issue(BS[st], b, (long long)kt * BK, wid);
+  };
+  f32x4 acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  bf16x8 af[FI], bfr[FJ];
+  auto read = [&](const bf16_t* as, const bf16_t* bs, int ks) {
+    Frags<TA, TB, BK, BM, FI>::read(as, wm * TMW, ks, lane, af);
+    Frags<TB, TA, BK, BN, FJ>::read(bs, wn * TNW, ks, lane, bfr);
+  };
+  auto multiply = [&]() {
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bfr[j], af[i], acc[i][j]);
+  };
+
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (kt0 + s < kt1) issue(kt0 + s, s);
+  if constexpr (NW == 8) {
+    // Two waves share a SIMD; the second four waves run one phase behind the first four, so one
+    // wave of each SIMD multiplies while the other reads its fragments. Phases end with a
+    // barrier; group 0 reads tile t in phase 2t and multiplies in 2t + 1, group 1 one phase
+    // later. Stage (t - 1) % NS is last read in phase 2t - 1, so tile t + NS - 1 may be loaded
+    // into it from phase 2t on; tile t + 1 is first read in phase 2t + 2, so every wave waits for
+    // its part of it before the barrier that ends phase 2t + 1.
+    static_assert(BK == 32 && NS == 4, "one fragment depth per phase");
+    const int n = kt1 - kt0, grp = wid >> 2;
+    auto landed = [&](int t) {   // tile t + 1, with at most tiles t + 2 and t + 3 in flight
+      if (t + 3 < n)
+        vm_wait<2 * PER>();
+      else if (t + 2 < n)
+        vm_wait<PER>();
+      else
+        vm_drain();
+    };
+    landed(-1);
+    lds_barrier();
+    if (grp == 1) lds_barrier();
+    for (int t0 = 0; t0 < n; t0 += NS) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const int t = t0 + s;
+        if (t < n) {
+          if (t + NS - 1 < n) issue(kt0 + t + NS - 1, (s + NS - 1) % NS);
+          read(AS[s], BS[s], 0);
+          lgkm_drain();
+          if (grp == 1) landed(t);
+          lds_barrier();
+          __builtin_amdgcn_s_setprio(1);
+          multiply();
+          __builtin_amdgcn_s_setprio(0);
+          if (grp == 0) landed(t);
+          lds_barrier();
+        }
+      }
+    }
+    if (grp == 0) lds_barrier();
+  } else {
+    for (int kt = kt0; kt < kt1; kt += NS) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const int t = kt + s;
+        if (t < kt1) {
+          // tile t has landed once at most the NS - 2 tiles issued after it are in flight
+          if (t + NS - 2 < kt1)
+            vm_wait<(NS - 2) * PER>();
+          else
+            vm_drain();
+          lds_barrier();     // every wave's loads of tile t are visible; stage s - 1 is free
+          if (t + NS - 1 < kt1) issue(t + NS - 1, (s + NS - 1) % NS);
+#pragma unroll
+          for (int ks = 0; ks < BK / 32; ++ks) {
+            read(AS[s], BS[s], ks);
+            multiply();
+          }
+        }
+      }
+    }
+  }
+  if (tail) {
+    __syncthreads();
+    la.tail(as0, a, m0, (long long)nkt * BK, wid, lane);
+    lb.tail(bs0, b, n0, (long long)nkt * BK, wid, lane);
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < BK / 32; ++ks) {
+      read(as0, bs0, ks);
+      multiply();
+    }
+  }
+
+  // Epilogue through LDS (the stages are free by then), RP rows of the wave's tile at a time in
+  // f32, so that stores are runs of whole lines; 16-byte chunk c of row x sits at c ^ (x mod 16).
+  constexpr int AB = 2 * (AE < BE ? AE : BE);
+  constexpr int RP = epi_rows(AB, TMW, TNW, NW);
+  constexpr int WPA = AB / (RP * TNW * 4);                             // waves per stage array
+  static_assert(WPA >= 1 && 4 * WPA >= NW && RP % 16 == 0, "epilogue regions");
+  constexpr int SM = TNW >= 64 ? 15 : 7;
+  lds_barrier();   // every wave has read the last tile
+  bf16_t* const arr = wid / WPA == 0 ? as0 : wid / WPA == 1 ? bs0 : wid / WPA == 2 ? as1 : bs1;
+  float* const reg = reinterpret_cast<float*>(arr) + (wid % WPA) * RP * TNW;
+  auto at = [&](int row, int chunk) { return reinterpret_cast<f32x4*>(reg + row * TNW + 4 * (chunk ^ (row & SM))); };
+  constexpr int LPR = TNW / 8, RPI = 64 / LPR;
+#pragma unroll
+  for (int i0 = 0; i0 < FI; i0 += RP / 16) {
+#pragma unroll
+    for (int i = 0; i < RP / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) *at(16 * i + (lane & 15), 4 * j + (lane >> 4)) = acc[i0 + i][j];
+    wave_sync();
+    const long long mw = m0 + wm * TMW + 16 * i0;
+    const int c = 8 * (lane % LPR), n = (int)n0 + wn * TNW + c;
+#pragma unroll 2
+    for (int x0 = 0; x0 < RP; x0 += RPI) {
+      const int x = x0 + lane / LPR;
+      const f32x4 u = *at(x, c / 4), w = *at(x, c / 4 + 1);
+      float v[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+      epi_store8(o, mw + x, n, v, blockIdx.y);
+    }
+    wave_sync();
+  }
+}
+
 // y = epilogue(sum over the splits, in order), four columns per thread
 template <typename T>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* __restrict__ part, int S, Epi<T> o) {
@@ -319,42 +581,73 @@ __global__ void __launch_bounds__(256) fill_zero_kernel(T* p, long long n) {
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-// Splits of a product's contraction: while the 128 x 128 tiles leave CUs idle, at least 8
-// contraction tiles each.
-int product_splits(long long M, int N, long long K) {
-  const long long tiles = ((M + 127) / 128) * ((N + 127) / 128), nkt = (K + 31) / 32;
-  int s = 1;
-  while (tiles * s < 256 && nkt / (2 * s) >= 8 && s < 64) s *= 2;
-  return s;
+// How a product runs: tile side (workgroup tile T x T) and splits of the contraction.
+struct Plan {
+  int T, S;
+};
+
+// bf16 products: 256 x 256 tiles (8 waves) where there are enough of them, else 128 x 128 and
+// 64 x 64; with may_split the contraction is split, in powers of two, until about every CU has a
+// workgroup, at least 512 contraction indices each. f32 products: 128 or 64.
+Plan plan_product(bool bf16, long long M, int N, long long K, bool may_split) {
+  auto tiles = [&](int T) { return ((M + T - 1) / T) * ((N + T - 1) / T); };
+  Plan p{128, 1};
+  if (bf16 && (tiles(256) >= 192 || (may_split && tiles(256) * (K / 512) >= 192)))
+    p.T = 256;
+  else if (tiles(128) < 256 && !(may_split && tiles(128) * (K / 512) >= 256))
+    p.T = 64;
+  if (may_split)
+    while (tiles(p.T) * p.S < (p.T == 256 ? 192 : 256) && K / (2 * p.S) >= 512 && p.S < 64) p.S *= 2;
+  return p;
 }
+
+bool dma_ok(const Mat<bf16_t>& m, bool tr, long long K) {
+  const bool whole = tr ? m.cols % 8 == 0 && m.cols >= 8 : K % 8 == 0;
+  // a tile's byte offsets fit 32 bits: 256 rows of at most 2^22 elements
+  return whole && m.ld % 8 == 0 && m.ld <= (1 << 22) && ((uintptr_t)m.p & 15) == 0;
+}
+bool dma_ok(const Mat<float>&, bool, long long) { return false; }
 
 // C = A B^T with the epilogue; S > 1: partial sums in part, joined by split_sum_kernel
 template <typename T, bool TA, bool TB>
-hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long long K, int S, float* part, Epi<T> o,
+hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long long K, Plan p, float* part, Epi<T> o,
                    hipStream_t st) {
-  const long long nkt = (K + 31) / 32, per = (nkt + S - 1) / S;
-  o.part = S > 1 ? part : nullptr;
-  const long long big = ((M + 127) / 128) * ((N + 127) / 128) * S;
-  if (big >= 256) {
-    const int ntn = (N + 127) / 128;
-    const dim3 grid((unsigned)(((M + 127) / 128) * ntn), (unsigned)S);
-    product_kernel<T, TA, TB, 128, 128><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
-  } else {
-    const int ntn = (N + 63) / 64;
-    const dim3 grid((unsigned)(((M + 63) / 64) * ntn), (unsigned)S);
-    product_kernel<T, TA, TB, 64, 64><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
+  o.part = p.S > 1 ? part : nullptr;
+  const bool dma = dma_ok(a, TA, K) && dma_ok(b, TB, K);
+  const int side = !dma && p.T == 256 ? 128 : p.T;
+  const int ntm = (int)((M + side - 1) / side), ntn = (N + side - 1) / side;
+  const dim3 grid((unsigned)((long long)ntm * ntn), (unsigned)p.S);
+  if constexpr (sizeof(T) == 2) {
+    if (dma) {
+      const int bk = side == 256 ? 32 : 64;
+      const int per = (int)((K / bk + p.S - 1) / p.S);
+      if (side == 256)
+        product_dma_kernel<TA, TB, 256, 256, 4, 2, 32, 4><<<grid, 512, 0, st>>>(a, b, K, ntm, ntn, per, o);
+      else if (side == 128)
+        product_dma_kernel<TA, TB, 128, 128, 2, 2, 64, 2><<<grid, 256, 0, st>>>(a, b, K, ntm, ntn, per, o);
+      else
+        product_dma_kernel<TA, TB, 64, 64, 2, 2, 64, 4><<<grid, 256, 0, st>>>(a, b, K, ntm, ntn, per, o);
+    }
+  }
+  if (!dma) {
+    const long long per = ((K + 31) / 32 + p.S - 1) / p.S;
+    if (side == 128)
+      product_kernel<T, TA, TB, 128, 128><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
+    else
+      product_kernel<T, TA, TB, 64, 64><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || S == 1) return e;
+  if (e != hipSuccess || p.S == 1) return e;
   o.part = nullptr;
   const long long n4 = M * ((N + 3) / 4);
-  split_sum_kernel<T><<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(part, S, o);
+  split_sum_kernel<T><<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(part, p.S, o);
   return hipGetLastError();
 }
 
 struct LinBwdWs {
   size_t dz, dbp, part, total;
-  int S, P;
+  Plan dw;
+  int P;
   long long rpg;
 };
 LinBwdWs linear_bwd_layout(const LinearArgs& a) {
@@ -363,7 +656,7 @@ LinBwdWs linear_bwd_layout(const LinearArgs& a) {
   const int E = 16 / (int)esz;
   size_t off = 0;
   auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
-  L.S = product_splits(a.n, a.k, a.m);
+  L.dw = plan_product(a.bf16, a.n, a.k, a.m, true);
   // row groups of the dz pass: about 1024 workgroups, at least 32 rows each
   const long long gx = (a.n + 32 * E - 1) / (32 * E);
   long long P = std::min<long long>(std::max<long long>(1024 / gx, 1), (a.m + 31) / 32);
@@ -372,7 +665,7 @@ LinBwdWs linear_bwd_layout(const LinearArgs& a) {
   L.P = (int)(L.rpg ? (a.m + L.rpg - 1) / L.rpg : 1);
   L.dz = put(a.act == kActNone ? 0 : esz * (size_t)a.m * a.n);
   L.dbp = put(sizeof(float) * (size_t)L.P * a.n);
-  L.part = put(L.S > 1 ? sizeof(float) * (size_t)L.S * a.n * a.k : 0);
+  L.part = put(L.dw.S > 1 ? sizeof(float) * (size_t)L.dw.S * a.n * a.k : 0);
   L.total = off;
   return L;
 }
@@ -382,7 +675,7 @@ hipError_t linear_fwd(const LinearArgs& a, const void* x, const void* w, const v
                       void* pre, void* ws, hipStream_t st) {
   Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, (const T*)res, a.ldr, (T*)pre, a.act, nullptr};
   return product<T, false, false>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.n,
-                                  a.k, 1, (float*)ws, o, st);
+                                  a.k, plan_product(a.bf16, a.m, a.n, a.k, false), (float*)ws, o, st);
 }
 
 template <typename T>
@@ -414,12 +707,13 @@ hipError_t linear_bwd(const LinearArgs& a, const void* x, const void* w, const v
   const Mat<T> mz{dz ? dz : (const T*)dy, dz ? a.n : a.lddy, a.m, a.n};
   if (dx) {
     Epi<T> o{a.m, a.k, (T*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
-    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n, 1, nullptr, o, st);
+    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n,
+                                             plan_product(a.bf16, a.m, a.k, a.n, false), nullptr, o, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
     Epi<T> o{a.n, a.k, (T*)dw, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
-    hipError_t e = product<T, true, true>(mz, Mat<T>{(const T*)x, a.ldx, a.m, a.k}, a.n, a.k, a.m, L.S,
+    hipError_t e = product<T, true, true>(mz, Mat<T>{(const T*)x, a.ldx, a.m, a.k}, a.n, a.k, a.m, L.dw,
                                           (float*)(c + L.part), o, st);
     if (e != hipSuccess) return e;
   }

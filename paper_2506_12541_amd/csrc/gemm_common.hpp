@@ -79,6 +79,25 @@ __device__ __forceinline__ void tr_frags4(const bf16_t* t, int k0, int m0, int l
     f[i] = __builtin_bit_cast(bf16x8, make_uint4(r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y));
 }
 
+// The same for two fragments (columns m0 and m0 + 16).
+template <int COLS>
+__device__ __forceinline__ void tr_frags2(const bf16_t* t, int k0, int m0, int lane, bf16x8 (&f)[2]) {
+  uint32_t a[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) tr_addr<COLS>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
+  uint2 r[4];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\t"
+      "ds_read_b64_tr_b16 %2, %6\n\tds_read_b64_tr_b16 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    f[i] = __builtin_bit_cast(bf16x8, make_uint4(r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y));
+}
+
 // 1 / (1 + exp(-x)): the hardware reciprocal and one Newton step (within an ulp of the divided
 // value, at a third of the division's instructions). Where exp(-x) leaves the range in which the
 // reciprocal is a normal number (x below -87) the reciprocal stands: the step would give NaN.
