@@ -18,20 +18,46 @@ namespace {
 
 // ---- activations ----
 
-__device__ __forceinline__ float gelu_cdf(float z) { return 0.5f * erfcf(-z * 0.70710678118654752f); }
+// Normal distribution function Phi(z) and e^(-z^2 / 2). f32 tensors take the library's erfc (f32
+// accurate in the lower tail as well). bf16 tensors take Abramowitz and Stegun 7.1.26, erfc(x) =
+// (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x >= 0, off by at most 1.5e-7: 2^-14 of a
+// bf16 step at 1. erfc's branches took longer than the products: at 65536 x 512 -> 2048 channels
+// the forward with GELU ran 427 us, the dz pass 253.
+template <typename T>
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  e = __expf(-0.5f * z * z);
+  if constexpr (sizeof(T) == 4) return 0.5f * erfcf(-z * 0.70710678118654752f);
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * e;
+  return z > 0.f ? 1.0f - tail : tail;
+}
 
+template <typename T>
 __device__ __forceinline__ float act_fwd(float z, int act) {
   switch (act) {
     case kActRelu: return z > 0.f ? z : z != z ? z : 0.f;
-    case kActGelu: return z * gelu_cdf(z);
+    case kActGelu: {
+      float e;
+      return z * normal_cdf<T>(z, e);
+    }
     case kActSilu: return z * sigmoid(z);
     default: return z;
   }
 }
+template <typename T>
 __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case kActRelu: return z > 0.f ? 1.f : 0.f;
-    case kActGelu: return fmaf(z, __expf(-0.5f * z * z) * 0.39894228040143268f, gelu_cdf(z));
+    case kActGelu: {
+      float e;
+      const float cdf = normal_cdf<T>(z, e);
+      return fmaf(z * e, 0.39894228040143268f, cdf);
+    }
     case kActSilu: {
       const float s = sigmoid(z);
       return s * fmaf(z, 1.f - s, 1.f);
@@ -73,7 +99,7 @@ __device__ __forceinline__ void epi_store(const Epi<T>& o, long long m, int n, f
       float z = v[e];
       if (o.bias) z += to_f32<T>(o.bias[n + e]);
       if (o.pre) o.pre[m * o.N + n + e] = from_f32<T>(z);
-      z = act_fwd(z, o.act);
+      z = act_fwd<T>(z, o.act);
       if (o.res) z += to_f32<T>(o.res[m * o.ldr + n + e]);
       o.out[m * o.ldo + n + e] = from_f32<T>(z);
     }
@@ -231,7 +257,7 @@ __global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long l
 // LDS, and each lane fetches the 16-byte piece that the swizzle puts there. Operand rows behind
 // the matrix repeat its last ones (their products are not stored); the contraction's last,
 // partial tile is staged through registers (tail), zeros behind its end.
-template <bool TR, int ROWS, int COLS, int NW>
+template <bool TR, bool MIX, int ROWS, int COLS, int NW>
 struct DmaTile {
   static constexpr int CPR = COLS / 8, NU = ROWS * CPR / (64 * NW);
   static_assert(NU * 64 * NW == ROWS * CPR, "tile / wave split");
@@ -244,7 +270,7 @@ struct DmaTile {
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       const int i = (wid * NU + u) * 64 + lane, row = i / CPR;
-      const int c = 8 * ((i % CPR) ^ tile_swz<COLS>(row));
+      const int c = 8 * ((i % CPR) ^ tile_swz<COLS, TR && MIX>(row));
       off[u] = 2u * (TR ? (uint32_t)row * (uint32_t)m.ld + min(c, last) : (uint32_t)min(row, last) * (uint32_t)m.ld + c);
     }
   }
@@ -258,40 +284,28 @@ struct DmaTile {
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       const int i = (wid * NU + u) * 64 + lane, row = i / CPR;
-      const int c = 8 * ((i % CPR) ^ tile_swz<COLS>(row));
+      const int c = 8 * ((i % CPR) ^ tile_swz<COLS, TR && MIX>(row));
       *reinterpret_cast<uint4*>(lds + 8 * i) = TR ? load_piece(m, k0 + row, (int)o0 + c) : load_piece(m, o0 + row, (int)k0 + c);
     }
   }
 };
 
-// Row-form fragment in the order of the transposing reads (4j.., 16 + 4j..).
-template <int BK>
-__device__ __forceinline__ bf16x8 frag_pairs(const bf16_t* t, int row, int ks, int j) {
-  auto half = [&](int c) {
-    return *reinterpret_cast<const uint2*>(t + row * BK + 8 * (c ^ tile_swz<BK>(row)) + 4 * (j & 1));
-  };
-  const uint2 a = half(4 * ks + j / 2), b = half(4 * ks + 2 + j / 2);
-  return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
-}
-
 // The NF fragments of operand rows r0 + 16 i of a staged tile at contraction step ks; TR: the tile
-// is in column form (COLS operand rows wide), PAIRS: its partner is.
-template <bool TR, bool PAIRS, int BK, int COLS, int NF>
+// is in column form, COLS operand rows wide; MIX: the partner is in the other form.
+template <bool TR, bool MIX, int BK, int COLS, int NF>
 struct Frags {
   __device__ __forceinline__ static void read(const bf16_t* t, int r0, int ks, int lane, bf16x8 (&f)[NF]) {
     if constexpr (!TR) {
 #pragma unroll
-      for (int i = 0; i < NF; ++i)
-        f[i] = PAIRS ? frag_pairs<BK>(t, r0 + 16 * i + (lane & 15), ks, lane >> 4)
-                     : frag_row<BK>(t, r0 + 16 * i + (lane & 15), 4 * ks + (lane >> 4));
+      for (int i = 0; i < NF; ++i) f[i] = frag_row<BK>(t, r0 + 16 * i + (lane & 15), 4 * ks + (lane >> 4));
     } else if constexpr (NF % 4 == 0) {
 #pragma unroll
       for (int i = 0; i < NF; i += 4)
-        tr_frags4<COLS>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[4]>(&f[i]));
+        tr_frags4<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[4]>(&f[i]));
     } else {
 #pragma unroll
       for (int i = 0; i < NF; i += 2)
-        tr_frags2<COLS>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[2]>(&f[i]));
+        tr_frags2<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[2]>(&f[i]));
     }
   }
 };
@@ -312,7 +326,7 @@ __device__ __forceinline__ void epi_store8(const Epi<bf16_t>& o, long long m, in
   if (o.pre) store16u(o.pre + m * o.N + n, pack16<bf16_t>(v));
   if (o.act != kActNone) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_fwd(v[e], o.act);
+    for (int e = 0; e < 8; ++e) v[e] = act_fwd<bf16_t>(v[e], o.act);
   }
   if (o.res) {
     float r[8];
@@ -348,8 +362,8 @@ __global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a
   const int kt0 = min((int)blockIdx.y * kt_per, nkt), kt1 = min(kt0 + kt_per, nkt);
   const bool tail = (blockIdx.y == gridDim.y - 1) && K > (long long)nkt * BK;
 
-  DmaTile<TA, TA ? BK : BM, TA ? BM : BK, NW> la;
-  DmaTile<TB, TB ? BK : BN, TB ? BN : BK, NW> lb;
+  DmaTile<TA, TA != TB, TA ? BK : BM, TA ? BM : BK, NW> la;
+  DmaTile<TB, TA != TB, TB ? BK : BN, TB ? BN : BK, NW> lb;
   la.init(a, m0, wid, lane);
   lb.init(b, n0, wid, lane);
   constexpr int PER = decltype(la)::NU + decltype(lb)::NU;   // wave load instructions per tile
@@ -367,8 +381,8 @@ __global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a
 
   bf16x8 af[FI], bfr[FJ];
   auto read = [&](const bf16_t* as, const bf16_t* bs, int ks) {
-    Frags<TA, TB, BK, BM, FI>::read(as, wm * TMW, ks, lane, af);
-    Frags<TB, TA, BK, BN, FJ>::read(bs, wn * TNW, ks, lane, bfr);
+    Frags<TA, TA != TB, BK, BM, FI>::read(as, wm * TMW, ks, lane, af);
+    Frags<TB, TA != TB, BK, BN, FJ>::read(bs, wn * TNW, ks, lane, bfr);
   };
   auto multiply = [&]() {
 #pragma unroll
@@ -529,7 +543,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ dy, long 
         float z[E];
         unpack16<T>(load_piece(mz, r, c), z);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] *= act_slope(z[e], act);
+        for (int e = 0; e < E; ++e) v[e] *= act_slope<T>(z[e], act);
         T* p = dz + r * n + c;
         if (c + E <= n)
           store16u(p, pack16<T>(v));

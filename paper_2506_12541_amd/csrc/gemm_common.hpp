@@ -9,8 +9,11 @@ namespace {
 // 16-byte chunk swizzle of a staged tile row: 4 or 8 chunks per row (row-fragment reads
 // of 16 consecutive rows on distinct banks) or 16 and more chunks per row (transposing
 // reads of 8 consecutive rows, chunk pairs on distinct banks).
-template <int COLS>
+// MIX: transposing reads of rows 8j + {0..3} (+ 4) instead, for a tile whose partner is read in
+// row fragments (rows 0-3 and 8-11, 4-7 and 12-15, .. on distinct banks).
+template <int COLS, bool MIX = false>
 __device__ __forceinline__ int tile_swz(int x) {
+  if (MIX) return COLS == 64 ? 2 * (((x >> 1) & 1) | ((x >> 2) & 2)) : 2 * ((x & 3) | ((x >> 1) & 4));
   return COLS == 32 ? ((x >> 1) & 3) : COLS == 64 ? (x & 7) : 2 * (x & 7);
 }
 
@@ -44,14 +47,15 @@ __device__ __forceinline__ void lgkm_drain() { asm volatile("s_waitcnt lgkmcnt(0
 // [BK][COLS] tile X (BK = 32 or 64): within each 16-lane group, ds_read_b64_tr_b16 hands lane l element
 // l % 4 of the 4-element runs addressed by lanes l / 4, 4 + l / 4, 8 + l / 4, 12 + l / 4, so
 // lane p addresses row k0 + 4j + p / 4 (then + 16) at columns m0 + 4 (p % 4) + [0, 4).
-template <int COLS>
+// MIX: X[k0 + 8j + i][m0 + p] and X[k0 + 8j + 4 + i][m0 + p] instead, the order of a row fragment.
+template <int COLS, bool MIX>
 __device__ __forceinline__ void tr_addr(const bf16_t* t, int k0, int m0, int lane, uint32_t& o0, uint32_t& o1) {
   const int p = lane & 15, j = lane >> 4;
   const int col = m0 + 4 * (p & 3);
   const int lc = col >> 3, sub = col & 7;
-  const int x0 = k0 + 4 * j + (p >> 2), x1 = x0 + 16;
-  const bf16_t* a0 = t + x0 * COLS + 8 * (lc ^ tile_swz<COLS>(x0)) + sub;
-  const bf16_t* a1 = t + x1 * COLS + 8 * (lc ^ tile_swz<COLS>(x1)) + sub;
+  const int x0 = k0 + (MIX ? 8 : 4) * j + (p >> 2), x1 = x0 + (MIX ? 4 : 16);
+  const bf16_t* a0 = t + x0 * COLS + 8 * (lc ^ tile_swz<COLS, MIX>(x0)) + sub;
+  const bf16_t* a1 = t + x1 * COLS + 8 * (lc ^ tile_swz<COLS, MIX>(x1)) + sub;
   o0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)a0;
   o1 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)a1;
 }
@@ -59,11 +63,11 @@ __device__ __forceinline__ void tr_addr(const bf16_t* t, int k0, int m0, int lan
 // Four operand fragments (columns m0 + 16 i, i = 0..3) of one 32-deep contraction step of
 // the transposed form, issued as one statement that also waits for them: every use of the
 // results follows the wait.
-template <int COLS>
+template <int COLS, bool MIX = false>
 __device__ __forceinline__ void tr_frags4(const bf16_t* t, int k0, int m0, int lane, bf16x8 (&f)[4]) {
   uint32_t a[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) tr_addr<COLS>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
+  for (int i = 0; i < 4; ++i) tr_addr<COLS, MIX>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
   uint2 r[8];
   asm volatile(
       "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\t"
@@ -80,11 +84,11 @@ __device__ __forceinline__ void tr_frags4(const bf16_t* t, int k0, int m0, int l
 }
 
 // The same for two fragments (columns m0 and m0 + 16).
-template <int COLS>
+template <int COLS, bool MIX = false>
 __device__ __forceinline__ void tr_frags2(const bf16_t* t, int k0, int m0, int lane, bf16x8 (&f)[2]) {
   uint32_t a[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) tr_addr<COLS>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
+  for (int i = 0; i < 2; ++i) tr_addr<COLS, MIX>(t, k0, m0 + 16 * i, lane, a[2 * i], a[2 * i + 1]);
   uint2 r[4];
   asm volatile(
       "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\t"
