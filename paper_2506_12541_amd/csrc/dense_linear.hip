@@ -2,8 +2,8 @@
 //   z = x w^T + bias, y = act(z) + res;   dz = dy act'(z), dx = dz w, dw = dz^T x, db = sum dz.
 // The three products are C[M, N] = sum_k A(m, k) B(n, k) with each operand stored either with
 // the contraction index fastest ("row" form: x and w of the forward, dz of dx) or with the
-// output index fastest ("column" form: w of dx, both operands of dw). bf16 operands feed the
-// bf16 matrix cores, f32 operands the f32 ones; sums, bias, activation and residual are
+// output index fastest ("column" form: w of dx, both operands of dw). The bf16 matrix cores
+// multiply, float32 tensors as three bf16 parts; sums, bias, activation and residual are
 // float32, rounded once to the storage type.
 #include <algorithm>
 #include <type_traits>
@@ -126,119 +126,279 @@ __device__ __forceinline__ uint4 load_piece(const Mat<T>& m, long long r, int c)
   return c + E <= m.cols ? load16u(p) : load_partial(p, m.cols - c);
 }
 
-// LDS tile of R operand rows x BK contraction indices, in the operand's own order: row form
-// [R][BK], column form [BK][R] (f32: 4 elements of padding a row). 16-byte pieces are
-// swizzled, except in the column form of f32, which is read element by element.
-template <typename T, bool TR, int R, int BK>
+// A product's operands as bf16 tiles in LDS: bf16 tensors are copied; a float32 value enters as the
+// sum of three bf16 values (P = 3 planes), x1 = bf16(x), x2 = bf16(x - x1), x3 = bf16(x - x1 - x2),
+// which holds its 24 bits, and a product as the six of nine part products that reach 2^-24 of it
+// (x2 y3, x3 y2, x3 y3 are left out, 2^-24 at most in all), accumulated in float32. That is 6 bf16
+// matrix instructions where the f32 ones take 16 times a bf16 one.
+struct Parts {
+  uint2 p[3];   // four values of each part
+};
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+// top: the largest magnitude split so far. Magnitudes of kNoSplit and above (what rounds to bf16
+// infinity, and infinity) do not split: a tile that holds one is formed again (plain_tile). NaN
+// splits into itself and NaN.
+constexpr float kNoSplit = 3.3895314e38f;   // the largest bf16 value
+__device__ __forceinline__ Parts split_parts(uint4 u, float& top) {
+  float v[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+  top = fmaxf(fmaxf(top, fabsf(v[0])), fabsf(v[1]));
+  top = fmaxf(fmaxf(top, fabsf(v[2])), fabsf(v[3]));
+  Parts r;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    r.p[k] = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    v[0] -= __uint_as_float(r.p[k].x << 16);
+    v[1] -= __uint_as_float(r.p[k].x & 0xffff0000u);
+    v[2] -= __uint_as_float(r.p[k].y << 16);
+    v[3] -= __uint_as_float(r.p[k].y & 0xffff0000u);
+  }
+  return r;
+}
+
+// A piece moved up by n elements (n < 0 or past its end: anything).
+template <typename T>
+__device__ __forceinline__ uint4 shift_piece(uint4 v, int n) {
+  const uint64_t lo = (uint64_t)v.x | (uint64_t)v.y << 32, hi = (uint64_t)v.z | (uint64_t)v.w << 32;
+  const int bits = n * 8 * (int)sizeof(T);
+  const uint64_t a = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
+  const uint64_t b = bits < 64 ? hi >> bits : 0;
+  return make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
+}
+
+// Tile of R operand rows x 32 contraction indices staged through registers, in the operand's own
+// order (row form [R][32], column form [32][R]); pieces outside the matrix are zero.
+template <typename T, bool TR, bool MIX, int R>
 struct RegTile {
-  static constexpr int E = 16 / (int)sizeof(T);
-  static constexpr int COLS = TR ? R : BK, ROWS = TR ? BK : R;
-  static constexpr int CPR = COLS / E;
-  static constexpr bool F32T = TR && sizeof(T) == 4;
-  static constexpr int LD = COLS + (F32T ? 4 : 0);
-  static constexpr int NV = ROWS * CPR / 256;
-  static constexpr int SIZE = ROWS * LD;
+  static constexpr int E = 16 / (int)sizeof(T), P = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int COLS = TR ? R : 32, ROWS = TR ? 32 : R, CPR = COLS / E;
+  static constexpr int NV = ROWS * CPR / 256, SIZE = R * 32;
   static_assert(NV * 256 == ROWS * CPR, "tile / thread split");
 
-  __device__ static int swz(int row) { return F32T ? 0 : CPR == 4 ? (row >> 1) & 3 : CPR == 8 ? row & 7 : 2 * (row & 7); }
-  // o0: first operand row of the tile, k0: first contraction index
-  __device__ static void load(uint4 (&v)[NV], const Mat<T>& m, long long o0, long long k0) {
+  const T* at[NV];   // this thread's pieces at contraction index 0; rows behind the matrix repeat its last
+  int shift[NV];     // column form: a piece that ends behind the row is loaded that many elements earlier
+
+  // o0: first operand row of the tile
+  __device__ __forceinline__ void init(const Mat<T>& m, long long o0) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int i = threadIdx.x + 256 * u, row = i / CPR, c = (i % CPR) * E;
+      if constexpr (TR) {
+        const int col = (int)o0 + c, in = max(min(col, m.cols - E), 0);
+        shift[u] = col - in;
+        at[u] = m.p + row * m.ld + in;
+      } else {
+        shift[u] = 0;
+        at[u] = m.p + (o0 + row < m.rows ? o0 + row : m.rows - 1) * m.ld + c;
+      }
+    }
+  }
+  // whole tiles: no branch lies between the loads and their use
+  __device__ __forceinline__ void load(uint4 (&v)[NV], const Mat<T>& m, long long k0) const {
+    const long long k = TR ? k0 * m.ld : k0;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) v[u] = load16u(at[u] + k);
+  }
+  __device__ __forceinline__ void settle(uint4 (&v)[NV], const Mat<T>& m, long long o0) const {
+    if constexpr (TR) {
+      if (o0 + R > m.cols) {   // uniform
+#pragma unroll
+        for (int u = 0; u < NV; ++u) v[u] = shift_piece<T>(v[u], shift[u]);
+      }
+    }
+  }
+  // the contraction's last, partial tile (k0: its first index)
+  __device__ __forceinline__ static void load_tail(uint4 (&v)[NV], const Mat<T>& m, long long o0, long long k0) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int i = threadIdx.x + 256 * u, row = i / CPR, c = (i % CPR) * E;
       v[u] = TR ? load_piece(m, k0 + row, (int)o0 + c) : load_piece(m, o0 + row, (int)k0 + c);
     }
   }
-  __device__ static void store(const uint4 (&v)[NV], T* t) {
+  __device__ __forceinline__ static void store(const uint4 (&v)[NV], bf16_t* t, float& top) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int i = threadIdx.x + 256 * u, row = i / CPR, c = i % CPR;
-      *reinterpret_cast<uint4*>(t + row * LD + E * (c ^ swz(row))) = v[u];
-    }
-  }
-  // Fragment of operand rows r0 + lane % 16 at contraction step ks (32 indices). PAIRS: the
-  // order of the transposing reads (4j.., 16 + 4j..), for a bf16 operand whose partner is in
-  // column form; else 8j...
-  template <bool PAIRS>
-  __device__ static typename Chunk<T>::type frag(const T* t, int r0, int ks, int lane) {
-    const int r = r0 + (lane & 15), j = lane >> 4;
-    if constexpr (!TR) {
-      const T* row = t + r * LD;
-      auto piece = [&](int c) { return *reinterpret_cast<const uint4*>(row + E * (c ^ swz(r))); };
-      if constexpr (sizeof(T) == 4) {
-        const uint4 a = piece(8 * ks + 2 * j), b = piece(8 * ks + 2 * j + 1);
-        return f32x8{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                     __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-      } else if constexpr (PAIRS) {
-        auto half = [&](int c) {
-          return *reinterpret_cast<const uint2*>(row + E * (c ^ swz(r)) + 4 * (j & 1));
-        };
-        const uint2 a = half(4 * ks + j / 2), b = half(4 * ks + 2 + j / 2);
-        return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+      const int i = threadIdx.x + 256 * u, row = i / CPR, c = (i % CPR) * E;
+      bf16_t* p = t + row * COLS + 8 * ((c >> 3) ^ tile_swz<COLS, TR && MIX>(row)) + (c & 7);
+      if constexpr (P == 1) {
+        *reinterpret_cast<uint4*>(p) = v[u];
       } else {
-        return __builtin_bit_cast(bf16x8, piece(4 * ks + j));
-      }
-    } else if constexpr (sizeof(T) == 4) {
-      f32x8 v;
+        const Parts s = split_parts(v[u], top);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = t[(32 * ks + 8 * j + e) * LD + r];
-      return v;
-    } else {
-      typedef short s16x4 __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-      const int p = lane & 15, col = r0 + 4 * (p & 3);
-      const int x0 = 32 * ks + 4 * j + (p >> 2), x1 = x0 + 16;
-      const T* a0 = t + x0 * LD + 8 * ((col >> 3) ^ swz(x0)) + (col & 7);
-      const T* a1 = t + x1 * LD + 8 * ((col >> 3) ^ swz(x1)) + (col & 7);
-      const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a0));
-      const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a1));
-      return __builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y));
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(p + k * SIZE) = s.p[k];
+      }
     }
   }
 };
 
-// 4 waves in a 2 x 2 arrangement; the next tile is in registers while one is multiplied.
+// The NF fragments of operand rows r0 + 16 i of a staged tile at contraction step ks; TR: the tile
+// is in column form, COLS operand rows wide; MIX: the partner is in the other form.
+template <bool TR, bool MIX, int BK, int COLS, int NF>
+struct Frags {
+  __device__ __forceinline__ static void read(const bf16_t* t, int r0, int ks, int lane, bf16x8 (&f)[NF]) {
+    if constexpr (!TR) {
+#pragma unroll
+      for (int i = 0; i < NF; ++i) f[i] = frag_row<BK>(t, r0 + 16 * i + (lane & 15), 4 * ks + (lane >> 4));
+    } else if constexpr (NF % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < NF; i += 4)
+        tr_frags4<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[4]>(&f[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NF; i += 2)
+        tr_frags2<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[2]>(&f[i]));
+    }
+  }
+};
+
+// Accumulators of a float32 wave tile by f32 matrix instructions, straight from memory: for tiles
+// with values that do not split into bf16 parts.
+template <bool TA, bool TB, int FI, int FJ>
+__device__ __forceinline__ void plain_tile(const Mat<float>& a, const Mat<float>& b, long long m0, long long n0, long long k0,
+                                        long long k1, int lane, f32x4 (&acc)[FI][FJ]) {
+  const int r = lane & 15, j = lane >> 4;
+  auto at = [](const Mat<float>& m, bool tr, long long o, long long k) {
+    const long long row = tr ? k : o, col = tr ? o : k;
+    return row < m.rows && col < m.cols ? m.p[row * m.ld + col] : 0.f;
+  };
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int jj = 0; jj < FJ; ++jj) acc[i][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (long long k = k0; k < k1; k += 4) {
+    float x[FI], y[FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i) x[i] = k + j < k1 ? at(a, TA, m0 + 16 * i + r, k + j) : 0.f;
+#pragma unroll
+    for (int i = 0; i < FJ; ++i) y[i] = k + j < k1 ? at(b, TB, n0 + 16 * i + r, k + j) : 0.f;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int jj = 0; jj < FJ; ++jj) acc[i][jj] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[jj], x[i], acc[i][jj], 0, 0, 0);
+  }
+}
+
+// Schedule of an iteration with VALU instructions of splitting beside 6 MF matrix instructions: the
+// former between the latter, so that both pipes work in one wave.
+template <int P, int MF, int VALU>
+__device__ __forceinline__ void interleave() {
+  constexpr int N = 6 * MF, per = (VALU + N - 1) / N;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x2, per, 0);
+  }
+}
+
+// 4 waves in a 2 x 2 arrangement. Tiles pass from memory through registers (two in flight) into
+// one of two LDS buffers: the next tile is split and stored while the current one is multiplied,
+// and an iteration has one barrier, without a fence (that of __syncthreads would wait for the
+// tiles in flight). float32 at 4096^3: 770 us, 178 TFLOP/s (f32 matrix instructions reach 151);
+// the matrix cores are busy 45% of the time, the VALU (splitting) 42%.
 // Accumulator lane L holds C[m + L % 16][n + 4 (L / 16) + e] (B's fragment comes first).
 template <typename T, bool TA, bool TB, int BM, int BN>
 __global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long long K, int ntn, long long kt_per, Epi<T> o) {
   constexpr int BK = 32, FI = BM / 32, FJ = BN / 32;
-  typedef RegTile<T, TA, BM, BK> LA;
-  typedef RegTile<T, TB, BN, BK> LB;
-  __shared__ __attribute__((aligned(16))) T as[LA::SIZE], bs[LB::SIZE];
+  typedef RegTile<T, TA, TA != TB, BM> LA;
+  typedef RegTile<T, TB, TA != TB, BN> LB;
+  constexpr int P = LA::P;
+  __shared__ __attribute__((aligned(1024))) bf16_t as[2][P * LA::SIZE], bs[2][P * LB::SIZE];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wm = wid >> 1, wn = wid & 1;
   const int tm = blockIdx.x / ntn, tn = blockIdx.x - tm * ntn;
   const long long m0 = (long long)tm * BM;
   const int n0 = tn * BN;
   const long long nkt = (K + BK - 1) / BK;
-  const long long kt0 = blockIdx.y * kt_per, kt1 = kt0 + kt_per < nkt ? kt0 + kt_per : nkt;
+  // whole tiles; none where a column-form operand is narrower than a piece
+  const long long nwhole = (TA && a.cols < LA::E) || (TB && b.cols < LB::E) ? 0 : K / BK;
+  const long long kt0 = min(blockIdx.y * kt_per, nkt), kt1 = min(kt0 + kt_per, nkt), kw = min(kt1, nwhole);
   f32x4 acc[FI][FJ];
 #pragma unroll
   for (int i = 0; i < FI; ++i)
 #pragma unroll
     for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  uint4 av[LA::NV], bv[LB::NV];
-  if (kt0 < kt1) {
-    LA::load(av, a, m0, kt0 * BK);
-    LB::load(bv, b, n0, kt0 * BK);
-  }
-  for (long long kt = kt0; kt < kt1; ++kt) {
-    __syncthreads();
-    LA::store(av, as);
-    LB::store(bv, bs);
-    __syncthreads();
-    if (kt + 1 < kt1) {
-      LA::load(av, a, m0, (kt + 1) * BK);
-      LB::load(bv, b, n0, (kt + 1) * BK);
+  LA la;
+  LB lb;
+  la.init(a, m0);
+  lb.init(b, n0);
+  float top = 0.f;
+  uint4 av[2][LA::NV], bv[2][LB::NV];
+  auto load = [&](int d, long long kt) {
+    la.load(av[d], a, kt * BK);
+    lb.load(bv[d], b, kt * BK);
+  };
+  auto store = [&](int d, int buf) {
+    la.settle(av[d], a, m0);
+    lb.settle(bv[d], b, n0);
+    LA::store(av[d], as[buf], top);
+    LB::store(bv[d], bs[buf], top);
+  };
+  bf16x8 af[P][FI], bf[P][FJ];
+  auto frags = [&](int buf) {
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      Frags<TA, TA != TB, BK, BM, FI>::read(as[buf] + k * LA::SIZE, wm * (BM / 2), 0, lane, af[k]);
+      Frags<TB, TA != TB, BK, BN, FJ>::read(bs[buf] + k * LB::SIZE, wn * (BN / 2), 0, lane, bf[k]);
     }
-    typename Chunk<T>::type af[FI], bf[FJ];
-#pragma unroll
-    for (int i = 0; i < FI; ++i) af[i] = LA::template frag<TB>(as, wm * (BM / 2) + 16 * i, 0, lane);
-#pragma unroll
-    for (int j = 0; j < FJ; ++j) bf[j] = LB::template frag<TA>(bs, wn * (BN / 2) + 16 * j, 0, lane);
+  };
+  auto multiply_parts = [&](int ka, int kb) {
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
-      for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bf[j], af[i], acc[i][j]);
+      for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bf[kb][j], af[ka][i], acc[i][j]);
+  };
+  auto multiply = [&]() {
+    if constexpr (P == 3) {   // the small part products first
+      multiply_parts(2, 0);
+      multiply_parts(0, 2);
+      multiply_parts(1, 1);
+      multiply_parts(1, 0);
+      multiply_parts(0, 1);
+    }
+    multiply_parts(0, 0);
+  };
+  if (kt0 < kw) {
+    load(0, kt0);
+    load(1, min(kt0 + 1, kw - 1));
+    store(0, 0);
+    load(0, min(kt0 + 2, kw - 1));
+  }
+  // loads past the last whole tile repeat it (never used), so that no branch surrounds them
+  auto iterate = [&](long long kt, int d) {
+    // tile kt lies in buffer d, kt + 1 in register set 1 - d, kt + 2 in set d
+    lgkm_drain();
+    lds_barrier();   // tile kt is visible; every wave has its fragments of kt - 1
+    frags(d);
+    store(1 - d, 1 - d);
+    load(1 - d, min(kt + 3, kw - 1));
+    multiply();
+    if constexpr (P == 3) interleave<P, FI * FJ, (LA::NV + LB::NV) * 30>();
+  };
+  long long t = kt0;
+  for (; t + 1 < kw; t += 2) {
+    iterate(t, 0);
+    iterate(t + 1, 1);
+  }
+  if (t < kw) iterate(t, 0);
+  for (long long kt = max(kt0, kw); kt < kt1; ++kt) {
+    LA::load_tail(av[0], a, m0, kt * BK);
+    LB::load_tail(bv[0], b, n0, kt * BK);
+    __syncthreads();
+    LA::store(av[0], as[0], top);
+    LB::store(bv[0], bs[0], top);
+    __syncthreads();
+    frags(0);
+    multiply();
+  }
+  if constexpr (P == 3) {
+    __shared__ int again;
+    if (threadIdx.x == 0) again = 0;
+    __syncthreads();
+    if (top >= kNoSplit) again = 1;
+    __syncthreads();
+    if (again)
+      plain_tile<TA, TB, FI, FJ>(a, b, m0 + wm * (BM / 2), n0 + wn * (BN / 2), kt0 * BK, min(kt1 * BK, K), lane, acc);
   }
 #pragma unroll
   for (int i = 0; i < FI; ++i)
@@ -286,26 +446,6 @@ struct DmaTile {
       const int i = (wid * NU + u) * 64 + lane, row = i / CPR;
       const int c = 8 * ((i % CPR) ^ tile_swz<COLS, TR && MIX>(row));
       *reinterpret_cast<uint4*>(lds + 8 * i) = TR ? load_piece(m, k0 + row, (int)o0 + c) : load_piece(m, o0 + row, (int)k0 + c);
-    }
-  }
-};
-
-// The NF fragments of operand rows r0 + 16 i of a staged tile at contraction step ks; TR: the tile
-// is in column form, COLS operand rows wide; MIX: the partner is in the other form.
-template <bool TR, bool MIX, int BK, int COLS, int NF>
-struct Frags {
-  __device__ __forceinline__ static void read(const bf16_t* t, int r0, int ks, int lane, bf16x8 (&f)[NF]) {
-    if constexpr (!TR) {
-#pragma unroll
-      for (int i = 0; i < NF; ++i) f[i] = frag_row<BK>(t, r0 + 16 * i + (lane & 15), 4 * ks + (lane >> 4));
-    } else if constexpr (NF % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < NF; i += 4)
-        tr_frags4<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[4]>(&f[i]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < NF; i += 2)
-        tr_frags2<COLS, MIX>(t, 32 * ks, r0 + 16 * i, lane, *reinterpret_cast<bf16x8(*)[2]>(&f[i]));
     }
   }
 };
@@ -606,6 +746,12 @@ struct Plan {
 Plan plan_product(bool bf16, long long M, int N, long long K, bool may_split) {
   auto tiles = [&](int T) { return ((M + T - 1) / T) * ((N + T - 1) / T); };
   Plan p{128, 1};
+  if (!bf16) {
+    if (tiles(128) < 512) p.T = 64;
+    if (may_split)
+      while (tiles(p.T) * p.S < 768 && K / (2 * p.S) >= 256 && p.S < 64) p.S *= 2;
+    return p;
+  }
   if (bf16 && (tiles(256) >= 192 || (may_split && tiles(256) * (K / 512) >= 192)))
     p.T = 256;
   else if (tiles(128) < 256 && !(may_split && tiles(128) * (K / 512) >= 256))

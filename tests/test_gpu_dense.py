@@ -158,6 +158,28 @@ def test_linear_no_rows_and_rows_that_are_not_finite():
         assert (y[0] == k).all() and y[1].isinf().all() and y[2].isnan().all() and (y[3:] == k).all()
 
 
+def test_linear_float32_values_that_do_not_split():
+    """Infinities, NaN and the largest float32 values go through the three-part products as through one."""
+    big = torch.finfo(F32).max
+    for m, k, n in ((5, 40, 24), (200, 70, 130), (700, 513, 300)):
+        g = gen(m)
+        x, w = normal(g, m, k), normal(g, n, k, scale=0.1)
+        x[0, k - 1] = math.inf
+        x[1, 3] = math.nan
+        x[2] = 0
+        x[2, 5] = big
+        w[:, 5] = 0.5
+        x[3] = 2.0 ** -120                       # its parts reach into the denormal numbers
+        y, _ = dense.linear_forward(x, w)
+        want = x.double().cpu() @ w.double().cpu().t()
+        inf = torch.sign(w[:, k - 1]) * math.inf
+        assert torch.equal(y[0], inf) and y[1].isnan().all() and (y[2] == big / 2).all()
+        size = x[3:].double().cpu().abs() @ w.double().cpu().abs().t()
+        ref.check("y", y[3:], want[3:], (k + 2) * ref.F * size + 2.0 ** -140)
+        got = dense.linear_backward(x, w, torch.ones(m, n, device="cuda"))
+        assert got["dw"][:, 3].isnan().all() and torch.equal(got["dw"][:, k - 1], torch.full((n,), math.inf, device="cuda"))
+
+
 # ---- packed attention ----
 
 def packed(lens):
