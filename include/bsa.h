@@ -368,7 +368,8 @@ typedef struct {
   int32_t seqs;                         /* >= 1                                         */
   int32_t heads, kv_heads;              /* kv_heads divides heads                       */
   int32_t head_dim;                     /* 32, 64 or 128                                */
-  int64_t total_q, total_k;             /* rows of q and of k and v, 0 .. 2^31 - 1      */
+  int64_t total_q, total_k;             /* rows of q and of k and v; total_q times
+                                           heads / kv_heads and total_k <= 2^30         */
   int32_t causal;                       /* 0 or 1                                       */
   int32_t dtype;                        /* bsa_dtype_t of q, k, v, o, d_o, dq, dk, dv   */
   float softmax_scale;                  /* 0 -> 1/sqrt(head_dim)                        */

@@ -79,9 +79,8 @@ bsa_status_t check(const bsa_attention_t* p, bsa::AttnArgs* a) {
     return set_error(BSA_ERR_UNSUPPORTED, "head_dim must be 32, 64 or 128");
   if (p->total_q < 0 || p->total_q > INT32_MAX || p->total_k < 0 || p->total_k > INT32_MAX)
     return bad("total_q and total_k must be in [0, 2^31)");
-  if (p->total_q * (p->heads / p->kv_heads) / 16 + p->seqs > INT32_MAX || p->total_k / 16 + p->seqs > INT32_MAX ||
-      p->total_q * p->heads > ((int64_t)1 << 33))
-    return set_error(BSA_ERR_UNSUPPORTED, "too many query rows times heads");
+  if (p->total_q * (p->heads / p->kv_heads) > ((int64_t)1 << 30) || p->total_k > ((int64_t)1 << 30) || p->seqs > (1 << 24))
+    return set_error(BSA_ERR_UNSUPPORTED, "query rows times heads / kv_heads and key rows must be <= 2^30, seqs <= 2^24");
   if (p->causal != 0 && p->causal != 1) return bad("causal must be 0/1");
   if (p->zero_rest != 0 && p->zero_rest != 1) return bad("zero_rest must be 0/1");
   if (!dtype_ok(p->dtype)) return bad("bad dtype");

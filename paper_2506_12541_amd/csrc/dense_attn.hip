@@ -19,6 +19,7 @@
 // workgroup finds its sequence by a 64-way search and leaves when its tile is empty.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 #include "attn_common.hpp"
@@ -42,13 +43,64 @@ __device__ __forceinline__ long long clampll(long long x, long long lo, long lon
   return x < lo ? lo : x > hi ? hi : x;
 }
 
-// The sequence that owns tile slot `slot` of rows-per-tile R (mult packed rows for each row of
-// cu). Offsets outside the tensors are pulled inside: no read or write leaves them.
-__device__ __forceinline__ Seq find_seq(long long slot, const int* cu, int mult, int R, const int* cu_q,
-                                        const int* cu_k, const int* used_k, int S, long long total_q,
-                                        long long total_k) {
+struct SeqArgs {
+  const int *cu_q, *cu_k, *used_k;
+  int S;
+  long long total_q, total_k;
+};
+
+// Offsets outside the tensors are pulled inside: no read or write leaves them.
+__device__ __forceinline__ Seq seq_at(const SeqArgs& a, int s) {
+  Seq q;
+  q.s = s;
+  q.q0 = clampll(a.cu_q[s], 0, a.total_q);
+  q.k0 = clampll(a.cu_k[s], 0, a.total_k);
+  q.lq = (int)(clampll(a.cu_q[s + 1], q.q0, a.total_q) - q.q0);
+  q.ek = (int)(clampll(a.cu_k[s + 1], q.k0, a.total_k) - q.k0);
+  q.lk = a.used_k ? (int)clampll(a.used_k[s], 0, q.ek) : q.ek;
+  q.eq = q.lq;
+  if (s + 1 == a.S) {
+    q.eq = (int)(a.total_q - q.q0);
+    q.ek = (int)(a.total_k - q.k0);
+  }
+  q.tile = 0;
+  return q;
+}
+
+// The sequence and tile that `slot` stands for, in tiles of R packed query rows (KEYS: of R key
+// rows); mult packed rows for each row of cu; rest: rows behind the sequence's are covered too.
+//
+// Up to 64 sequences: those with the most work a tile come first (a tile's work is the other
+// side's length), found from every lane holding one sequence, so that the last workgroups to
+// finish are short ones (16 clouds of 1800 to 3586 rows in rising order, 8 heads of 64: the
+// key-major pass took 716 us in that order, 641 so, with the XCD numbering below). More: in their
+// order, sequence s from slot floor(cu[s] mult / R) + s on, by a 64-way search.
+template <bool KEYS>
+__device__ __forceinline__ Seq find_seq(long long slot, const SeqArgs& a, int mult, int R, bool rest) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, n = S;
+  Seq q;
+  if (a.S <= 64) {
+    const Seq me = seq_at(a, min(lane, a.S - 1));
+    const long long mine = KEYS ? (rest ? me.ek : me.lk) : (long long)(rest ? me.eq : me.lq) * mult;
+    const int n = lane < a.S ? (int)((mine + R - 1) / R) : 0, weight = KEYS ? me.lq : me.lk;
+    int before = 0;     // tiles of the sequences that come first
+    for (int i = 0; i < a.S; ++i) {
+      const int w = __builtin_amdgcn_readlane(weight, i), m = __builtin_amdgcn_readlane(n, i);
+      before += w > weight || (w == weight && i < lane) ? m : 0;
+    }
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(slot >= before && slot < before + n);
+    if (hit == 0) {
+      q = seq_at(a, 0);
+      q.tile = -1;
+      return q;
+    }
+    const int s = __builtin_ctzll(hit);
+    q = seq_at(a, s);
+    q.tile = slot - __builtin_amdgcn_readlane(before, s);
+    return q;
+  }
+  const int* cu = KEYS ? a.cu_k : a.cu_q;
+  int lo = 0, n = a.S;
   while (n > 1) {
     const int step = (n + 63) / 64;
     const int i = lane * step;
@@ -57,18 +109,26 @@ __device__ __forceinline__ Seq find_seq(long long slot, const int* cu, int mult,
     lo += c * step;
     n = min(step, n - c * step);
   }
-  Seq q;
-  q.s = __builtin_amdgcn_readfirstlane(lo);
-  const long long qb = clampll(cu_q[q.s], 0, total_q), kb = clampll(cu_k[q.s], 0, total_k);
-  q.q0 = qb;
-  q.k0 = kb;
-  q.lq = (int)(clampll(cu_q[q.s + 1], qb, total_q) - qb);
-  q.ek = (int)(clampll(cu_k[q.s + 1], kb, total_k) - kb);
-  q.lk = used_k ? (int)clampll(used_k[q.s], 0, q.ek) : q.ek;
-  q.eq = q.s + 1 < S ? q.lq : (int)(total_q - qb);
-  if (q.s + 1 >= S) q.ek = (int)(total_k - kb);
+  q = seq_at(a, __builtin_amdgcn_readfirstlane(lo));
   q.tile = slot - ((long long)cu[q.s] * mult / R + q.s);
   return q;
+}
+
+// Workgroups are dealt to the 8 XCDs round-robin by linear id, and each XCD has its own L2: the
+// grid (x tile slots, a multiple of 8; y key heads) is renumbered so that the workgroups of a key
+// head run on as few XCDs as possible. A bijection for 8 k key heads or a divisor of 8; else
+// the grid is kept.
+__device__ __forceinline__ void xcd_slot(int& slot, int& hk) {
+  const unsigned nx = gridDim.x, ny = gridDim.y, lin = blockIdx.x + nx * blockIdx.y, c = lin % 8, i = lin / 8;
+  slot = blockIdx.x;
+  hk = blockIdx.y;
+  if (ny % 8 == 0) {
+    hk = c + 8 * (i / nx);
+    slot = i % nx;
+  } else if (8 % ny == 0) {
+    hk = c % ny;
+    slot = i * (8 / ny) + c / ny;
+  }
 }
 
 template <typename T> struct AttnTile {
@@ -124,14 +184,25 @@ __device__ __forceinline__ f32x8 col_frag(const float* t, int k0, int m0, int la
   return v;
 }
 
+// Quotients by the group size: floor(x / G) by a multiplication, one too large at most (x < 2^31).
+struct Group {
+  int G;
+  uint32_t magic;    // floor(2^32 / G) + 1
+  __device__ __forceinline__ int div(int x) const {
+    if (G == 1) return x;
+    const int q = (int)__umulhi((uint32_t)x, magic);
+    return q * G > x ? q - 1 : q;
+  }
+};
+
 // Element offsets of a packed row: query row t = q0 + p / G, head hk G + p % G.
 struct RowAt {
   long long t;
   int h;
 };
-__device__ __forceinline__ RowAt packed_row(const Seq& sq, int hk, int G, long long p) {
-  const int q = (int)(p / G);
-  return RowAt{sq.q0 + q, hk * G + (int)(p - (long long)q * G)};
+__device__ __forceinline__ RowAt packed_row(const Seq& sq, int hk, const Group& g, int p) {
+  const int q = g.div(p);
+  return RowAt{sq.q0 + q, hk * g.G + p - q * g.G};
 }
 
 // The same for packed rows r0 + [0, ROWS) (rows of them, > 0).
@@ -140,7 +211,7 @@ struct PackedLoad {
   static constexpr int E = 16 / (int)sizeof(T), CPR = HD / E, NI = ROWS * CPR / 64;
   static_assert(NI % kWaves == 0, "tile / wave split");
   __device__ __forceinline__ static void issue(T* lds, const T* g, long long row_ld, long long head_ld, const Seq& sq,
-                                               int hk, int G, long long r0, long long rows, int wid, int lane) {
+                                               int hk, const Group& G, int r0, int rows, int wid, int lane) {
 #pragma unroll
     for (int u = 0; u < NI / kWaves; ++u) {
       const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
@@ -156,7 +227,8 @@ struct PackedLoad {
 struct FwdP {
   AttnArgs a;
   const void *q, *k, *v;
-  const int *cu_q, *cu_k, *used_k;
+  SeqArgs seq;
+  Group G;
   void* o;
   float* lse;
   float sl2;         // scale log2(e)
@@ -178,19 +250,22 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
   typedef typename Chunk<T>::type CT;
   __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
   const AttnArgs& a = p.a;
-  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const Seq sq = find_seq(blockIdx.x, p.cu_q, G, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
-  const long long rows = (long long)sq.lq * G, ext = (long long)sq.eq * G;
+  int slot, hk;
+  xcd_slot(slot, hk);
+  const Seq sq = find_seq<false>(slot, p.seq, G.G, R, a.zero_rest);
+  const int rows = sq.lq * G.G, ext = sq.eq * G.G;
   // tiles in descending order: with a causal mask the longest rows come first
-  const long long nt = (rows + R - 1) / R;
+  const int nt = (rows + R - 1) / R;
   const long long tile = sq.tile < nt ? nt - 1 - sq.tile : sq.tile;
-  const long long p0 = tile * R;
-  if (p0 < 0 || p0 >= ext || (p0 >= rows && (!a.zero_rest || p.nsplit > 1))) return;
+  if (tile < 0 || tile * R >= ext) return;
+  const int p0 = (int)tile * R;
+  if (p0 >= ext || (p0 >= rows && (!a.zero_rest || p.nsplit > 1))) return;
   T* const out = (T*)p.o;
 
-  long long pr[QB];
+  int pr[QB];
   int lim[QB];        // the last key that this lane's query sees
   CT qf[QB][NCH];
   f32x4 o[QB][DB];
@@ -213,14 +288,13 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
   // the workgroup's keys: its split's, cut behind the last key that its last query sees
   int k_lo, k_hi;
   split_range(sq.lk, p.nsplit, blockIdx.z, KT, k_lo, k_hi);
-  const long long plast = min(p0 + R, rows) - 1;
+  const int plast = min(p0 + R, rows) - 1;
   if (p0 >= rows)
     k_hi = k_lo;
   else if (a.causal)
-    k_hi = max(min(k_hi, (int)(plast / G) + off + 1), k_lo);
-  // keys up to here are seen by every query of this wave
-  const long long wfirst = p0 + wid * QB * 16;
-  const int all = wfirst >= rows ? 0 : a.causal ? min((int)(wfirst / G) + off + 1, sq.lk) : sq.lk;
+    k_hi = max(min(k_hi, G.div(plast) + off + 1), k_lo);
+  // keys up to here are seen by every query of the workgroup: tiles below need no mask
+  const int all = min(a.causal ? max(G.div(min(p0, rows)) + off + 1, 0) : sq.lk, k_hi);
 
   const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
   const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
@@ -228,7 +302,7 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
     TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
     TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
   };
-  auto step = [&](int t0, const T* kc, const T* vc, T* kn, T* vn) {
+  auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
     vm_drain();
     __syncthreads();
     if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
@@ -242,12 +316,11 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
         for (int qb = 0; qb < QB; ++qb)
           s[qb][kb] = mma(kf, qf[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qb][kb]);
       }
-    const bool mask = t0 + KT > all;
     CT pf[QB][KB / 2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float tmax = kNegInf;
-      if (mask) {
+      if constexpr (decltype(mask)::value) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -294,9 +367,14 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
   };
   if (k_lo < k_hi) {
     issue(k_lo, ks0, vs0);
-    for (int t0 = k_lo; t0 < k_hi; t0 += 2 * KT) {
-      step(t0, ks0, vs0, ks1, vs1);
-      if (t0 + KT < k_hi) step(t0 + KT, ks1, vs1, ks0, vs0);
+    int t0 = k_lo;
+    for (; t0 + 2 * KT <= all; t0 += 2 * KT) {
+      step(std::false_type{}, t0, ks0, vs0, ks1, vs1);
+      step(std::false_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+    }
+    for (; t0 < k_hi; t0 += 2 * KT) {
+      step(std::true_type{}, t0, ks0, vs0, ks1, vs1);
+      if (t0 + KT < k_hi) step(std::true_type{}, t0 + KT, ks1, vs1, ks0, vs0);
     }
   }
 #pragma unroll
@@ -334,7 +412,7 @@ __global__ void __launch_bounds__(256) packed_join_kernel(FwdP p) {
   if (row >= a.total_q * a.heads) return;
   const long long t = row / a.heads;
   const int h = (int)(row - t * a.heads);
-  const bool in = t < p.cu_q[a.seqs];
+  const bool in = t < p.seq.cu_q[a.seqs];
   if (!in && !a.zero_rest) return;
   float m = kNegInf, l = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
@@ -360,7 +438,8 @@ struct BwdP {
   AttnArgs a;
   const void *q, *k, *v, *o, *d_o;
   const float* lse;
-  const int *cu_q, *cu_k, *used_k;
+  SeqArgs seq;
+  Group G;
   void *dq, *dk, *dv;
   float2* terms;     // [kv_heads][total_q G] packed rows: lse in log2 units (+inf: sees nothing), D
   float sl2;
@@ -373,17 +452,20 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
   typedef typename Chunk<T>::type CT;
   __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
   const AttnArgs& a = p.a;
-  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const Seq sq = find_seq(blockIdx.x, p.cu_q, G, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
-  const long long rows = (long long)sq.lq * G, ext = (long long)sq.eq * G;
-  const long long nt = (rows + R - 1) / R;
+  int slot, hk;
+  xcd_slot(slot, hk);
+  const Seq sq = find_seq<false>(slot, p.seq, G.G, R, a.zero_rest);
+  const int rows = sq.lq * G.G, ext = sq.eq * G.G;
+  const int nt = (rows + R - 1) / R;
   const long long tile = sq.tile < nt ? nt - 1 - sq.tile : sq.tile;
-  const long long p0 = tile * R;
-  if (p0 < 0 || p0 >= ext || (p0 >= rows && !a.zero_rest)) return;
+  if (tile < 0 || tile * R >= ext) return;
+  const int p0 = (int)tile * R;
+  if (p0 >= ext || (p0 >= rows && !a.zero_rest)) return;
 
-  long long pr[QB];
+  int pr[QB];
   int lim[QB];
   CT qf[QB][NCH], df[QB][NCH];
   f32x4 acc[QB][DB];
@@ -413,14 +495,13 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
     }
     dd[qb] = col_sum(d);
     l2[qb] = on && lim[qb] >= 0 ? p.lse[at.h * a.total_q + at.t] * kLog2e : __builtin_huge_valf();
-    if (on && j == 0) p.terms[((long long)hk * a.total_q + sq.q0) * G + pr[qb]] = make_float2(l2[qb], dd[qb]);
+    if (on && j == 0) p.terms[((long long)hk * a.total_q + sq.q0) * G.G + pr[qb]] = make_float2(l2[qb], dd[qb]);
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const long long plast = min(p0 + R, rows) - 1;
-  const int k_hi = p0 >= rows ? 0 : a.causal ? max(min(sq.lk, (int)(plast / G) + off + 1), 0) : sq.lk;
-  const long long wfirst = p0 + wid * QB * 16;
-  const int all = wfirst >= rows ? 0 : a.causal ? min((int)(wfirst / G) + off + 1, sq.lk) : sq.lk;
+  const int plast = min(p0 + R, rows) - 1;
+  const int k_hi = p0 >= rows ? 0 : a.causal ? max(min(sq.lk, G.div(plast) + off + 1), 0) : sq.lk;
+  const int all = min(a.causal ? max(G.div(min(p0, rows)) + off + 1, 0) : sq.lk, k_hi);
 
   const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
   const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
@@ -428,11 +509,10 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
     TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
     TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
   };
-  auto step = [&](int t0, const T* kc, const T* vc, T* kn, T* vn) {
+  auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
     vm_drain();
     __syncthreads();
     if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
-    const bool mask = t0 + KT > all;
 #pragma unroll
     for (int kp = 0; kp < KT / 32; ++kp) {
       f32x4 s[QB][2], g[QB][2];
@@ -445,7 +525,7 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) {
             s[qb][kb] = mma(kf, qf[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qb][kb]);
-            g[qb][kb] = mma(vf, df[qb][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : g[qb][kb]);
+            g[qb][kb] = mma(vf, df[qb][c], c == 0 ? f32x4{-dd[qb], -dd[qb], -dd[qb], -dd[qb]} : g[qb][kb]);
           }
         }
       CT ds[QB];
@@ -457,9 +537,9 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float pv = fast_exp2(__builtin_fmaf(s[qb][kb][i], p.sl2, -l2[qb]));
-            float x = pv * (g[qb][kb][i] - dd[qb]);
-            if (mask && t0 + kp * 32 + kb * 16 + 4 * j + i > lim[qb]) x = 0.f;
-            v8[4 * kb + i] = x;
+            const float x = pv * g[qb][kb][i];
+            const bool see = !decltype(mask)::value || t0 + kp * 32 + kb * 16 + 4 * j + i <= lim[qb];
+            v8[4 * kb + i] = see ? x : 0.f;
           }
         ds[qb] = make_chunk<T>(v8);
       }
@@ -473,9 +553,14 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
   };
   if (k_hi > 0) {
     issue(0, ks0, vs0);
-    for (int t0 = 0; t0 < k_hi; t0 += 2 * KT) {
-      step(t0, ks0, vs0, ks1, vs1);
-      if (t0 + KT < k_hi) step(t0 + KT, ks1, vs1, ks0, vs0);
+    int t0 = 0;
+    for (; t0 + 2 * KT <= all; t0 += 2 * KT) {
+      step(std::false_type{}, t0, ks0, vs0, ks1, vs1);
+      step(std::false_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+    }
+    for (; t0 < k_hi; t0 += 2 * KT) {
+      step(std::true_type{}, t0, ks0, vs0, ks1, vs1);
+      if (t0 + KT < k_hi) step(std::true_type{}, t0 + KT, ks1, vs1, ks0, vs0);
     }
   }
 #pragma unroll
@@ -495,26 +580,28 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
   constexpr int QT = AttnTile<T>::keys, NCH = HD / 32, DB = HD / 16, R = 16 * KW * kWaves;
   typedef typename Chunk<T>::type CT;
   __shared__ __attribute__((aligned(1024))) T qs0[QT * HD], ds0[QT * HD], qs1[QT * HD], ds1[QT * HD];
-  __shared__ __attribute__((aligned(16))) float2 tm0[QT], tm1[QT];
+  __shared__ __attribute__((aligned(16))) float tm0[2 * QT], tm1[2 * QT];   // lse, then -D, of the tile's rows
   const AttnArgs& a = p.a;
-  const int G = a.heads / a.kv_heads, hk = blockIdx.y;
+  const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const Seq sq = find_seq(blockIdx.x, p.cu_k, 1, R, p.cu_q, p.cu_k, p.used_k, a.seqs, a.total_q, a.total_k);
+  int slot, hk;
+  xcd_slot(slot, hk);
+  const Seq sq = find_seq<true>(slot, p.seq, 1, R, a.zero_rest);
   const long long k0 = sq.tile * R;
   if (k0 < 0 || k0 >= sq.ek || (k0 >= sq.lk && !a.zero_rest)) return;
-  const long long rows = (long long)sq.lq * G;
+  const int rows = sq.lq * G.G;
   const int off = sq.lk - sq.lq;
 
   int key[KW];
-  long long first[KW];     // the first packed row that sees this lane's key
+  int first[KW];           // the first packed row that sees this lane's key
   CT kf[KW][NCH], vf[KW][NCH];
   f32x4 dk[KW][DB], dv[KW][DB];
 #pragma unroll
   for (int w = 0; w < KW; ++w) {
     key[w] = (int)k0 + (wid * KW + w) * 16 + r;
     const bool on = key[w] < sq.lk;
-    first[w] = !on ? rows : a.causal ? max((long long)(key[w] - off), 0LL) * G : 0;
+    first[w] = !on ? rows : a.causal ? max(key[w] - off, 0) * G.G : 0;
     const long long row = sq.k0 + (on ? key[w] : 0);
     const T* kp = (const T*)p.k + row * a.k_row + hk * a.k_head;
     const T* vp = (const T*)p.v + row * a.v_row + hk * a.v_head;
@@ -529,30 +616,33 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
       dv[w][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
-  // rows from here on are seen by every key of the wave (causal: by its last)
-  const long long wkey = k0 + (wid * KW + KW) * 16 - 1;
-  const long long all = wkey >= sq.lk ? rows : a.causal ? max(wkey - off, 0LL) * G : 0;
-  const long long p_lo = k0 >= sq.lk ? rows : a.causal ? max(k0 - off, 0LL) * G / QT * QT : 0;
+  // Rows from here on see every key of the workgroup. Only the causal diagonal is masked: rows
+  // behind the sequence's last repeat it with an lse of +inf (P = 0), and what keys behind its end
+  // sum up is not stored.
+  const int all = a.causal ? max((int)min(k0 + R, (long long)sq.lk) - 1 - off, 0) * G.G : 0;
+  const int p_lo = k0 >= sq.lk ? rows : a.causal ? max((int)k0 - off, 0) * G.G / QT * QT : 0;
 
   // tile rows are packed rows: query and head vary by row
-  auto issue = [&](long long t0, T* qd, T* dd, float2* td) {
+  auto issue = [&](int t0, T* qd, T* dd, float* td) {
     PackedLoad<T, HD, QT>::issue(qd, (const T*)p.q, a.q_row, a.q_head, sq, hk, G, t0, rows, wid, lane);
     PackedLoad<T, HD, QT>::issue(dd, (const T*)p.d_o, a.do_row, a.do_head, sq, hk, G, t0, rows, wid, lane);
-    if (threadIdx.x < QT)
-      td[threadIdx.x] = t0 + threadIdx.x < rows ? p.terms[((long long)hk * a.total_q + sq.q0) * G + t0 + threadIdx.x]
-                                                : make_float2(__builtin_huge_valf(), 0.f);
+    if (threadIdx.x < QT) {
+      const float2 t = t0 + threadIdx.x < rows ? p.terms[((long long)hk * a.total_q + sq.q0) * G.G + t0 + threadIdx.x]
+                                               : make_float2(__builtin_huge_valf(), 0.f);
+      td[threadIdx.x] = t.x;
+      td[QT + threadIdx.x] = -t.y;
+    }
   };
-  auto step = [&](long long t0, const T* qc, const T* dc, const float2* tc, T* qn, T* dn, float2* tn) {
+  auto step = [&](auto mask, int t0, const T* qc, const T* dc, const float* tc, T* qn, T* dn, float* tn) __attribute__((always_inline)) {
     vm_drain();
     __syncthreads();
     if (t0 + QT < rows) issue(t0 + QT, qn, dn, tn);
-    const bool mask = t0 < all || t0 + QT > rows;
+    f32x4 s[KW][2], g[KW][2];
+    CT pf[KW], sf[KW];
+    auto scores = [&](int qp) __attribute__((always_inline)) {
 #pragma unroll
-    for (int qp = 0; qp < QT / 32; ++qp) {
-      CT pf[KW], sf[KW];
-      f32x4 s[KW][2], g[KW][2];
-#pragma unroll
-      for (int qb = 0; qb < 2; ++qb)
+      for (int qb = 0; qb < 2; ++qb) {
+        const f32x4 nd = *reinterpret_cast<const f32x4*>(tc + QT + qp * 32 + qb * 16 + 4 * j);
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
           const CT qf = row_frag<HD>(qc, qp * 32 + qb * 16 + r, 4 * c + j);
@@ -560,14 +650,15 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
 #pragma unroll
           for (int w = 0; w < KW; ++w) {
             s[w][qb] = mma(qf, kf[w][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[w][qb]);
-            g[w][qb] = mma(df, vf[w][c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : g[w][qb]);
+            g[w][qb] = mma(df, vf[w][c], c == 0 ? nd : g[w][qb]);
           }
         }
-      float2 tt[2][4];
+      }
+    };
+    auto probs = [&](int qp) __attribute__((always_inline)) {
+      f32x4 l2[2];
 #pragma unroll
-      for (int qb = 0; qb < 2; ++qb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tt[qb][i] = tc[qp * 32 + qb * 16 + 4 * j + i];
+      for (int qb = 0; qb < 2; ++qb) l2[qb] = *reinterpret_cast<const f32x4*>(tc + qp * 32 + qb * 16 + 4 * j);
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         float p8[8], s8[8];
@@ -575,11 +666,11 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
         for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float pv = fast_exp2(__builtin_fmaf(s[w][qb][i], p.sl2, -tt[qb][i].x));
-            float x = pv * (g[w][qb][i] - tt[qb][i].y);
-            if (mask) {
-              const long long row = t0 + qp * 32 + qb * 16 + 4 * j + i;
-              const bool see = row >= first[w] && row < rows;
+            float pv = fast_exp2(__builtin_fmaf(s[w][qb][i], p.sl2, -l2[qb][i]));
+            float x = pv * g[w][qb][i];
+            if constexpr (decltype(mask)::value) {
+              const int row = t0 + qp * 32 + qb * 16 + 4 * j + i;
+              const bool see = row >= first[w];
               pv = see ? pv : 0.f;
               x = see ? x : 0.f;
             }
@@ -589,6 +680,8 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
         pf[w] = make_chunk<T>(p8);
         sf[w] = make_chunk<T>(s8);
       }
+    };
+    auto grads = [&](int qp) __attribute__((always_inline)) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const CT dt = col_frag<HD>(dc, 32 * qp, 16 * db, lane);
@@ -599,13 +692,24 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
           dk[w][db] = mma(qt, sf[w], dk[w][db]);
         }
       }
+    };
+#pragma unroll
+    for (int qp = 0; qp < QT / 32; ++qp) {
+      scores(qp);
+      probs(qp);
+      grads(qp);
     }
   };
   if (p_lo < rows) {
     issue(p_lo, qs0, ds0, tm0);
-    for (long long t0 = p_lo; t0 < rows; t0 += 2 * QT) {
-      step(t0, qs0, ds0, tm0, qs1, ds1, tm1);
-      if (t0 + QT < rows) step(t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
+    int t0 = p_lo;
+    for (; t0 < min(all, rows); t0 += 2 * QT) {
+      step(std::true_type{}, t0, qs0, ds0, tm0, qs1, ds1, tm1);
+      if (t0 + QT < rows) step(std::true_type{}, t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
+    }
+    for (; t0 < rows; t0 += 2 * QT) {
+      step(std::false_type{}, t0, qs0, ds0, tm0, qs1, ds1, tm1);
+      if (t0 + QT < rows) step(std::false_type{}, t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
     }
   }
 #pragma unroll
@@ -614,8 +718,9 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
     const long long row = ((sq.k0 + key[w]) * a.kv_heads + hk) * HD;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      store4((T*)p.dk + row + 16 * db + 4 * j, dk[w][db], a.scale);
-      store4((T*)p.dv + row + 16 * db + 4 * j, dv[w][db], 1.f);
+      const f32x4 none{0.f, 0.f, 0.f, 0.f};
+      store4((T*)p.dk + row + 16 * db + 4 * j, key[w] < sq.lk ? dk[w][db] : none, a.scale);
+      store4((T*)p.dv + row + 16 * db + 4 * j, key[w] < sq.lk ? dv[w][db] : none, 1.f);
     }
   }
 }
@@ -624,7 +729,10 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-unsigned tile_slots(long long total, int mult, int R, int S) { return (unsigned)(total * mult / R + S); }
+// A multiple of 8 (xcd_slot).
+unsigned tile_slots(long long total, int mult, int R, int S) { return (unsigned)((total * mult / R + S + 7) / 8 * 8); }
+
+Group group_of(const AttnArgs& a) { return Group{a.group(), (uint32_t)((1ull << 32) / a.group() + 1)}; }
 
 // Splits of the key axis: where the row tiles leave CUs idle, up to two workgroups per CU with
 // at least 256 keys of an average sequence each.
@@ -652,7 +760,7 @@ hipError_t attn_fwd(FwdP p, hipStream_t st) {
 
 template <typename T, int HD>
 hipError_t attn_bwd(BwdP p, hipStream_t st) {
-  constexpr int QB = HD == 128 ? 1 : 2, KW = 1;
+  constexpr int QB = HD == 128 ? 1 : 2, KW = HD == 128 || sizeof(T) == 4 ? 1 : 2;
   const AttnArgs& a = p.a;
   if (a.total_q > 0) {
     packed_dq_kernel<T, HD, QB>
@@ -688,7 +796,7 @@ size_t attention_fwd_ws_bytes(const AttnArgs& a) {
 hipError_t launch_attention_fwd(const AttnArgs& a, const void* q, const void* k, const void* v, const int* cu_q,
                                 const int* cu_k, const int* used_k, void* o, float* lse, void* ws, hipStream_t st) {
   if (a.total_q == 0) return hipSuccess;
-  FwdP p{a, q, k, v, cu_q, cu_k, used_k, o, lse, a.scale * kLog2e, fwd_splits(a, 16 * kFwdQB * kWaves), nullptr, nullptr};
+  FwdP p{a, q, k, v, SeqArgs{cu_q, cu_k, used_k, a.seqs, a.total_q, a.total_k}, group_of(a), o, lse, a.scale * kLog2e, fwd_splits(a, 16 * kFwdQB * kWaves), nullptr, nullptr};
   if (p.nsplit > 1) {
     p.part = (float*)ws;
     p.ml = (float2*)((char*)ws + align256((size_t)p.nsplit * a.total_q * a.heads * a.hd * sizeof(float)));
@@ -701,7 +809,7 @@ size_t attention_bwd_ws_bytes(const AttnArgs& a) { return align256(sizeof(float2
 hipError_t launch_attention_bwd(const AttnArgs& a, const void* q, const void* k, const void* v, const void* o,
                                 const float* lse, const void* d_o, const int* cu_q, const int* cu_k, const int* used_k,
                                 void* dq, void* dk, void* dv, void* ws, hipStream_t st) {
-  BwdP p{a, q, k, v, o, d_o, lse, cu_q, cu_k, used_k, dq, dk, dv, (float2*)ws, a.scale * kLog2e};
+  BwdP p{a, q, k, v, o, d_o, lse, SeqArgs{cu_q, cu_k, used_k, a.seqs, a.total_q, a.total_k}, group_of(a), dq, dk, dv, (float2*)ws, a.scale * kLog2e};
   return BSA_ATTN_DISPATCH(attn_bwd, a, p, st);
 }
 
