@@ -714,8 +714,10 @@ __global__ void __launch_bounds__(1024) db_sum_kernel(const float* __restrict__ 
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (c < n)
+  if (c < n) {
+#pragma unroll 8
     for (int i = w; i < P; i += 16) s += part[(long long)i * n + c];
+  }
   red[w][lane] = s;
   __syncthreads();
   if (w == 0 && c < n) {

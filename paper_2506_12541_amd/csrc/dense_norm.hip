@@ -76,9 +76,27 @@ __device__ __forceinline__ void norm_store(T* row, int idx, int cols, const floa
   else if (c < cols)
     store_partial(row + c, pack16<T>(v), cols - c);
 }
-__device__ __forceinline__ void norm_params(const float* p, int idx, int E, int cols, float fill, float* out) {
+// Gain or bias of vector idx's columns (fill: without p, and behind the row).
+template <int E>
+__device__ __forceinline__ void norm_params(const float* p, int idx, int cols, float fill, float* out) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) out[e] = p && idx * E + e < cols ? p[idx * E + e] : fill;
+  for (int e = 0; e < E; e += 4) {
+    const int c = idx * E + e;
+    float4 v = make_float4(fill, fill, fill, fill);
+    if (p) {
+      if (c + 4 <= cols) {
+        __builtin_memcpy(&v, p + c, 16);
+      } else {
+        if (c < cols) v.x = p[c];
+        if (c + 1 < cols) v.y = p[c + 1];
+        if (c + 2 < cols) v.z = p[c + 2];
+      }
+    }
+    out[e] = v.x;
+    out[e + 1] = v.y;
+    out[e + 2] = v.z;
+    out[e + 3] = v.w;
+  }
 }
 
 template <typename T, int L, int NV, int NT>
@@ -89,25 +107,37 @@ __global__ void __launch_bounds__(NT) layernorm_fwd_kernel(const T* __restrict__
   constexpr int E = NormVec<T>::E, GPW = NT / L;   // groups (rows at a time) per workgroup
   __shared__ float red[2 * NT / 64];
   const int l = threadIdx.x % L;
-  float g[NV][E], b[NV][E];
+  // gain and bias stay in registers over the rows while they are few (wide rows: read again)
+  constexpr bool KEEP = NV * E <= 16;
+  float g[KEEP ? NV : 1][E], b[KEEP ? NV : 1][E];
+  if constexpr (KEEP) {
 #pragma unroll
-  for (int t = 0; t < NV; ++t) {
-    norm_params(gain, l + L * t, E, a.cols, 1.f, g[t]);
-    norm_params(bias, l + L * t, E, a.cols, 0.f, b[t]);
+    for (int t = 0; t < NV; ++t) {
+      norm_params<E>(gain, l + L * t, a.cols, 1.f, g[t]);
+      norm_params<E>(bias, l + L * t, a.cols, 0.f, b[t]);
+    }
   }
-  // every group of a workgroup makes the same number of steps (they meet in group_sum)
-  for (long long r0 = (long long)blockIdx.x * GPW; r0 < a.rows; r0 += (long long)gridDim.x * GPW) {
+  // every group of a workgroup makes the same number of steps (they meet in group_sum); the next
+  // row is on its way while this one is reduced
+  const long long step = (long long)gridDim.x * GPW;
+  uint4 u[NV];
+  auto fetch = [&](long long row) {
+#pragma unroll
+    for (int t = 0; t < NV; ++t) u[t] = row < a.rows ? norm_load(x + row * a.ldx, l + L * t, a.cols) : make_uint4(0, 0, 0, 0);
+  };
+  fetch((long long)blockIdx.x * GPW + threadIdx.x / L);
+  for (long long r0 = (long long)blockIdx.x * GPW; r0 < a.rows; r0 += step) {
     const long long row = r0 + threadIdx.x / L;
     const bool on = row < a.rows;
     float v[NV][E];
     float s[1] = {0.f};
 #pragma unroll
     for (int t = 0; t < NV; ++t) {
-      const uint4 u = on ? norm_load(x + row * a.ldx, l + L * t, a.cols) : make_uint4(0, 0, 0, 0);
-      unpack16<T>(u, v[t]);
+      unpack16<T>(u[t], v[t]);
 #pragma unroll
       for (int e = 0; e < E; ++e) s[0] += v[t][e];
     }
+    if (r0 + step < a.rows) fetch(row + step);
     group_sum<L>(s, red);
     const float mu = s[0] / (float)a.cols;
     // the deviations' own mean is the rounding error of mu: it is taken out of them again, so
@@ -127,8 +157,13 @@ __global__ void __launch_bounds__(NT) layernorm_fwd_kernel(const T* __restrict__
     if (on) {
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
+        constexpr int K = KEEP ? 1 : 0;
+        if constexpr (!KEEP) {
+          norm_params<E>(gain, l + L * t, a.cols, 1.f, g[0]);
+          norm_params<E>(bias, l + L * t, a.cols, 0.f, b[0]);
+        }
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[t][e] = fmaf((v[t][e] - d) * rs, g[t][e], b[t][e]);
+        for (int e = 0; e < E; ++e) v[t][e] = fmaf((v[t][e] - d) * rs, g[K * t][e], b[K * t][e]);
         norm_store(y + row * a.ldy, l + L * t, a.cols, v[t]);
       }
       if (l == 0) {
@@ -155,7 +190,7 @@ __global__ void __launch_bounds__(NT) layernorm_bwd_kernel(const T* __restrict__
   float g[NV][E], ag[NV][E], ab[NV][E];
 #pragma unroll
   for (int t = 0; t < NV; ++t) {
-    norm_params(gain, l + L * t, E, a.cols, 0.f, g[t]);
+    norm_params<E>(gain, l + L * t, a.cols, 0.f, g[t]);
 #pragma unroll
     for (int e = 0; e < E; ++e) ag[t][e] = ab[t][e] = 0.f;
   }
@@ -249,8 +284,10 @@ __global__ void __launch_bounds__(1024) norm_colsum_kernel(const float* __restri
   float* const out = blockIdx.y ? dbias : dgain;
   const float* p = part + (long long)blockIdx.y * cols;
   float s = 0.f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 8
     for (int i = w; i < P; i += 16) s += p[(long long)i * 2 * cols + c];
+  }
   red[w][lane] = s;
   __syncthreads();
   if (w == 0 && c < cols && out) {
@@ -268,8 +305,10 @@ __global__ void __launch_bounds__(256) norm_zero_kernel(float* a, float* b, int 
   }
 }
 
-// Lanes per row and vectors per lane: the smallest group that holds the row.
-template <typename T, typename F>
+// Lanes per row and vectors per lane: the smallest group that holds the row. (The backward of bf16
+// rows of 4097 to 8192 columns takes 1024 lanes with one vector: with four a lane its sums leave
+// the registers.)
+template <typename T, bool BWD, typename F>
 hipError_t norm_dispatch(int cols, F f) {
   const int v = (cols + NormVec<T>::E - 1) / NormVec<T>::E;   // vectors of a row
   if (v <= 16) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
@@ -278,18 +317,24 @@ hipError_t norm_dispatch(int cols, F f) {
   if (v <= 128) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
   if (v <= 256) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   if (v <= 512) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
-  if (v <= 1024) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  if constexpr (BWD && sizeof(T) == 2) {
+    if (v <= 1024) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+  } else {
+    if (v <= 1024) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  }
   if (v <= 2048) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
   if (v <= 4096) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
   return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
 }
 
+// Workgroups of the backward: one for up to four steps of its groups (about 1 us each, where the
+// second launch that joins several workgroups' sums costs 5 us), else up to one per CU.
 template <typename T>
 int norm_bwd_groups(const NormArgs& a) {
   int wgs = 0;
-  (void)norm_dispatch<T>(a.cols, [&](auto L, auto) {
+  (void)norm_dispatch<T, true>(a.cols, [&](auto L, auto) {
     constexpr int GPW = 1024 / decltype(L)::value;
-    wgs = (int)std::min<long long>((a.rows + GPW - 1) / GPW, 256);
+    wgs = a.rows <= 4 * GPW ? 1 : (int)std::min<long long>((a.rows + GPW - 1) / GPW, 256);
     return hipSuccess;
   });
   return wgs;
@@ -298,7 +343,7 @@ int norm_bwd_groups(const NormArgs& a) {
 template <typename T>
 hipError_t norm_fwd(const NormArgs& a, const void* x, const float* gain, const float* bias, void* y, float* mean,
                     float* rstd, hipStream_t st) {
-  return norm_dispatch<T>(a.cols, [&](auto L, auto NV) {
+  return norm_dispatch<T, false>(a.cols, [&](auto L, auto NV) {
     constexpr int l = decltype(L)::value, nv = decltype(NV)::value, nt = l > 256 ? l : 256;
     const long long wgs = std::min<long long>((a.rows + nt / l - 1) / (nt / l), 256 * (2048 / nt));
     layernorm_fwd_kernel<T, l, nv, nt><<<(unsigned)wgs, nt, 0, st>>>((const T*)x, gain, bias, a, (T*)y, mean, rstd);
@@ -310,7 +355,7 @@ template <typename T>
 hipError_t norm_bwd(const NormArgs& a, const void* x, const float* gain, const float* mean, const float* rstd,
                     const void* dy, void* dx, float* dgain, float* dbias, float* part, hipStream_t st) {
   const int wgs = norm_bwd_groups<T>(a);
-  hipError_t e = norm_dispatch<T>(a.cols, [&](auto L, auto NV) {
+  hipError_t e = norm_dispatch<T, true>(a.cols, [&](auto L, auto NV) {
     constexpr int l = decltype(L)::value, nv = decltype(NV)::value;
     if (wgs == 1)
       layernorm_bwd_kernel<T, l, nv, 1024><<<1, 1024, 0, st>>>((const T*)x, gain, mean, rstd, (const T*)dy, a, (T*)dx,

@@ -23,6 +23,7 @@ __all__ = ["ACTIVATIONS", "layernorm_forward", "layernorm_backward", "linear_for
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 _CODES = {torch.bfloat16: BSA_BF16, torch.float32: BSA_F32}
+_HERE = contextlib.nullcontext()
 
 
 def _ptr(t):
@@ -76,13 +77,15 @@ def _on(dev, stream):
         if stream.device != dev:
             raise ValueError(f"stream must be on {dev}, got {stream.device}")
         return torch.cuda.stream(stream)
-    if dev.index != torch.cuda.current_device():
+    if dev.index != torch._C._cuda_getDevice():
         return torch.cuda.device(dev)
-    return contextlib.nullcontext()
+    return _HERE
 
 
 def _queue(dev):
-    return torch.cuda.current_stream(dev).cuda_stream
+    """The device's current stream as the C ABI takes it (torch.cuda.current_stream builds a Stream
+    object: 1.8 us of a call's 10)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def _workspace(nbytes, dev):
