@@ -131,24 +131,67 @@ __device__ __forceinline__ void xcd_slot(int& slot, int& hk) {
   }
 }
 
-template <typename T> struct AttnTile {
-  static constexpr int keys = sizeof(T) == 2 ? 64 : 32;   // keys (or query rows) of a staged tile
+// How a workgroup shares its work. Usually its waves own different rows (of queries, or of keys)
+// and walk tiles of the other side together. Where that leaves CUs idle or rows unused (single
+// tokens against a cache, short sequences: SPLIT), its waves own the same 16 rows and each walks
+// every NW-th tile of 32, staged for itself alone without a barrier; their results are joined in LDS.
+template <typename T, int HD, bool SPLIT> struct Share {
+  // two staged tiles of two tensors and every wave within 128 KB
+  static constexpr int NW = SPLIT && sizeof(T) * HD > 256 ? 2 : kWaves;
+  static constexpr int tile = SPLIT || sizeof(T) == 4 ? 32 : 64;   // rows of a staged tile
+  static constexpr int LW = SPLIT ? 1 : NW;                        // waves that load a tile
+  static constexpr int elems = (SPLIT ? NW : 1) * tile * HD;       // of one staged tensor
+  static constexpr int step = SPLIT ? NW * tile : tile;            // rows from a wave's tile to its next
 };
+
+// The next tile may be read: every wave's part of it has landed.
+template <bool SPLIT>
+__device__ __forceinline__ void tile_ready() {
+  vm_drain();
+  if constexpr (SPLIT)
+    wave_sync();
+  else
+    __syncthreads();
+}
+
+// 16 x HD float32 results of one wave in transposed accumulators (lane: row lane % 16, columns 16 db +
+// 4 (lane / 16) + i), row-major in LDS; columns are swizzled by row against bank conflicts.
+template <int HD>
+__device__ __forceinline__ f32x4* join_at(float* m, int row, int c4) {
+  return reinterpret_cast<f32x4*>(m + row * HD + 4 * (c4 ^ (row & (HD / 4 - 1))));
+}
+
+// The sum of the NW waves' results (at m, NW x 16 x HD floats), in order, four columns at a time.
+template <int HD, int NW, typename F>
+__device__ __forceinline__ void join_sum(float* m, const f32x4 (&acc)[HD / 16], F store) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  __syncthreads();   // every wave has read its last tile
+#pragma unroll
+  for (int db = 0; db < HD / 16; ++db) *join_at<HD>(m + wid * 16 * HD, lane & 15, 4 * db + (lane >> 4)) = acc[db];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * (HD / 4); i += 64 * NW) {
+    const int row = i / (HD / 4), c4 = i % (HD / 4);
+    f32x4 v = *join_at<HD>(m, row, c4);
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v += *join_at<HD>(m + w * 16 * HD, row, c4);
+    store(row, 4 * c4, v);
+  }
+}
 
 // ---- LDS tiles of ROWS x HD elements, filled by direct loads, 16-byte pieces swizzled ----
 
 template <typename T, int HD> __device__ __forceinline__ int tswz(int row) { return swz<HD * (int)sizeof(T) / 2>(row); }
 
-// Rows r0 + [0, ROWS) of a matrix with row stride ld; rows at or past nrows repeat the last one
-// (masked by the caller; nrows > 0).
-template <typename T, int HD, int ROWS>
+// Rows r0 + [0, ROWS) of a matrix with row stride ld, by NW waves; rows at or past nrows repeat the
+// last one (masked by the caller; nrows > 0).
+template <typename T, int HD, int ROWS, int NW>
 struct TileLoad {
   static constexpr int E = 16 / (int)sizeof(T), CPR = HD / E, NI = ROWS * CPR / 64;
-  static_assert(NI % kWaves == 0, "tile / wave split");
+  static_assert(NI % NW == 0, "tile / wave split");
   __device__ __forceinline__ static void issue(T* lds, const T* g, long long ld, int r0, int nrows, int wid, int lane) {
 #pragma unroll
-    for (int u = 0; u < NI / kWaves; ++u) {
-      const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
+    for (int u = 0; u < NI / NW; ++u) {
+      const int blk = wid * (NI / NW) + u, idx = blk * 64 + lane;
       const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
       const int r = min(r0 + row, nrows - 1);
       load_lds16(g + r * ld + E * c, lds + blk * 64 * E);
@@ -206,15 +249,15 @@ __device__ __forceinline__ RowAt packed_row(const Seq& sq, int hk, const Group& 
 }
 
 // The same for packed rows r0 + [0, ROWS) (rows of them, > 0).
-template <typename T, int HD, int ROWS>
+template <typename T, int HD, int ROWS, int NW>
 struct PackedLoad {
   static constexpr int E = 16 / (int)sizeof(T), CPR = HD / E, NI = ROWS * CPR / 64;
-  static_assert(NI % kWaves == 0, "tile / wave split");
+  static_assert(NI % NW == 0, "tile / wave split");
   __device__ __forceinline__ static void issue(T* lds, const T* g, long long row_ld, long long head_ld, const Seq& sq,
                                                int hk, const Group& G, int r0, int rows, int wid, int lane) {
 #pragma unroll
-    for (int u = 0; u < NI / kWaves; ++u) {
-      const int blk = wid * (NI / kWaves) + u, idx = blk * 64 + lane;
+    for (int u = 0; u < NI / NW; ++u) {
+      const int blk = wid * (NI / NW) + u, idx = blk * 64 + lane;
       const int row = idx / CPR, c = (idx % CPR) ^ tswz<T, HD>(row);
       const RowAt at = packed_row(sq, hk, G, min(r0 + row, rows - 1));
       load_lds16(g + at.t * row_ld + at.h * head_ld + E * c, lds + blk * 64 * E);
@@ -244,11 +287,13 @@ __device__ __forceinline__ void split_range(int lk, int nsplit, int z, int KT, i
   hi = min(lo + per * KT, lk);
 }
 
-template <typename T, int HD, int QB>
-__global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
-  constexpr int KT = AttnTile<T>::keys, KB = KT / 16, NCH = HD / 32, DB = HD / 16, R = 16 * QB * kWaves;
+template <typename T, int HD, int QB, bool SPLIT>
+__global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_fwd_kernel(FwdP p) {
+  typedef Share<T, HD, SPLIT> SH;
+  static_assert(!SPLIT || QB == 1, "one block of rows");
+  constexpr int KT = SH::tile, KB = KT / 16, NCH = HD / 32, DB = HD / 16, R = 16 * QB * (SPLIT ? 1 : SH::NW), ST = SH::step;
   typedef typename Chunk<T>::type CT;
-  __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
+  __shared__ __attribute__((aligned(1024))) T ks0a[SH::elems], vs0a[SH::elems], ks1a[SH::elems], vs1a[SH::elems];
   const AttnArgs& a = p.a;
   const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -273,7 +318,7 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
   const int off = sq.lk - sq.lq;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    pr[qb] = p0 + (wid * QB + qb) * 16 + r;
+    pr[qb] = p0 + ((SPLIT ? 0 : wid * QB) + qb) * 16 + r;
     const bool on = pr[qb] < rows;
     const RowAt at = packed_row(sq, hk, G, on ? pr[qb] : 0);
     lim[qb] = !on ? -1 : a.causal ? min((int)(at.t - sq.q0) + off, sq.lk - 1) : sq.lk - 1;
@@ -298,14 +343,15 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
 
   const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
   const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
-  auto issue = [&](int t0, T* kd, T* vd) {
-    TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
-    TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
+  const int lw = SPLIT ? 0 : wid, own = SPLIT ? wid * KT * HD : 0;
+  T *const ks0 = ks0a + own, *const vs0 = vs0a + own, *const ks1 = ks1a + own, *const vs1 = vs1a + own;
+  auto issue = [&](int t0, T* kd, T* vd) __attribute__((always_inline)) {
+    TileLoad<T, HD, KT, SH::LW>::issue(kd, kh, a.k_row, t0, sq.lk, lw, lane);
+    TileLoad<T, HD, KT, SH::LW>::issue(vd, vh, a.v_row, t0, sq.lk, lw, lane);
   };
   auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
-    vm_drain();
-    __syncthreads();
-    if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
+    tile_ready<SPLIT>();
+    if (t0 + ST < k_hi) issue(t0 + ST, kn, vn);
     f32x4 s[QB][KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -365,38 +411,66 @@ __global__ void __launch_bounds__(64 * kWaves) packed_fwd_kernel(FwdP p) {
         for (int qb = 0; qb < QB; ++qb) o[qb][db] = mma(vf, pf[qb][kp], o[qb][db]);
       }
   };
-  if (k_lo < k_hi) {
-    issue(k_lo, ks0, vs0);
-    int t0 = k_lo;
-    for (; t0 + 2 * KT <= all; t0 += 2 * KT) {
+  const int k_first = k_lo + (SPLIT ? wid * KT : 0);
+  if (k_first < k_hi) {
+    issue(k_first, ks0, vs0);
+    int t0 = k_first;
+    for (; t0 + ST + KT <= all; t0 += 2 * ST) {
       step(std::false_type{}, t0, ks0, vs0, ks1, vs1);
-      step(std::false_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+      step(std::false_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
-    for (; t0 < k_hi; t0 += 2 * KT) {
+    for (; t0 < k_hi; t0 += 2 * ST) {
       step(std::true_type{}, t0, ks0, vs0, ks1, vs1);
-      if (t0 + KT < k_hi) step(std::true_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+      if (t0 + ST < k_hi) step(std::true_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
   }
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    if (pr[qb] >= ext) continue;
-    const RowAt at = packed_row(sq, hk, G, pr[qb]);
+  // four columns of a finished row (first: the thread that also writes the row's statistics)
+  auto store = [&](int row, int c, f32x4 v, float m, float l, bool first) {
+    if (row >= ext) return;
+    const RowAt at = packed_row(sq, hk, G, row);
     if (p.nsplit > 1) {
-      const float l = col_sum(ls[qb]);
-      if (pr[qb] >= rows) continue;
-      const long long row = ((long long)blockIdx.z * a.total_q + at.t) * a.heads + at.h;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) store4(p.part + row * HD + 16 * db + 4 * j, o[qb][db], 1.f);
-      if (j == 0) p.ml[row] = make_float2(mx[qb], l);
+      if (row >= rows) return;
+      const long long pos = ((long long)blockIdx.z * a.total_q + at.t) * a.heads + at.h;
+      if (k_lo < k_hi) store4(p.part + pos * HD + c, v, 1.f);   // else l = 0: not read
+      if (first) p.ml[pos] = make_float2(m, l);
     } else {
-      const float l = col_sum(ls[qb]);
-      if (pr[qb] >= rows && !a.zero_rest) continue;
-      const bool any = pr[qb] < rows && !(l == 0.f);   // a sum of NaN stays one
-      const float inv = any ? 1.0f / l : 0.f;
+      if (row >= rows && !a.zero_rest) return;
+      const bool any = row < rows && !(l == 0.f);   // a sum of NaN stays one
+      store4(out + at.t * a.o_row + at.h * a.o_head + c, any ? v : f32x4{0.f, 0.f, 0.f, 0.f}, any ? 1.0f / l : 0.f);
+      if (first) p.lse[at.h * a.total_q + at.t] = any ? (m + log2f(l)) * kLn2 : kNegInf;
+    }
+  };
+  if constexpr (!SPLIT) {
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        store4(out + at.t * a.o_row + at.h * a.o_head + 16 * db + 4 * j, any ? o[qb][db] : f32x4{0.f, 0.f, 0.f, 0.f}, inv);
-      if (j == 0) p.lse[at.h * a.total_q + at.t] = any ? (mx[qb] + log2f(l)) * kLn2 : kNegInf;
+    for (int qb = 0; qb < QB; ++qb) {
+      const float l = col_sum(ls[qb]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store(pr[qb], 16 * db + 4 * j, o[qb][db], mx[qb], l, db == 0 && j == 0);
+    }
+  } else {
+    __shared__ float2 mls[SH::NW][16];
+    const float l = col_sum(ls[0]);
+    __syncthreads();   // every wave has read its last tile
+    static_assert(SH::NW * 16 * HD * 4 <= SH::elems * sizeof(T), "the waves' results in a staged tensor's place");
+    float* const mine = reinterpret_cast<float*>(ks0a) + wid * 16 * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *join_at<HD>(mine, r, 4 * db + j) = o[0][db];
+    if (j == 0) mls[wid][r] = make_float2(mx[0], l);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (HD / 4); i += 64 * SH::NW) {
+      const int row = i / (HD / 4), c4 = i % (HD / 4);
+      float m = kNegInf, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < SH::NW; ++w) m = fmaxf(m, mls[w][row].x);
+      const float mref = m == kNegInf ? 0.f : m;
+      f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < SH::NW; ++w) {
+        const float f = fast_exp2(mls[w][row].x - mref);
+        sum += f * mls[w][row].y;
+        v += f * *join_at<HD>(reinterpret_cast<float*>(ks0a) + w * 16 * HD, row, c4);
+      }
+      store(p0 + row, 4 * c4, v, m, sum, c4 == 0);
     }
   }
 }
@@ -422,6 +496,7 @@ __global__ void __launch_bounds__(256) packed_join_kernel(FwdP p) {
     const float mref = m == kNegInf ? 0.f : m;
     for (int z = 0; z < p.nsplit; ++z) {
       const float2 ml = p.ml[z * per + row];
+      if (ml.y == 0.f) continue;    // saw nothing: its part is not written
       const float w = fast_exp2(ml.x - mref);
       l += w * ml.y;
       acc += w * *reinterpret_cast<const f32x4*>(p.part + (z * per + row) * HD + c);
@@ -446,11 +521,13 @@ struct BwdP {
 };
 
 // dq, and each row's terms for the key-major pass.
-template <typename T, int HD, int QB>
-__global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
-  constexpr int KT = AttnTile<T>::keys, NCH = HD / 32, DB = HD / 16, R = 16 * QB * kWaves;
+template <typename T, int HD, int QB, bool SPLIT>
+__global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kernel(BwdP p) {
+  typedef Share<T, HD, SPLIT> SH;
+  static_assert(!SPLIT || QB == 1, "one block of rows");
+  constexpr int KT = SH::tile, NCH = HD / 32, DB = HD / 16, R = 16 * QB * (SPLIT ? 1 : SH::NW), ST = SH::step;
   typedef typename Chunk<T>::type CT;
-  __shared__ __attribute__((aligned(1024))) T ks0[KT * HD], vs0[KT * HD], ks1[KT * HD], vs1[KT * HD];
+  __shared__ __attribute__((aligned(1024))) T ks0a[SH::elems], vs0a[SH::elems], ks1a[SH::elems], vs1a[SH::elems];
   const AttnArgs& a = p.a;
   const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -473,7 +550,7 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
   const int off = sq.lk - sq.lq;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    pr[qb] = p0 + (wid * QB + qb) * 16 + r;
+    pr[qb] = p0 + ((SPLIT ? 0 : wid * QB) + qb) * 16 + r;
     const bool on = pr[qb] < rows;
     const RowAt at = packed_row(sq, hk, G, on ? pr[qb] : 0);
     lim[qb] = !on ? -1 : a.causal ? min((int)(at.t - sq.q0) + off, sq.lk - 1) : sq.lk - 1;
@@ -495,7 +572,8 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
     }
     dd[qb] = col_sum(d);
     l2[qb] = on && lim[qb] >= 0 ? p.lse[at.h * a.total_q + at.t] * kLog2e : __builtin_huge_valf();
-    if (on && j == 0) p.terms[((long long)hk * a.total_q + sq.q0) * G.G + pr[qb]] = make_float2(l2[qb], dd[qb]);
+    if (on && j == 0 && (!SPLIT || wid == 0))
+      p.terms[((long long)hk * a.total_q + sq.q0) * G.G + pr[qb]] = make_float2(l2[qb], dd[qb]);
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -505,14 +583,15 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
 
   const T* const kh = (const T*)p.k + sq.k0 * a.k_row + hk * a.k_head;
   const T* const vh = (const T*)p.v + sq.k0 * a.v_row + hk * a.v_head;
-  auto issue = [&](int t0, T* kd, T* vd) {
-    TileLoad<T, HD, KT>::issue(kd, kh, a.k_row, t0, sq.lk, wid, lane);
-    TileLoad<T, HD, KT>::issue(vd, vh, a.v_row, t0, sq.lk, wid, lane);
+  const int lw = SPLIT ? 0 : wid, own = SPLIT ? wid * KT * HD : 0;
+  T *const ks0 = ks0a + own, *const vs0 = vs0a + own, *const ks1 = ks1a + own, *const vs1 = vs1a + own;
+  auto issue = [&](int t0, T* kd, T* vd) __attribute__((always_inline)) {
+    TileLoad<T, HD, KT, SH::LW>::issue(kd, kh, a.k_row, t0, sq.lk, lw, lane);
+    TileLoad<T, HD, KT, SH::LW>::issue(vd, vh, a.v_row, t0, sq.lk, lw, lane);
   };
   auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
-    vm_drain();
-    __syncthreads();
-    if (t0 + KT < k_hi) issue(t0 + KT, kn, vn);
+    tile_ready<SPLIT>();
+    if (t0 + ST < k_hi) issue(t0 + ST, kn, vn);
 #pragma unroll
     for (int kp = 0; kp < KT / 32; ++kp) {
       f32x4 s[QB][2], g[QB][2];
@@ -551,36 +630,45 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dq_kernel(BwdP p) {
       }
     }
   };
-  if (k_hi > 0) {
-    issue(0, ks0, vs0);
-    int t0 = 0;
-    for (; t0 + 2 * KT <= all; t0 += 2 * KT) {
+  const int k_first = SPLIT ? wid * KT : 0;
+  if (k_first < k_hi) {
+    issue(k_first, ks0, vs0);
+    int t0 = k_first;
+    for (; t0 + ST + KT <= all; t0 += 2 * ST) {
       step(std::false_type{}, t0, ks0, vs0, ks1, vs1);
-      step(std::false_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+      step(std::false_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
-    for (; t0 < k_hi; t0 += 2 * KT) {
+    for (; t0 < k_hi; t0 += 2 * ST) {
       step(std::true_type{}, t0, ks0, vs0, ks1, vs1);
-      if (t0 + KT < k_hi) step(std::true_type{}, t0 + KT, ks1, vs1, ks0, vs0);
+      if (t0 + ST < k_hi) step(std::true_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
   }
+  auto store = [&](int row, int c, f32x4 v) {
+    if (row >= ext || (row >= rows && !a.zero_rest)) return;
+    const RowAt at = packed_row(sq, hk, G, row);
+    store4((T*)p.dq + (at.t * a.heads + at.h) * HD + c, v, a.scale);
+  };
+  if constexpr (!SPLIT) {
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    if (pr[qb] >= ext || (pr[qb] >= rows && !a.zero_rest)) continue;
-    const RowAt at = packed_row(sq, hk, G, pr[qb]);
-    T* const out = (T*)p.dq + (at.t * a.heads + at.h) * HD;
+    for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) store4(out + 16 * db + 4 * j, acc[qb][db], a.scale);
+      for (int db = 0; db < DB; ++db) store(pr[qb], 16 * db + 4 * j, acc[qb][db]);
+  } else {
+    join_sum<HD, SH::NW>(reinterpret_cast<float*>(ks0a), acc[0], [&](int row, int c, f32x4 v) { store(p0 + row, c, v); });
   }
 }
 
 // dk and dv of 16 KW keys per wave (a lane owns a key column, S = Q K^T), over the packed query
 // rows that see them, in tiles of KT rows.
-template <typename T, int HD, int KW>
-__global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
-  constexpr int QT = AttnTile<T>::keys, NCH = HD / 32, DB = HD / 16, R = 16 * KW * kWaves;
+template <typename T, int HD, int KW, bool SPLIT>
+__global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dkv_kernel(BwdP p) {
+  typedef Share<T, HD, SPLIT> SH;
+  static_assert(!SPLIT || KW == 1, "one block of keys");
+  constexpr int QT = SH::tile, NCH = HD / 32, DB = HD / 16, R = 16 * KW * (SPLIT ? 1 : SH::NW), ST = SH::step;
+  constexpr int TM = (SPLIT ? SH::NW : 1) * 2 * QT;
   typedef typename Chunk<T>::type CT;
-  __shared__ __attribute__((aligned(1024))) T qs0[QT * HD], ds0[QT * HD], qs1[QT * HD], ds1[QT * HD];
-  __shared__ __attribute__((aligned(16))) float tm0[2 * QT], tm1[2 * QT];   // lse, then -D, of the tile's rows
+  __shared__ __attribute__((aligned(1024))) T qs0a[SH::elems], ds0a[SH::elems], qs1a[SH::elems], ds1a[SH::elems];
+  __shared__ __attribute__((aligned(16))) float tm0a[TM], tm1a[TM];   // lse, then -D, of a tile's rows
   const AttnArgs& a = p.a;
   const Group G = p.G;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -599,7 +687,7 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
   f32x4 dk[KW][DB], dv[KW][DB];
 #pragma unroll
   for (int w = 0; w < KW; ++w) {
-    key[w] = (int)k0 + (wid * KW + w) * 16 + r;
+    key[w] = (int)k0 + ((SPLIT ? 0 : wid * KW) + w) * 16 + r;
     const bool on = key[w] < sq.lk;
     first[w] = !on ? rows : a.causal ? max(key[w] - off, 0) * G.G : 0;
     const long long row = sq.k0 + (on ? key[w] : 0);
@@ -622,21 +710,23 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
   const int all = a.causal ? max((int)min(k0 + R, (long long)sq.lk) - 1 - off, 0) * G.G : 0;
   const int p_lo = k0 >= sq.lk ? rows : a.causal ? max((int)k0 - off, 0) * G.G / QT * QT : 0;
 
+  const int lw = SPLIT ? 0 : wid, own = SPLIT ? wid * QT * HD : 0, tid = SPLIT ? lane : threadIdx.x;
+  T *const qs0 = qs0a + own, *const ds0 = ds0a + own, *const qs1 = qs1a + own, *const ds1 = ds1a + own;
+  float *const tm0 = tm0a + (SPLIT ? wid * 2 * QT : 0), *const tm1 = tm1a + (SPLIT ? wid * 2 * QT : 0);
   // tile rows are packed rows: query and head vary by row
-  auto issue = [&](int t0, T* qd, T* dd, float* td) {
-    PackedLoad<T, HD, QT>::issue(qd, (const T*)p.q, a.q_row, a.q_head, sq, hk, G, t0, rows, wid, lane);
-    PackedLoad<T, HD, QT>::issue(dd, (const T*)p.d_o, a.do_row, a.do_head, sq, hk, G, t0, rows, wid, lane);
-    if (threadIdx.x < QT) {
-      const float2 t = t0 + threadIdx.x < rows ? p.terms[((long long)hk * a.total_q + sq.q0) * G.G + t0 + threadIdx.x]
-                                               : make_float2(__builtin_huge_valf(), 0.f);
-      td[threadIdx.x] = t.x;
-      td[QT + threadIdx.x] = -t.y;
+  auto issue = [&](int t0, T* qd, T* dd, float* td) __attribute__((always_inline)) {
+    PackedLoad<T, HD, QT, SH::LW>::issue(qd, (const T*)p.q, a.q_row, a.q_head, sq, hk, G, t0, rows, lw, lane);
+    PackedLoad<T, HD, QT, SH::LW>::issue(dd, (const T*)p.d_o, a.do_row, a.do_head, sq, hk, G, t0, rows, lw, lane);
+    if (tid < QT) {
+      const float2 t = t0 + tid < rows ? p.terms[((long long)hk * a.total_q + sq.q0) * G.G + t0 + tid]
+                                       : make_float2(__builtin_huge_valf(), 0.f);
+      td[tid] = t.x;
+      td[QT + tid] = -t.y;
     }
   };
   auto step = [&](auto mask, int t0, const T* qc, const T* dc, const float* tc, T* qn, T* dn, float* tn) __attribute__((always_inline)) {
-    vm_drain();
-    __syncthreads();
-    if (t0 + QT < rows) issue(t0 + QT, qn, dn, tn);
+    tile_ready<SPLIT>();
+    if (t0 + ST < rows) issue(t0 + ST, qn, dn, tn);
     f32x4 s[KW][2], g[KW][2];
     CT pf[KW], sf[KW];
     auto scores = [&](int qp) __attribute__((always_inline)) {
@@ -700,28 +790,36 @@ __global__ void __launch_bounds__(64 * kWaves) packed_dkv_kernel(BwdP p) {
       grads(qp);
     }
   };
-  if (p_lo < rows) {
-    issue(p_lo, qs0, ds0, tm0);
-    int t0 = p_lo;
-    for (; t0 < min(all, rows); t0 += 2 * QT) {
+  const int p_first = p_lo + (SPLIT ? wid * QT : 0);
+  if (p_first < rows) {
+    issue(p_first, qs0, ds0, tm0);
+    int t0 = p_first;
+    for (; t0 < min(all, rows); t0 += 2 * ST) {
       step(std::true_type{}, t0, qs0, ds0, tm0, qs1, ds1, tm1);
-      if (t0 + QT < rows) step(std::true_type{}, t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
+      if (t0 + ST < rows) step(std::true_type{}, t0 + ST, qs1, ds1, tm1, qs0, ds0, tm0);
     }
-    for (; t0 < rows; t0 += 2 * QT) {
+    for (; t0 < rows; t0 += 2 * ST) {
       step(std::false_type{}, t0, qs0, ds0, tm0, qs1, ds1, tm1);
-      if (t0 + QT < rows) step(std::false_type{}, t0 + QT, qs1, ds1, tm1, qs0, ds0, tm0);
+      if (t0 + ST < rows) step(std::false_type{}, t0 + ST, qs1, ds1, tm1, qs0, ds0, tm0);
     }
   }
+  auto store = [&](T* out, int k, int c, f32x4 v, float sc) {
+    if (k >= sq.ek || (k >= sq.lk && !a.zero_rest)) return;
+    store4(out + ((sq.k0 + k) * a.kv_heads + hk) * HD + c, k < sq.lk ? v : f32x4{0.f, 0.f, 0.f, 0.f}, sc);
+  };
+  if constexpr (!SPLIT) {
 #pragma unroll
-  for (int w = 0; w < KW; ++w) {
-    if (key[w] >= sq.ek || (key[w] >= sq.lk && !a.zero_rest)) continue;
-    const long long row = ((sq.k0 + key[w]) * a.kv_heads + hk) * HD;
+    for (int w = 0; w < KW; ++w)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      const f32x4 none{0.f, 0.f, 0.f, 0.f};
-      store4((T*)p.dk + row + 16 * db + 4 * j, key[w] < sq.lk ? dk[w][db] : none, a.scale);
-      store4((T*)p.dv + row + 16 * db + 4 * j, key[w] < sq.lk ? dv[w][db] : none, 1.f);
-    }
+      for (int db = 0; db < DB; ++db) {
+        store((T*)p.dk, key[w], 16 * db + 4 * j, dk[w][db], a.scale);
+        store((T*)p.dv, key[w], 16 * db + 4 * j, dv[w][db], 1.f);
+      }
+  } else {
+    join_sum<HD, SH::NW>(reinterpret_cast<float*>(qs0a), dk[0],
+                         [&](int row, int c, f32x4 v) { store((T*)p.dk, (int)k0 + row, c, v, a.scale); });
+    join_sum<HD, SH::NW>(reinterpret_cast<float*>(ds0a), dv[0],
+                         [&](int row, int c, f32x4 v) { store((T*)p.dv, (int)k0 + row, c, v, 1.f); });
   }
 }
 
@@ -734,23 +832,35 @@ unsigned tile_slots(long long total, int mult, int R, int S) { return (unsigned)
 
 Group group_of(const AttnArgs& a) { return Group{a.group(), (uint32_t)((1ull << 32) / a.group() + 1)}; }
 
-// Splits of the key axis: where the row tiles leave CUs idle, up to two workgroups per CU with
-// at least 256 keys of an average sequence each.
-int fwd_splits(const AttnArgs& a, int R) {
-  const long long tiles = (a.total_q * a.group() / R + a.seqs) * a.kv_heads;
-  const long long avg = a.total_k / std::max(a.seqs, 1);
-  long long s = std::min<long long>(std::max<long long>(512 / std::max<long long>(tiles, 1), 1), avg / 256);
-  return (int)std::max<long long>(std::min<long long>(s, 64), 1);
+// How the forward runs: SPLIT (Share) where a sequence has 32 packed rows or fewer on average, or
+// the 128-row tiles would leave half of the CUs idle; and the splits of the key axis, while
+// the workgroups are few (split kernels: 2048, whose lengths vary; else two per CU), at least 256
+// keys of an average sequence each. The lengths are on the device: a cache counts with its
+// capacity.
+struct FwdPlan {
+  bool split;
+  int nsplit;
+};
+constexpr int kFwdQB = 2;
+FwdPlan fwd_plan(const AttnArgs& a) {
+  const long long rows = a.total_q * a.group();
+  const long long avg_k = a.total_k / a.seqs;
+  auto wgs = [&](int R) { return std::max<long long>((rows + R - 1) / R, a.seqs) * a.kv_heads; };
+  FwdPlan f;
+  f.split = rows <= 32LL * a.seqs || wgs(16 * kFwdQB * kWaves) < 128;
+  const long long n = f.split ? 2048 / wgs(16) : 512 / wgs(16 * kFwdQB * kWaves);
+  f.nsplit = (int)std::max<long long>(std::min<long long>(std::min<long long>(n, avg_k / 256), 64), 1);
+  return f;
 }
 
-constexpr int kFwdQB = 2;
-
 template <typename T, int HD>
-hipError_t attn_fwd(FwdP p, hipStream_t st) {
-  constexpr int R = 16 * kFwdQB * kWaves;
+hipError_t attn_fwd(FwdP p, bool split, hipStream_t st) {
   const AttnArgs& a = p.a;
-  const dim3 grid(tile_slots(a.total_q, a.group(), R, a.seqs), a.kv_heads, p.nsplit);
-  packed_fwd_kernel<T, HD, kFwdQB><<<grid, 64 * kWaves, 0, st>>>(p);
+  auto grid = [&](int R) { return dim3(tile_slots(a.total_q, a.group(), R, a.seqs), a.kv_heads, p.nsplit); };
+  if (split)
+    packed_fwd_kernel<T, HD, 1, true><<<grid(16), 64 * Share<T, HD, true>::NW, 0, st>>>(p);
+  else
+    packed_fwd_kernel<T, HD, kFwdQB, false><<<grid(16 * kFwdQB * kWaves), 64 * kWaves, 0, st>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const long long n = a.total_q * a.heads, per = 256 / (HD / 4);
@@ -758,19 +868,28 @@ hipError_t attn_fwd(FwdP p, hipStream_t st) {
   return hipGetLastError();
 }
 
+// The backward's passes SPLIT where their usual tiles would not give three workgroups to every
+// four CUs.
 template <typename T, int HD>
 hipError_t attn_bwd(BwdP p, hipStream_t st) {
   constexpr int QB = HD == 128 ? 1 : 2, KW = HD == 128 || sizeof(T) == 4 ? 1 : 2;
+  constexpr int RQ = 16 * QB * kWaves, RK = 16 * KW * kWaves;
   const AttnArgs& a = p.a;
   if (a.total_q > 0) {
-    packed_dq_kernel<T, HD, QB>
-        <<<dim3(tile_slots(a.total_q, a.group(), 16 * QB * kWaves, a.seqs), a.kv_heads), 64 * kWaves, 0, st>>>(p);
+    auto grid = [&](int R) { return dim3(tile_slots(a.total_q, a.group(), R, a.seqs), a.kv_heads); };
+    if ((a.total_q * a.group() + RQ - 1) / RQ * a.kv_heads < 192)
+      packed_dq_kernel<T, HD, 1, true><<<grid(16), 64 * Share<T, HD, true>::NW, 0, st>>>(p);
+    else
+      packed_dq_kernel<T, HD, QB, false><<<grid(RQ), 64 * kWaves, 0, st>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.total_k > 0) {
-    packed_dkv_kernel<T, HD, KW>
-        <<<dim3(tile_slots(a.total_k, 1, 16 * KW * kWaves, a.seqs), a.kv_heads), 64 * kWaves, 0, st>>>(p);
+    auto grid = [&](int R) { return dim3(tile_slots(a.total_k, 1, R, a.seqs), a.kv_heads); };
+    if ((a.total_k + RK - 1) / RK * a.kv_heads < 192)
+      packed_dkv_kernel<T, HD, 1, true><<<grid(16), 64 * Share<T, HD, true>::NW, 0, st>>>(p);
+    else
+      packed_dkv_kernel<T, HD, KW, false><<<grid(RK), 64 * kWaves, 0, st>>>(p);
     return hipGetLastError();
   }
   return hipSuccess;
@@ -787,7 +906,7 @@ hipError_t attn_bwd(BwdP p, hipStream_t st) {
 }  // namespace
 
 size_t attention_fwd_ws_bytes(const AttnArgs& a) {
-  const int s = fwd_splits(a, 16 * kFwdQB * kWaves);
+  const int s = fwd_plan(a).nsplit;
   if (s == 1) return 0;
   const size_t rows = (size_t)s * a.total_q * a.heads;
   return align256(rows * a.hd * sizeof(float)) + align256(rows * sizeof(float2));
@@ -796,12 +915,14 @@ size_t attention_fwd_ws_bytes(const AttnArgs& a) {
 hipError_t launch_attention_fwd(const AttnArgs& a, const void* q, const void* k, const void* v, const int* cu_q,
                                 const int* cu_k, const int* used_k, void* o, float* lse, void* ws, hipStream_t st) {
   if (a.total_q == 0) return hipSuccess;
-  FwdP p{a, q, k, v, SeqArgs{cu_q, cu_k, used_k, a.seqs, a.total_q, a.total_k}, group_of(a), o, lse, a.scale * kLog2e, fwd_splits(a, 16 * kFwdQB * kWaves), nullptr, nullptr};
+  const FwdPlan f = fwd_plan(a);
+  FwdP p{a, q, k, v, SeqArgs{cu_q, cu_k, used_k, a.seqs, a.total_q, a.total_k}, group_of(a), o, lse, a.scale * kLog2e,
+         f.nsplit, nullptr, nullptr};
   if (p.nsplit > 1) {
     p.part = (float*)ws;
     p.ml = (float2*)((char*)ws + align256((size_t)p.nsplit * a.total_q * a.heads * a.hd * sizeof(float)));
   }
-  return BSA_ATTN_DISPATCH(attn_fwd, a, p, st);
+  return BSA_ATTN_DISPATCH(attn_fwd, a, p, f.split, st);
 }
 
 size_t attention_bwd_ws_bytes(const AttnArgs& a) { return align256(sizeof(float2) * (size_t)a.total_q * a.heads); }
