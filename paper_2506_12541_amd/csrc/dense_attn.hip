@@ -492,14 +492,17 @@ __global__ void __launch_bounds__(256) packed_join_kernel(FwdP p) {
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
   if (in) {
     const long long per = a.total_q * a.heads;
+#pragma unroll 8
     for (int z = 0; z < p.nsplit; ++z) m = fmaxf(m, p.ml[z * per + row].x);
     const float mref = m == kNegInf ? 0.f : m;
+#pragma unroll 8
     for (int z = 0; z < p.nsplit; ++z) {
       const float2 ml = p.ml[z * per + row];
-      if (ml.y == 0.f) continue;    // saw nothing: its part is not written
+      const f32x4 part = *reinterpret_cast<const f32x4*>(p.part + (z * per + row) * HD + c);
       const float w = fast_exp2(ml.x - mref);
       l += w * ml.y;
-      acc += w * *reinterpret_cast<const f32x4*>(p.part + (z * per + row) * HD + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += ml.y == 0.f ? 0.f : w * part[e];   // saw nothing: not written
     }
   }
   const bool any = !(l == 0.f);
@@ -833,10 +836,11 @@ unsigned tile_slots(long long total, int mult, int R, int S) { return (unsigned)
 Group group_of(const AttnArgs& a) { return Group{a.group(), (uint32_t)((1ull << 32) / a.group() + 1)}; }
 
 // How the forward runs: SPLIT (Share) where a sequence has 32 packed rows or fewer on average, or
-// the 128-row tiles would leave half of the CUs idle; and the splits of the key axis, while
-// the workgroups are few (split kernels: 2048, whose lengths vary; else two per CU), at least 256
-// keys of an average sequence each. The lengths are on the device: a cache counts with its
-// capacity.
+// the 128-row tiles would leave half of the CUs idle; and the splits of the key axis, up to two
+// workgroups per CU with at least 256 keys of an average sequence each (32 single tokens against
+// caches of up to 8192 rows, 8 key heads of 128: 116 us with 2 splits, 120 with 4, 138 with 8: a
+// workgroup's start costs about as much as 100 keys). The lengths are on the device: a cache
+// counts with its capacity.
 struct FwdPlan {
   bool split;
   int nsplit;
@@ -848,7 +852,7 @@ FwdPlan fwd_plan(const AttnArgs& a) {
   auto wgs = [&](int R) { return std::max<long long>((rows + R - 1) / R, a.seqs) * a.kv_heads; };
   FwdPlan f;
   f.split = rows <= 32LL * a.seqs || wgs(16 * kFwdQB * kWaves) < 128;
-  const long long n = f.split ? 2048 / wgs(16) : 512 / wgs(16 * kFwdQB * kWaves);
+  const long long n = 512 / wgs(f.split ? 16 : 16 * kFwdQB * kWaves);
   f.nsplit = (int)std::max<long long>(std::min<long long>(std::min<long long>(n, avg_k / 256), 64), 1);
   return f;
 }
