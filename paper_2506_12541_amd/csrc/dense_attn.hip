@@ -523,9 +523,14 @@ struct BwdP {
   float sl2;
 };
 
-// dq, and each row's terms for the key-major pass.
+// dq, and each row's terms for the key-major pass. D comes from the output as it was rounded to
+// bf16, and an error e of D is common to a row's keys: where few keys carry a row dP - D cancels,
+// and e dominates (scores with a deviation of 9: dq and dk were off by 0.005 of their norm, three
+// times the rounding of the result). But sum P (dP - D) = -e is summed beside, in float32: with M =
+// sum P k, which takes one product more, dq = scale (sum P (dP - D) k - sum P (dP - D) M), and the
+// key-major pass gets D + sum P (dP - D).
 template <typename T, int HD, int QB, bool SPLIT>
-__global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kernel(BwdP p) {
+__global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD == 128 ? 2 : 1)) packed_dq_kernel(BwdP p) {
   typedef Share<T, HD, SPLIT> SH;
   static_assert(!SPLIT || QB == 1, "one block of rows");
   constexpr int KT = SH::tile, NCH = HD / 32, DB = HD / 16, R = 16 * QB * (SPLIT ? 1 : SH::NW), ST = SH::step;
@@ -548,8 +553,9 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kern
   int pr[QB];
   int lim[QB];
   CT qf[QB][NCH], df[QB][NCH];
-  f32x4 acc[QB][DB];
-  float l2[QB], dd[QB];
+  constexpr bool FIX = sizeof(T) == 2;   // float32 outputs are exact enough
+  f32x4 acc[QB][DB], mean[FIX ? QB : 1][DB];
+  float l2[QB], dd[QB], e[QB];
   const int off = sq.lk - sq.lq;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
@@ -575,10 +581,12 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kern
     }
     dd[qb] = col_sum(d);
     l2[qb] = on && lim[qb] >= 0 ? p.lse[at.h * a.total_q + at.t] * kLog2e : __builtin_huge_valf();
-    if (on && j == 0 && (!SPLIT || wid == 0))
-      p.terms[((long long)hk * a.total_q + sq.q0) * G.G + pr[qb]] = make_float2(l2[qb], dd[qb]);
+    e[qb] = 0.f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int db = 0; db < DB; ++db) {
+      acc[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (FIX) mean[qb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
   }
   const int plast = min(p0 + R, rows) - 1;
   const int k_hi = p0 >= rows ? 0 : a.causal ? max(min(sq.lk, G.div(plast) + off + 1), 0) : sq.lk;
@@ -610,10 +618,10 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kern
             g[qb][kb] = mma(vf, df[qb][c], c == 0 ? f32x4{-dd[qb], -dd[qb], -dd[qb], -dd[qb]} : g[qb][kb]);
           }
         }
-      CT ds[QB];
+      CT ds[QB], pf[QB];
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        float v8[8];
+        float v8[8], p8[8];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -622,14 +630,20 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kern
             const float x = pv * g[qb][kb][i];
             const bool see = !decltype(mask)::value || t0 + kp * 32 + kb * 16 + 4 * j + i <= lim[qb];
             v8[4 * kb + i] = see ? x : 0.f;
+            p8[4 * kb + i] = see ? pv : 0.f;
+            if constexpr (FIX) e[qb] += v8[4 * kb + i];
           }
         ds[qb] = make_chunk<T>(v8);
+        if constexpr (FIX) pf[qb] = make_chunk<T>(p8);
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const CT kt = col_frag<HD>(kc, 32 * kp, 16 * db, lane);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) acc[qb][db] = mma(kt, ds[qb], acc[qb][db]);
+        for (int qb = 0; qb < QB; ++qb) {
+          acc[qb][db] = mma(kt, ds[qb], acc[qb][db]);
+          if constexpr (FIX) mean[qb][db] = mma(kt, pf[qb], mean[qb][db]);
+        }
       }
     }
   };
@@ -646,6 +660,28 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dq_kern
       if (t0 + ST < k_hi) step(std::true_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
   }
+  if constexpr (FIX) {
+    if constexpr (SPLIT) {   // the sum over the waves, in each of them
+      __shared__ float es[SH::NW][16];
+      e[0] = col_sum(e[0]);
+      if (j == 0) es[wid][r] = e[0];
+      __syncthreads();
+      e[0] = es[0][r];
+#pragma unroll
+      for (int w = 1; w < SH::NW; ++w) e[0] += es[w][r];
+    } else {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) e[qb] = col_sum(e[qb]);
+    }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[qb][db] -= e[qb] * mean[qb][db];
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+    if (pr[qb] < rows && j == 0 && (!SPLIT || wid == 0))
+      p.terms[((long long)hk * a.total_q + sq.q0) * G.G + pr[qb]] = make_float2(l2[qb], dd[qb] + e[qb]);
   auto store = [&](int row, int c, f32x4 v) {
     if (row >= ext || (row >= rows && !a.zero_rest)) return;
     const RowAt at = packed_row(sq, hk, G, row);

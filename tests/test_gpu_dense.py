@@ -253,6 +253,23 @@ def test_attention_scale_and_sharp_scores():
     check_attention(gen(15), "f32", [90, 200], [90, 200], 2, 2, 32, True, scale=0.5)
 
 
+@pytest.mark.parametrize("lens,d", [([600], 64), ([10, 70, 3], 64), ([400, 33], 128), ([40] * 30, 32)])
+def test_attention_gradients_of_sharp_rows(lens, d):
+    """Rows that few keys carry: dP - D cancels, so D may not come from the rounded output alone. By
+    norm dq and dk may be off by two independent roundings to bf16 (dS and the result), each of
+    half a step over sqrt(3) at most."""
+    g = gen(23)
+    cu, n = packed(lens), sum(lens)
+    q, k = normal(g, n, 4, d, dtype=BF, scale=3.0), normal(g, n, 2, d, dtype=BF, scale=3.0)
+    v, do = normal(g, n, 2, d, dtype=BF), normal(g, n, 4, d, dtype=BF)
+    want = ref.attention(q, k, v, cu, cu, None, True, None, do)
+    o, lse = dense.attention_forward(q, k, v, cu, causal=True)
+    got = dense.attention_backward(q, k, v, o, lse, do, cu, causal=True)
+    for name in ("dq", "dk", "dv"):
+        err = (got[name].double().cpu() - want[name][0]).norm() / want[name][0].norm()
+        assert err <= math.sqrt(2 / 3) * ref.HALF[BF], (name, err.item())
+
+
 def test_attention_values_of_keys_behind_the_end_do_not_enter():
     """NaN in unused cache rows, in rows of no sequence, and in other sequences stays out."""
     g = gen(16)
