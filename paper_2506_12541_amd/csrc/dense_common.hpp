@@ -61,5 +61,24 @@ template <> __device__ __forceinline__ uint4 pack16<bf16_t>(const float* v) {
   return __builtin_bit_cast(uint4, make_chunk<bf16_t>(v));
 }
 
+// Eight consecutive elements at element alignment; load_chunk_to: the first n of them (n <= 0:
+// none), zeros behind.
+__device__ __forceinline__ bf16x8 load_chunk_u(const bf16_t* p) { return __builtin_bit_cast(bf16x8, load16u(p)); }
+__device__ __forceinline__ f32x8 load_chunk_u(const float* p) {
+  f32x8 v;
+  __builtin_memcpy(&v, p, 32);
+  return v;
+}
+__device__ __forceinline__ bf16x8 load_chunk_to(const bf16_t* p, int n) {
+  const uint4 v = n >= 8 ? load16u(p) : n > 0 ? load_partial(p, n) : make_uint4(0, 0, 0, 0);
+  return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ f32x8 load_chunk_to(const float* p, int n) {
+  f32x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+  return v;
+}
+
 }  // namespace
 }  // namespace bsa

@@ -82,27 +82,63 @@ struct Epi {
   float* part;        // not NULL: the bare sums go to part[split][M][N] instead
 };
 
-// Four (EN) consecutive columns n.. of row m.
-template <typename T, int EN>
-__device__ __forceinline__ void epi_store(const Epi<T>& o, long long m, int n, float (&v)[EN], int split) {
+// Four consecutive columns of a row at element alignment.
+__device__ __forceinline__ void load4u(const float* p, float (&v)[4]) { __builtin_memcpy(v, p, 16); }
+__device__ __forceinline__ void load4u(const bf16_t* p, float (&v)[4]) {
+  uint2 u;
+  __builtin_memcpy(&u, p, 8);
+  v[0] = __uint_as_float(u.x << 16);
+  v[1] = __uint_as_float(u.x & 0xffff0000u);
+  v[2] = __uint_as_float(u.y << 16);
+  v[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void store4u(float* p, const float (&v)[4]) { __builtin_memcpy(p, v, 16); }
+__device__ __forceinline__ void store4u(bf16_t* p, const float (&v)[4]) {
+  const uint2 u = make_uint2((uint32_t)f2bf(v[0]) | ((uint32_t)f2bf(v[1]) << 16), (uint32_t)f2bf(v[2]) | ((uint32_t)f2bf(v[3]) << 16));
+  __builtin_memcpy(p, &u, 8);
+}
+
+// Four consecutive columns n.. of row m.
+template <typename T>
+__device__ __forceinline__ void epi_store4(const Epi<T>& o, long long m, int n, float (&v)[4], int split) {
   if (m >= o.M || n >= o.N) return;
-  if (o.part) {
-    float* p = o.part + ((long long)split * o.M + m) * o.N + n;
+  if (n + 4 <= o.N) {
+    if (o.part) {
+      store4u(o.part + ((long long)split * o.M + m) * o.N + n, v);
+      return;
+    }
+    float t[4];
+    if (o.bias) {
+      load4u(o.bias + n, t);
 #pragma unroll
-    for (int e = 0; e < EN; ++e)
-      if (n + e < o.N) p[e] = v[e];
+      for (int e = 0; e < 4; ++e) v[e] += t[e];
+    }
+    if (o.pre) store4u(o.pre + m * o.N + n, v);
+    if (o.act != kActNone) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = act_fwd<T>(v[e], o.act);
+    }
+    if (o.res) {
+      load4u(o.res + m * o.ldr + n, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += t[e];
+    }
+    store4u(o.out + m * o.ldo + n, v);
     return;
   }
 #pragma unroll
-  for (int e = 0; e < EN; ++e) {
-    if (n + e < o.N) {
-      float z = v[e];
-      if (o.bias) z += to_f32<T>(o.bias[n + e]);
-      if (o.pre) o.pre[m * o.N + n + e] = from_f32<T>(z);
-      z = act_fwd<T>(z, o.act);
-      if (o.res) z += to_f32<T>(o.res[m * o.ldr + n + e]);
-      o.out[m * o.ldo + n + e] = from_f32<T>(z);
+  for (int e = 0; e < 3; ++e) {   // the row ends inside
+    if (n + e >= o.N) break;
+    if (o.part) {
+      o.part[((long long)split * o.M + m) * o.N + n + e] = v[e];
+      continue;
     }
+    float z = v[e];
+    if (o.bias) z += to_f32<T>(o.bias[n + e]);
+    if (o.pre) o.pre[m * o.N + n + e] = from_f32<T>(z);
+    z = act_fwd<T>(z, o.act);
+    if (o.res) z += to_f32<T>(o.res[m * o.ldr + n + e]);
+    o.out[m * o.ldo + n + e] = from_f32<T>(z);
   }
 }
 
@@ -405,7 +441,7 @@ __global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long l
 #pragma unroll
     for (int j = 0; j < FJ; ++j) {
       float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      epi_store<T, 4>(o, m0 + wm * (BM / 2) + 16 * i + (lane & 15), n0 + wn * (BN / 2) + 16 * j + 4 * (lane >> 4), v,
+      epi_store4(o, m0 + wm * (BM / 2) + 16 * i + (lane & 15), n0 + wn * (BN / 2) + 16 * j + 4 * (lane >> 4), v,
                       blockIdx.y);
     }
 }
@@ -453,7 +489,9 @@ struct DmaTile {
 // Eight consecutive columns of a row: whole 16-byte pieces unless the row ends inside.
 __device__ __forceinline__ void epi_store8(const Epi<bf16_t>& o, long long m, int n, float (&v)[8], int split) {
   if (n + 8 > o.N || o.part) {
-    epi_store<bf16_t, 8>(o, m, n, v, split);
+    float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+    epi_store4(o, m, n, a, split);
+    epi_store4(o, m, n + 4, b, split);
     return;
   }
   if (m >= o.M) return;
@@ -639,6 +677,64 @@ __global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a
   }
 }
 
+// ---- few rows: the weight is streamed once ----
+
+// y of up to 16 MB rows of x: a workgroup owns 16 output columns (rows of w) and its NW waves split
+// the contraction, 128 indices at a time in turn. Weights go from memory into the matrix
+// instructions' operand (the weight's 16 rows first, x's rows the columns), no LDS on the way;
+// x comes from the caches. The waves' sums meet in LDS, added in order. Bound by the weight's
+// bytes: 4 rows, 4096 -> 8192 channels (67 MB) take 14.6 us, 4.6 TB/s; with the tiles above 24.
+template <typename T, int MB, int NW>
+__global__ void __launch_bounds__(64 * NW) few_rows_kernel(Mat<T> x, Mat<T> w, int K, Epi<T> o) {
+  typedef typename Chunk<T>::type CT;
+  __shared__ __attribute__((aligned(16))) float part[NW][MB][256];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, r = lane & 15, j = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const T* const wp = w.p + (long long)min(n0 + r, (int)w.rows - 1) * w.ld + 8 * j;
+  const T* xp[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) xp[b] = x.p + min((long long)(16 * b + r), x.rows - 1) * x.ld + 8 * j;
+  f32x4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int whole = K / 128;
+#pragma unroll 2
+  for (int g = wid; g < whole; g += NW) {
+    CT wf[4], xf[MB][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      wf[c] = load_chunk_u(wp + 128 * g + 32 * c);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) xf[b][c] = load_chunk_u(xp[b] + 128 * g + 32 * c);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) acc[b] = mma(wf[c], xf[b][c], acc[b]);
+  }
+  if (wid == whole % NW) {   // the rest of the contraction
+    for (int k = 128 * whole; k < K; k += 32) {
+      const CT wf = load_chunk_to(wp + k, K - k - 8 * j);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) acc[b] = mma(wf, load_chunk_to(xp[b] + k, K - k - 8 * j), acc[b]);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < MB; ++b) *reinterpret_cast<f32x4*>(&part[wid][b][4 * lane]) = acc[b];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * MB; i += 64 * NW) {
+    const int b = i / 64, l = i % 64;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = part[0][b][4 * l + e];
+#pragma unroll
+      for (int q = 1; q < NW; ++q) v[e] += part[q][b][4 * l + e];
+    }
+    epi_store4(o, 16 * b + (l & 15), n0 + 4 * (l >> 4), v, 0);
+  }
+}
+
 // y = epilogue(sum over the splits, in order), four columns per thread
 template <typename T>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* __restrict__ part, int S, Epi<T> o) {
@@ -648,13 +744,21 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const float* __restrict_
   const long long m = i / nq;
   const int n = (int)(i - m * nq) * 4;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int s = 0; s < S; ++s) {
     const float* p = part + ((long long)s * o.M + m) * o.N + n;
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n + 4 <= o.N) {
+      load4u(p, t);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < o.N) v[e] += p[e];
+      for (int e = 0; e < 3; ++e)
+        if (n + e < o.N) t[e] = p[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += t[e];
   }
-  epi_store<T, 4>(o, m, n, v, 0);
+  epi_store4(o, m, n, v, 0);
 }
 
 // ---- dz = dy act'(z) and the partial column sums of dz ----
@@ -742,25 +846,40 @@ struct Plan {
   int T, S;
 };
 
-// bf16 products: 256 x 256 tiles (8 waves) where there are enough of them, else 128 x 128 and
-// 64 x 64; with may_split the contraction is split, in powers of two, until about every CU has a
-// workgroup, at least 512 contraction indices each. f32 products: 128 or 64.
-Plan plan_product(bool bf16, long long M, int N, long long K, bool may_split) {
+// bf16: 256 x 256 tiles (8 waves) where there are 192 of them, else 128 x 128 where there are 256,
+// else 64 x 64; float32: 128 x 128 where there are 512 of them, else 64 x 64. The contraction is
+// split, in powers of two, while the tiles leave CUs idle: each split writes and reads its sums
+// once more and takes a second launch, which 256 indices (512 of the largest tiles) pay for.
+Plan plan_product(bool bf16, long long M, int N, long long K) {
   auto tiles = [&](int T) { return ((M + T - 1) / T) * ((N + T - 1) / T); };
-  Plan p{128, 1};
+  Plan p{64, 1};
   if (!bf16) {
-    if (tiles(128) < 512) p.T = 64;
-    if (may_split)
-      while (tiles(p.T) * p.S < 768 && K / (2 * p.S) >= 256 && p.S < 64) p.S *= 2;
-    return p;
-  }
-  if (bf16 && (tiles(256) >= 192 || (may_split && tiles(256) * (K / 512) >= 192)))
+    if (tiles(128) >= 512) p.T = 128;
+  } else if (tiles(256) * std::max<long long>(K / 512, 1) >= 192 && tiles(256) >= 12) {
     p.T = 256;
-  else if (tiles(128) < 256 && !(may_split && tiles(128) * (K / 512) >= 256))
-    p.T = 64;
-  if (may_split)
-    while (tiles(p.T) * p.S < (p.T == 256 ? 192 : 256) && K / (2 * p.S) >= 512 && p.S < 64) p.S *= 2;
+  } else if (tiles(128) * std::max<long long>(K / 512, 1) >= 256) {
+    p.T = 128;
+  }
+  const long long want = p.T == 256 ? 192 : bf16 ? 256 : 512, least = p.T == 64 ? 256 : 512;
+  while (tiles(p.T) * p.S < want && K / (2 * p.S) >= least && p.S < 64) p.S *= 2;
   return p;
+}
+
+size_t plan_bytes(const Plan& p, long long M, long long N) { return p.S > 1 ? sizeof(float) * (size_t)p.S * M * N : 0; }
+
+// Whether the forward streams the weight through few_rows_kernel: up to 16 rows, and up to 64 where the
+// contraction is too short to pay for a split product's second launch. (bf16, 64 rows, 1024 -> 1024
+// channels: 9.2 us, split 13.0; 4096 -> 4096: 21.3 us, split 15.6, as every 16 columns read all of x.)
+bool few_rows_ok(const LinearArgs& a) { return a.m <= 16 || (a.m <= 64 && a.k <= 1024); }
+
+template <typename T, int NW>
+void few_rows(int MB, dim3 grid, const Mat<T>& x, const Mat<T>& w, int K, const Epi<T>& o, hipStream_t st) {
+  if (MB == 1)
+    few_rows_kernel<T, 1, NW><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
+  else if (MB == 2)
+    few_rows_kernel<T, 2, NW><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
+  else
+    few_rows_kernel<T, 4, NW><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
 }
 
 bool dma_ok(const Mat<bf16_t>& m, bool tr, long long K) {
@@ -808,7 +927,7 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
 
 struct LinBwdWs {
   size_t dz, dbp, part, total;
-  Plan dw;
+  Plan dx, dw;
   int P;
   long long rpg;
 };
@@ -818,7 +937,8 @@ LinBwdWs linear_bwd_layout(const LinearArgs& a) {
   const int E = 16 / (int)esz;
   size_t off = 0;
   auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
-  L.dw = plan_product(a.bf16, a.n, a.k, a.m, true);
+  L.dx = plan_product(a.bf16, a.m, a.k, a.n);
+  L.dw = plan_product(a.bf16, a.n, a.k, a.m);
   // row groups of the dz pass: about 1024 workgroups, at least 32 rows each
   const long long gx = (a.n + 32 * E - 1) / (32 * E);
   long long P = std::min<long long>(std::max<long long>(1024 / gx, 1), (a.m + 31) / 32);
@@ -827,7 +947,7 @@ LinBwdWs linear_bwd_layout(const LinearArgs& a) {
   L.P = (int)(L.rpg ? (a.m + L.rpg - 1) / L.rpg : 1);
   L.dz = put(a.act == kActNone ? 0 : esz * (size_t)a.m * a.n);
   L.dbp = put(sizeof(float) * (size_t)L.P * a.n);
-  L.part = put(L.dw.S > 1 ? sizeof(float) * (size_t)L.dw.S * a.n * a.k : 0);
+  L.part = put(std::max(plan_bytes(L.dx, a.m, a.k), plan_bytes(L.dw, a.n, a.k)));
   L.total = off;
   return L;
 }
@@ -835,9 +955,22 @@ LinBwdWs linear_bwd_layout(const LinearArgs& a) {
 template <typename T>
 hipError_t linear_fwd(const LinearArgs& a, const void* x, const void* w, const void* bias, const void* res, void* y,
                       void* pre, void* ws, hipStream_t st) {
-  Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, (const T*)res, a.ldr, (T*)pre, a.act, nullptr};
-  return product<T, false, false>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.n,
-                                  a.k, plan_product(a.bf16, a.m, a.n, a.k, false), (float*)ws, o, st);
+  const Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, (const T*)res, a.ldr, (T*)pre, a.act, nullptr};
+  const Mat<T> mx{(const T*)x, a.ldx, a.m, a.k}, mw{(const T*)w, a.ldw, a.n, a.k};
+  if (few_rows_ok(a)) {
+    const int MB = a.m <= 16 ? 1 : a.m <= 32 ? 2 : 4;
+    const dim3 grid((a.n + 15) / 16);
+    // waves per workgroup: about two per SIMD of the chip, at most one per 128 indices
+    const long long wg = grid.x;
+    if (wg >= 512 || a.k <= 512)
+      few_rows<T, 4>(MB, grid, mx, mw, a.k, o, st);
+    else if (wg >= 256 || a.k <= 1024)
+      few_rows<T, 8>(MB, grid, mx, mw, a.k, o, st);
+    else
+      few_rows<T, 16>(MB, grid, mx, mw, a.k, o, st);
+    return hipGetLastError();
+  }
+  return product<T, false, false>(mx, mw, a.m, a.n, a.k, plan_product(a.bf16, a.m, a.n, a.k), (float*)ws, o, st);
 }
 
 template <typename T>
@@ -869,8 +1002,8 @@ hipError_t linear_bwd(const LinearArgs& a, const void* x, const void* w, const v
   const Mat<T> mz{dz ? dz : (const T*)dy, dz ? a.n : a.lddy, a.m, a.n};
   if (dx) {
     Epi<T> o{a.m, a.k, (T*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
-    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n,
-                                             plan_product(a.bf16, a.m, a.k, a.n, false), nullptr, o, st);
+    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n, L.dx,
+                                             (float*)(c + L.part), o, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
@@ -888,7 +1021,9 @@ hipError_t linear_bwd(const LinearArgs& a, const void* x, const void* w, const v
 
 }  // namespace
 
-size_t linear_fwd_ws_bytes(const LinearArgs&) { return 0; }
+size_t linear_fwd_ws_bytes(const LinearArgs& a) {
+  return few_rows_ok(a) ? 0 : plan_bytes(plan_product(a.bf16, a.m, a.n, a.k), a.m, a.n);
+}
 
 hipError_t launch_linear_fwd(const LinearArgs& a, const void* x, const void* w, const void* bias, const void* res,
                              void* y, void* pre, void* ws, hipStream_t st) {
