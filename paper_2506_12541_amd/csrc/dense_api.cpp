@@ -227,6 +227,10 @@ bsa_status_t bsa_attention_forward(const bsa_attention_t* p, const void* q, cons
     if (!q || !cu_q || !cu_k || !o || !lse) return bad("q, cu_q, cu_k, o and lse must be non-NULL");
     if (a.total_k > 0 && (!k || !v)) return bad("k and v must be non-NULL");
     if (o == q || o == k || o == v) return bad("o may not alias an input");
+    const long long d = a.hd, rows = (a.total_q - 1) * a.o_row + d, heads = (a.heads - 1) * a.o_head + d;
+    if (!((a.heads == 1 || a.o_head >= d) && (a.total_q == 1 || a.o_row >= heads)) &&
+        !((a.total_q == 1 || a.o_row >= d) && (a.heads == 1 || a.o_head >= rows)))
+      return bad("o's rows and heads may not overlap");
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16))
       return bad("q, k, v and o must be 16-byte aligned");
     const size_t need = bsa::attention_fwd_ws_bytes(a);

@@ -174,15 +174,16 @@ __global__ void __launch_bounds__(NT) layernorm_fwd_kernel(const T* __restrict__
   }
 }
 
+// A row is read whole before it is written: dx may be x or dy.
 // Workgroup b takes rows b GPW .. in steps of the grid; the column sums of its rows go to
 // part[b][2][cols] (dgain, dbias): each lane sums its own columns over its rows, then the
 // groups are added in order through LDS.
 template <typename T, int L, int NV, int NT>
-__global__ void __launch_bounds__(NT) layernorm_bwd_kernel(const T* __restrict__ x, const float* __restrict__ gain,
+__global__ void __launch_bounds__(NT) layernorm_bwd_kernel(const T* x, const float* __restrict__ gain,
                                                            const float* __restrict__ mean,
-                                                           const float* __restrict__ rstd, const T* __restrict__ dy,
-                                                           NormArgs a, T* __restrict__ dx, float* __restrict__ part,
-                                                           float* __restrict__ part_b, long long part_ld) {
+                                                           const float* __restrict__ rstd, const T* dy, NormArgs a, T* dx,
+                                                           float* __restrict__ part, float* __restrict__ part_b,
+                                                           long long part_ld) {
   constexpr int E = NormVec<T>::E, GPW = NT / L;
   __shared__ __attribute__((aligned(16))) float sums[GPW > 1 ? NT * 2 * E : 2 * NT / 64];
   const int l = threadIdx.x % L, grp = threadIdx.x / L;

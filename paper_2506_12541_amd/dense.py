@@ -64,9 +64,10 @@ def _rows(t, name, cols=None, dtype=None, dev=None, rows=None):
     m = t.numel() // n
     if rows is not None and m != rows:
         raise ValueError(f"{name} must have {rows} rows, got {m}")
-    if t.is_contiguous():
-        return m, n, n
-    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= n:
+    if t.is_contiguous() or m <= 1:
+        if t.stride(-1) == 1 or n == 1:
+            return m, n, n
+    elif t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= n:
         return m, n, t.stride(0)
     raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows that do not overlap")
 
@@ -211,11 +212,16 @@ def _heads(t, name, dtype=None, dev=None, shape=None):
         raise ValueError(f"{name} must be [rows, heads, head_dim]")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    packed = t.shape[1] * t.shape[2], t.shape[2]
     if t.is_contiguous():
-        return t.shape[1] * t.shape[2], t.shape[2]
+        return packed
     if t.stride(2) != 1:
         raise ValueError(f"{name} must be contiguous along head_dim")
-    return t.stride(0), t.stride(1)
+    # the stride of a dimension of one entry says nothing
+    row, head = (t.stride(i) if t.shape[i] != 1 else packed[i] for i in (0, 1))
+    if row % (16 // t.element_size()) or head % (16 // t.element_size()):
+        raise ValueError(f"{name}'s rows and heads must lie multiples of 16 bytes apart")
+    return row, head
 
 
 def _attention_params(q, k, v, cu_q, cu_k, used_k, causal, softmax_scale, zero_rest):
@@ -226,6 +232,10 @@ def _attention_params(q, k, v, cu_q, cu_k, used_k, causal, softmax_scale, zero_r
     if k.shape[2] != d or k.shape[1] == 0:
         raise ValueError(f"k must have head_dim {d} and at least one head, got {tuple(k.shape)}")
     v_row, v_head = _heads(v, "v", dt, dev, k.shape)
+    if cu_k is None:
+        if tq != k.shape[0]:
+            raise ValueError("cu_k is needed where k has other rows than q")
+        cu_k = cu_q
     _tensor(cu_q, "cu_q", torch.int32, dev)
     if cu_q.dim() != 1 or cu_q.numel() < 2 or not cu_q.is_contiguous():
         raise ValueError("cu_q must be a contiguous [sequences + 1] tensor")
@@ -252,10 +262,10 @@ def attention_forward(q, k, v, cu_q, cu_k=None, used_k=None, causal: bool = Fals
     1 / sqrt(d). Returns (o, lse): o like q, lse [heads, rows] float32. Rows in no sequence are 0 (lse
     -inf); in an o and lse that the caller passes they keep what they held."""
     lib = _lib.load()
-    cu_k = cu_q if cu_k is None else cu_k
     if (o is None) != (lse is None):
         raise ValueError("pass both o and lse, or neither")
     p = _attention_params(q, k, v, cu_q, cu_k, used_k, causal, softmax_scale, o is None)
+    cu_k = cu_q if cu_k is None else cu_k
     dev = q.device
     if o is not None:
         p.o_row, p.o_head = _heads(o, "o", q.dtype, dev, q.shape)
@@ -277,8 +287,8 @@ def attention_backward(q, k, v, o, lse, d_o, cu_q, cu_k=None, used_k=None, causa
     """Gradients of attention_forward given d_o (like o): dict(dq, dk, dv), contiguous, in q's type; dk and dv
     are summed over a key head's query heads. Rows in no sequence and unused cache rows are 0."""
     lib = _lib.load()
-    cu_k = cu_q if cu_k is None else cu_k
     p = _attention_params(q, k, v, cu_q, cu_k, used_k, causal, softmax_scale, True)
+    cu_k = cu_q if cu_k is None else cu_k
     dev = q.device
     p.o_row, p.o_head = _heads(o, "o", q.dtype, dev, q.shape)
     p.do_row, p.do_head = _heads(d_o, "d_o", q.dtype, dev, q.shape)

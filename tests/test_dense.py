@@ -114,6 +114,11 @@ def test_attention_pointers(lib):
     assert fwd(q=PTR + 8) == fwd(k=PTR + 2) == fwd(o=PTR + 8) == INVALID and "aligned" in lib.bsa_last_error().decode()
     assert fwd(o=PTR) == INVALID
     assert fwd(n=f.value - 1) == SMALL
+    p.o_row, p.o_head = 256, 32                     # heads of o on top of each other
+    assert fwd() == INVALID and "overlap" in lib.bsa_last_error().decode()
+    p.o_row, p.o_head = 64, 8 * 64                  # head-major is fine (the short workspace is found next)
+    assert fwd(n=f.value - 1) == SMALL
+    p.o_row = p.o_head = 0
     back = lambda dq=2 * PTR, dk=3 * PTR, n=1 << 40: lib.bsa_attention_backward(
         C.byref(p), *[PTR] * 8, None, dq, dk, 4 * PTR, PTR, n, None)
     assert back(dq=None) == back(dk=None) == back(dq=PTR) == back(dk=PTR + 4) == INVALID

@@ -1,12 +1,13 @@
 """Layer norm, affine map and packed attention on the GPU against their float64 definitions, within
 bounds derived from the types (tests/dense_ref.py)."""
+import ctypes as C
 import math
 
 import pytest
 import torch
 
 import dense_ref as ref
-from paper_2506_12541_amd import dense
+from paper_2506_12541_amd import _lib, dense
 
 pytestmark = pytest.mark.gpu
 
@@ -82,6 +83,27 @@ def test_layernorm_constant_rows_no_rows_and_values_that_are_not_finite():
     assert y.shape == (0, 48) and not got["dgain"].any() and not got["dbias"].any()
 
 
+def test_layernorm_backward_in_place():
+    """The C entry point with dx on top of dy, and of x."""
+    lib = _lib.load()
+    for rows, cols in ((300, 200), (40, 5000)):
+        g = gen(rows)
+        x, dy = normal(g, rows, cols, dtype=BF), normal(g, rows, cols, dtype=BF)
+        gain = normal(g, cols)
+        _, mean, rstd = dense.layernorm_forward(x, gain)
+        want = dense.layernorm_backward(x, gain, mean, rstd, dy)
+        p, need = _lib.bsa_layernorm_t(rows, cols, 1, 1e-5, 0, 0, 0, 0), C.c_size_t()
+        assert lib.bsa_layernorm_sizes(C.byref(p), C.byref(need)) == 0
+        ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device="cuda")
+        for over in (0, 1):
+            t = [x.clone(), dy.clone()]
+            dg, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+            assert lib.bsa_layernorm_backward(C.byref(p), t[0].data_ptr(), gain.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                              t[1].data_ptr(), t[over].data_ptr(), dg.data_ptr(), db.data_ptr(),
+                                              ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+            assert torch.equal(t[over], want["dx"]) and torch.equal(dg, want["dgain"]) and torch.equal(db, want["dbias"])
+
+
 # ---- affine map ----
 
 def check_linear(g, dtype, m, k, n, act, bias, residual, train=True, x=None):
@@ -142,6 +164,21 @@ def test_linear_strides(dtype):
     assert only["dx"] is None and torch.equal(only["dw"], a["dw"]) and torch.equal(only["db"], a["db"])
     only = dense.linear_backward(x, w, dy, pre, act="gelu", need_dw=False)
     assert only["dw"] is None and only["db"] is None and torch.equal(only["dx"], a["dx"])
+
+
+def test_linear_onto_the_residual():
+    """The C entry point with y on top of res, whichever way the product runs."""
+    lib = _lib.load()
+    for dt, m, k, n in ((BF, 4, 256, 96), (BF, 100, 2048, 96), (BF, 3000, 128, 2048), (F32, 100, 1024, 99), (F32, 9, 70, 33)):
+        g = gen(m + k)
+        x, w, r = normal(g, m, k, dtype=dt), normal(g, n, k, dtype=dt, scale=0.1), normal(g, m, n, dtype=dt)
+        want, _ = dense.linear_forward(x, w, None, r, act="silu")
+        p, need = _lib.bsa_linear_t(m, k, n, int(dt == BF), 3, 0, 0, 0, 0, 0), C.c_size_t()
+        assert lib.bsa_linear_sizes(C.byref(p), C.byref(need), None) == 0
+        ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device="cuda")
+        assert lib.bsa_linear_forward(C.byref(p), x.data_ptr(), w.data_ptr(), None, r.data_ptr(), r.data_ptr(), None,
+                                      ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(r, want)
 
 
 def test_linear_no_rows_and_rows_that_are_not_finite():
@@ -238,6 +275,7 @@ def test_attention_steps_against_a_cache(dtype, heads, kv, d):
 def test_attention_many_sequences():
     lens = [(i * 7) % 23 for i in range(300)]
     check_attention(gen(10), "bf16", lens, lens, 2, 1, 32, True)
+    check_attention(gen(11), "bf16", lens, [24] * 300, 4, 2, 64, True, used=[i % 25 for i in range(300)], tail=70)
     check_attention(gen(11), "bf16", [1] * 300, [64] * 300, 2, 2, 32, True, train=False, used=[i % 65 for i in range(300)])
 
 
@@ -322,6 +360,26 @@ def test_attention_strides(dtype):
     c = dense.attention_backward(hm(q), hm(k), hm(v), hm(o), lse, hm(do), cu, causal=True)
     for x, y in ((o, o2), (o, o3), (lse, lse2), (lse, lse3), *((a[n], b[n]) for n in a), *((a[n], c[n]) for n in a)):
         assert torch.equal(x, y)
+
+
+def test_attention_heads_and_rows_of_one():
+    """Views whose dimensions of one entry have strides that mean nothing, and refused ones."""
+    g = gen(24)
+    cu1, cu = packed([1]), packed([30])
+    base = normal(g, 30, 5, 64, dtype=BF)
+    q, k = base[7:8, 1:4], base[:, 4:5]
+    o, lse = dense.attention_forward(q, k, k, cu1, cu)
+    o2, lse2 = dense.attention_forward(q.contiguous(), k.contiguous(), k.contiguous(), cu1, cu)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    odd = torch.zeros(30, 67, device="cuda", dtype=BF).as_strided((30, 1, 64), (67, 64, 1))
+    with pytest.raises(ValueError, match="16 bytes"):
+        dense.attention_forward(odd, odd, odd, cu)
+    with pytest.raises(ValueError, match="cu_k"):
+        dense.attention_forward(q, k, k, cu1)
+    with pytest.raises(ValueError, match="int32"):
+        dense.attention_forward(q, k, k, cu1, cu.long())
+    with pytest.raises(ValueError, match="CUDA"):
+        dense.attention_forward(q, k, k, cu1, cu.cpu())
 
 
 def test_attention_without_rows():
