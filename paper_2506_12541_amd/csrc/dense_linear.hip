@@ -335,7 +335,7 @@ __device__ __forceinline__ void interleave() {
 // the matrix cores are busy 45% of the time, the VALU (splitting) 42%.
 // Accumulator lane L holds C[m + L % 16][n + 4 (L / 16) + e] (B's fragment comes first).
 template <typename T, bool TA, bool TB, int BM, int BN>
-__global__ void __launch_bounds__(256) product_kernel(Mat<T> a, Mat<T> b, long long K, int ntn, long long kt_per, Epi<T> o) {
+__global__ void __launch_bounds__(256, (BM * BN <= 8192 ? 2 : 1)) product_kernel(Mat<T> a, Mat<T> b, long long K, int ntn, long long kt_per, Epi<T> o) {
   constexpr int BK = 32, FI = BM / 32, FJ = BN / 32;
   typedef RegTile<T, TA, TA != TB, BM> LA;
   typedef RegTile<T, TB, TA != TB, BN> LB;
@@ -912,10 +912,15 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
   }
   if (!dma) {
     const long long per = ((K + 31) / 32 + p.S - 1) / p.S;
+    // float32: 128 x 64 tiles split a quarter less, where there are enough of them (3586 x 512 -> 1024:
+    // 35 us, 64 x 64 tiles 42; 261 tiles of the odd map's dx: 65 us, 64 x 64 tiles 59)
+    const long long tall = (M + 127) / 128 * ntn;
     if (side == 128)
       product_kernel<T, TA, TB, 128, 128><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
-    else
+    else if (sizeof(T) == 2 || tall * p.S < 320)
       product_kernel<T, TA, TB, 64, 64><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
+    else if constexpr (sizeof(T) == 4)
+      product_kernel<T, TA, TB, 128, 64><<<dim3((unsigned)tall, (unsigned)p.S), 256, 0, st>>>(a, b, K, ntn, per, o);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.S == 1) return e;
