@@ -180,7 +180,14 @@ __device__ __forceinline__ void join_sum(float* m, const f32x4 (&acc)[HD / 16], 
 
 // ---- LDS tiles of ROWS x HD elements, filled by direct loads, 16-byte pieces swizzled ----
 
-template <typename T, int HD> __device__ __forceinline__ int tswz(int row) { return swz<HD * (int)sizeof(T) / 2>(row); }
+// 256-byte bf16 rows (each starts at bank 0) are read both as row fragments and by transposing reads;
+// an even exclusive-or by the row's low bits keeps the pairs of pieces that a transposing read takes
+// together and puts 8 rows on distinct banks. (swz<128> serves row fragments alone: with it a third of
+// the forward's LDS cycles were conflicts, now none are; d = 128 passes over 4096 tokens -0 to -2 %.)
+template <typename T, int HD>
+__device__ __forceinline__ int tswz(int row) {
+  return sizeof(T) == 2 && HD == 128 ? 2 * (row & 7) : swz<HD * (int)sizeof(T) / 2>(row);
+}
 
 // Rows r0 + [0, ROWS) of a matrix with row stride ld, by NW waves; rows at or past nrows repeat the
 // last one (masked by the caller; nrows > 0).
@@ -201,7 +208,9 @@ struct TileLoad {
 
 // 8 consecutive elements (chunk lc) of a tile row
 template <int HD>
-__device__ __forceinline__ bf16x8 row_frag(const bf16_t* t, int x, int lc) { return lds_row_chunk<HD>(t, x, lc); }
+__device__ __forceinline__ bf16x8 row_frag(const bf16_t* t, int x, int lc) {
+  return *reinterpret_cast<const bf16x8*>(t + x * HD + 8 * (lc ^ tswz<bf16_t, HD>(x)));
+}
 template <int HD>
 __device__ __forceinline__ f32x8 row_frag(const float* t, int x, int lc) {
   const float* row = t + x * HD;
@@ -213,7 +222,18 @@ __device__ __forceinline__ f32x8 row_frag(const float* t, int x, int lc) {
 // column m0 + lane % 16 at rows k0 + 4j + i and k0 + 16 + 4j + i (j = lane / 16, i = 0..3)
 template <int HD>
 __device__ __forceinline__ bf16x8 col_frag(const bf16_t* t, int k0, int m0, int lane) {
-  return lds_tr_chunk<HD>(t, k0, m0, lane);
+  if constexpr (HD != 128) {
+    return lds_tr_chunk<HD>(t, k0, m0, lane);
+  } else {   // the same reads with this file's swizzle
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int p = lane & 15, x0 = k0 + 4 * (lane >> 4) + (p >> 2), x1 = x0 + 16, col = m0 + 4 * (p & 3);
+    const bf16_t* a0 = t + x0 * HD + 8 * ((col >> 3) ^ tswz<bf16_t, HD>(x0)) + (col & 7);
+    const bf16_t* a1 = t + x1 * HD + 8 * ((col >> 3) ^ tswz<bf16_t, HD>(x1)) + (col & 7);
+    const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a0));
+    const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a1));
+    return __builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y));
+  }
 }
 template <int HD>
 __device__ __forceinline__ f32x8 col_frag(const float* t, int k0, int m0, int lane) {
