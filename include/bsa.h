@@ -358,8 +358,8 @@ bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const voi
  * filled so far) or, with used_k NULL, cu_k[s+1] - cu_k[s]. Query head h reads key head
  * h / (heads / kv_heads). o = softmax(scale q k^T) v over the visible keys: all of the sequence's, or,
  * causal, key j for query i when j <= i + (l - query rows): the last query sees every key. A query
- * that sees no key has o = 0 and lse = -inf and takes no part in the gradients. A value of v, d_o, q or
- * k that is not finite may reach every row of the 64-row tile that it is read in.
+ * that sees no key has o = 0 and lse = -inf and takes no part in the gradients. A value that is not
+ * finite reaches rows and keys that see it (where it may become NaN in all columns), and no others.
  * cu_q, cu_k [seqs + 1] and used_k [seqs] are device arrays (int32): from 0, not decreasing, at most
  * total_q, total_k and the capacity cu_k[s+1] - cu_k[s]. They cannot be checked on the host: values
  * outside the tensors are pulled inside (nothing is read or written out of bounds), and then

@@ -247,6 +247,53 @@ __device__ __forceinline__ f32x8 col_frag(const float* t, int k0, int m0, int la
   return v;
 }
 
+// ---- values that are not finite, behind the causal mask ----
+//
+// A masked probability is 0, but 0 times an infinity or NaN of a masked row is NaN in a matrix product.
+// So before a tile on the causal diagonal is used, its 16-byte pieces that hold such a value are zeroed, and the rows
+// that see one get their NaN apart: o and dq from the first such key, the key-major pass from the row's lse. (Doing it within the products cost 10 to 40 % in registers on calls that hold no
+// such value.)
+
+// An exponent of all ones carries into its value's sign bit.
+template <typename T>
+__device__ __forceinline__ bool odd_piece(const uint4& u) {
+  constexpr uint32_t ones = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, low = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+  const uint32_t any = ((u.x & ones) + low) | ((u.y & ones) + low) | ((u.z & ones) + low) | ((u.w & ones) + low);
+  return any & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u);
+}
+
+__device__ __forceinline__ bool odd_chunk(const bf16x8& x) { return odd_piece<bf16_t>(__builtin_bit_cast(uint4, x)); }
+__device__ __forceinline__ bool odd_chunk(const f32x8& x) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) any |= (__float_as_uint(x[e]) & 0x7f800000u) + 0x00800000u;
+  return any & 0x80000000u;
+}
+
+// Clears a landed tile of ROWS x HD; returns its first row that held such a value (ROWS: none). Every wave
+// that shares the tile searches all of it, so that all of them take the same way.
+template <typename T, int HD, int ROWS, bool SPLIT>
+__device__ __forceinline__ int clear_tile(T* tile) {
+  constexpr int CPR = HD * (int)sizeof(T) / 16;
+  uint4* const piece = reinterpret_cast<uint4*>(tile);
+  const int lane = threadIdx.x & 63;
+  uint32_t odd = 0;      // one bit per piece of this lane
+  static_assert(ROWS * CPR / 64 <= 32, "a bit each");
+#pragma unroll 4
+  for (int u = 0; u < ROWS * CPR / 64; ++u) odd |= (uint32_t)odd_piece<T>(piece[u * 64 + lane]) << u;
+  if (!__builtin_amdgcn_ballot_w64(odd != 0)) return ROWS;
+  int first = odd ? (__builtin_ctz(odd) * 64 + lane) / CPR : ROWS;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
+  if constexpr (!SPLIT) __syncthreads();   // every wave has searched it
+  for (; odd; odd &= odd - 1) piece[__builtin_ctz(odd) * 64 + lane] = make_uint4(0, 0, 0, 0);
+  if constexpr (SPLIT)
+    wave_sync();
+  else
+    __syncthreads();
+  return __builtin_amdgcn_readfirstlane(first);
+}
+
 // Quotients by the group size: floor(x / G) by a multiplication, one too large at most (x < 2^31).
 struct Group {
   int G;
@@ -369,8 +416,15 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_fwd_ker
     TileLoad<T, HD, KT, SH::LW>::issue(kd, kh, a.k_row, t0, sq.lk, lw, lane);
     TileLoad<T, HD, KT, SH::LW>::issue(vd, vh, a.v_row, t0, sq.lk, lw, lane);
   };
-  auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
+  int odd_key = INT32_MAX;   // the first key with a v that is not finite, from the diagonal's tiles
+  auto step = [&](auto mask, int t0, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
     tile_ready<SPLIT>();
+    if constexpr (decltype(mask)::value) {
+      if (a.causal) {
+        const int x = clear_tile<T, HD, KT, SPLIT>(vc);
+        odd_key = x < KT ? min(odd_key, t0 + x) : odd_key;
+      }
+    }
     if (t0 + ST < k_hi) issue(t0 + ST, kn, vn);
     f32x4 s[QB][KB];
 #pragma unroll
@@ -443,6 +497,13 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_fwd_ker
       step(std::true_type{}, t0, ks0, vs0, ks1, vs1);
       if (t0 + ST < k_hi) step(std::true_type{}, t0 + ST, ks1, vs1, ks0, vs0);
     }
+  }
+  if (odd_key != INT32_MAX) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        if (odd_key <= lim[qb]) o[qb][db] *= __builtin_nanf("");
   }
   // four columns of a finished row (first: the thread that also writes the row's statistics)
   auto store = [&](int row, int c, f32x4 v, float m, float l, bool first) {
@@ -587,6 +648,7 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD 
     const T* dp = (const T*)p.d_o + at.t * a.do_row + at.h * a.do_head;
     const T* op = (const T*)p.o + at.t * a.o_row + at.h * a.o_head;
     float d = 0.f;
+    bool odd = false;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       qf[qb][c] = zero_chunk(CT{});
@@ -595,12 +657,15 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD 
         qf[qb][c] = load_chunk(qp + 32 * c + 8 * j);
         df[qb][c] = load_chunk(dp + 32 * c + 8 * j);
         const CT of = load_chunk(op + 32 * c + 8 * j);
+        odd |= odd_chunk(qf[qb][c]) || odd_chunk(df[qb][c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d = fmaf((float)df[qb][c][e], (float)of[e], d);
       }
     }
     dd[qb] = col_sum(d);
     l2[qb] = on && lim[qb] >= 0 ? p.lse[at.h * a.total_q + at.t] * kLog2e : __builtin_huge_valf();
+    // a row whose q or dO is not finite: the key-major pass, which clears it, gets its NaN from here
+    if (col_max(odd ? 1.f : 0.f) != 0.f) l2[qb] = __builtin_nanf("");
     e[qb] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -620,8 +685,15 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD 
     TileLoad<T, HD, KT, SH::LW>::issue(kd, kh, a.k_row, t0, sq.lk, lw, lane);
     TileLoad<T, HD, KT, SH::LW>::issue(vd, vh, a.v_row, t0, sq.lk, lw, lane);
   };
-  auto step = [&](auto mask, int t0, const T* kc, const T* vc, T* kn, T* vn) __attribute__((always_inline)) {
+  int odd_key = INT32_MAX;   // the first key with a k that is not finite, from the diagonal's tiles
+  auto step = [&](auto mask, int t0, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
     tile_ready<SPLIT>();
+    if constexpr (decltype(mask)::value) {
+      if (a.causal) {
+        const int x = clear_tile<T, HD, KT, SPLIT>(kc);
+        odd_key = x < KT ? min(odd_key, t0 + x) : odd_key;
+      }
+    }
     if (t0 + ST < k_hi) issue(t0 + ST, kn, vn);
 #pragma unroll
     for (int kp = 0; kp < KT / 32; ++kp) {
@@ -697,6 +769,13 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD 
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[qb][db] -= e[qb] * mean[qb][db];
+  }
+  if (odd_key != INT32_MAX) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        if (odd_key <= lim[qb]) acc[qb][db] *= __builtin_nanf("");
   }
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb)
@@ -783,8 +862,12 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW)) packed_dkv_ker
       td[QT + tid] = -t.y;
     }
   };
-  auto step = [&](auto mask, int t0, const T* qc, const T* dc, const float* tc, T* qn, T* dn, float* tn) __attribute__((always_inline)) {
+  auto step = [&](auto mask, int t0, T* qc, T* dc, const float* tc, T* qn, T* dn, float* tn) __attribute__((always_inline)) {
     tile_ready<SPLIT>();
+    if constexpr (decltype(mask)::value) {   // masked tiles are the causal diagonal's
+      clear_tile<T, HD, QT, SPLIT>(qc);      // keys that such a row sees get NaN from its lse
+      clear_tile<T, HD, QT, SPLIT>(dc);
+    }
     if (t0 + ST < rows) issue(t0 + ST, qn, dn, tn);
     f32x4 s[KW][2], g[KW][2];
     CT pf[KW], sf[KW];

@@ -330,6 +330,45 @@ def test_attention_values_of_keys_behind_the_end_do_not_enter():
         assert not a[n][70:100].any() and not a[n][141:].any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("lens", [[100, 75], [100] * 130])
+def test_attention_values_that_are_not_finite_behind_the_causal_mask(lens, d, dtype):
+    """An infinity or NaN reaches the rows and keys that see it, all of them and no others."""
+    g, n, at, t = gen(25), sum(lens), lens[0], 37            # sequence 1, its row t
+    cu, row, end = packed(lens), lens[0] + 37, lens[0] + lens[1]
+    clean = dict(q=normal(g, n, 4, d, dtype=DT[dtype]), k=normal(g, n, 2, d, dtype=DT[dtype]),
+                 v=normal(g, n, 2, d, dtype=DT[dtype]), do=normal(g, n, 4, d, dtype=DT[dtype]))
+
+    def both(ts):
+        o, lse = dense.attention_forward(ts["q"], ts["k"], ts["v"], cu, causal=True)
+        return dict(dense.attention_backward(ts["q"], ts["k"], ts["v"], o, lse, ts["do"], cu, causal=True), o=o, lse=lse)
+
+    want = both(clean)
+    later, keys = slice(row, end), slice(at, row + 1)
+    for name, value, head in (("q", math.nan, 1), ("do", math.inf, 1), ("do", math.nan, 1), ("k", math.nan, 0),
+                              ("v", -math.inf, 0), ("v", math.nan, 0)):
+        ts = dict(clean, **{name: clean[name].clone()})
+        ts[name][row, head, 5] = value
+        got = both(ts)
+        # per output: rows and heads (and column) that are not finite
+        one, pair, every = slice(head, head + 1), slice(0, 2), slice(None)
+        bad = {"q": dict(o=(row, one, every), dq=(row, one, every), dk=(keys, 0, every), dv=(keys, 0, every)),
+               "do": dict(dq=(row, one, every), dk=(keys, 0, every), dv=(keys, 0, every)),
+               "k": dict(o=(later, pair, every), dq=(later, pair, every), dk=(slice(at, end), 0, every),
+                         dv=(slice(at, end), 0, every)),
+               "v": dict(o=(later, pair, every), dq=(later, pair, every), dk=(slice(at, end), 0, every))}[name]
+        for out in ("o", "dq", "dk", "dv"):
+            mark = torch.zeros_like(got[out], dtype=torch.bool)
+            if out in bad:
+                mark[bad[out]] = True
+            fin = got[out].isfinite()
+            assert torch.equal(got[out][~mark], want[out][~mark]), (name, value, out)
+            if (name, out) in (("do", "dv"), ("v", "o")):    # column 5 at least
+                mark[..., :5] = mark[..., 6:] = False
+            assert not fin[mark].any(), (name, value, out, fin[mark].sum().item())
+
+
 @pytest.mark.parametrize("lk", [100, 3000])
 def test_attention_leaves_rows_behind_the_last_sequence(lk):
     g = gen(17)
