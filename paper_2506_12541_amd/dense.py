@@ -219,6 +219,8 @@ def _heads(t, name, dtype=None, dev=None, shape=None):
         raise ValueError(f"{name} must be contiguous along head_dim")
     # the stride of a dimension of one entry says nothing
     row, head = (t.stride(i) if t.shape[i] != 1 else packed[i] for i in (0, 1))
+    if row == 0 and head == 0:    # the C ABI's packed tensor
+        raise ValueError(f"{name} may be broadcast over its rows or its heads, not over both: pass {name}.contiguous()")
     if row % (16 // t.element_size()) or head % (16 // t.element_size()):
         raise ValueError(f"{name}'s rows and heads must lie multiples of 16 bytes apart")
     return row, head
@@ -256,11 +258,11 @@ def _attention_sizes(lib, p):
 def attention_forward(q, k, v, cu_q, cu_k=None, used_k=None, causal: bool = False, softmax_scale: float = 0.0,
                       o=None, lse=None, stream=None):
     """Attention over packed sequences: q [rows, heads, d], k and v [key rows, kv_heads, d] (kv_heads divides
-    heads; strided views of a fused projection are fine), cu_q and cu_k [sequences + 1] int32 first rows of
-    the sequences and the end (cu_k None: the same rows as cu_q), used_k [sequences] int32 the key rows in
-    use of each sequence's cache. causal: the last query of a sequence sees its last key. softmax_scale 0:
-    1 / sqrt(d). Returns (o, lse): o like q, lse [heads, rows] float32. Rows in no sequence are 0 (lse
-    -inf); in an o and lse that the caller passes they keep what they held."""
+    heads; strided views of a fused projection are fine, tensors broadcast over rows and heads are refused), cu_q
+    and cu_k [sequences + 1] int32 first rows of the sequences and the end (cu_k None: the same rows as cu_q),
+    used_k [sequences] int32 the key rows in use of each sequence's cache. causal: the last query of a sequence
+    sees its last key. softmax_scale 0: 1 / sqrt(d). Returns (o, lse): o like q, lse [heads, rows] float32. Rows
+    in no sequence are 0 (lse -inf); in an o and lse that the caller passes they keep what they held."""
     lib = _lib.load()
     if (o is None) != (lse is None):
         raise ValueError("pass both o and lse, or neither")

@@ -137,3 +137,28 @@ def test_binding_refuses_what_is_not_on_a_gpu():
         dense.attention_forward(x.view(4, 1, 8), x.view(4, 1, 8), x.view(4, 1, 8), cu)
     with pytest.raises(ValueError, match="both"):
         dense.attention_forward(x.view(4, 1, 8), x.view(4, 1, 8), x.view(4, 1, 8), cu, o=x)
+
+
+def test_binding_refuses_heads_that_are_broadcast_over_rows_and_heads(monkeypatch):
+    """Strides of 0 and 0 are the C ABI's packed tensor: a [rows, heads, d] tensor over the storage of one row of d
+    elements (the gradient of o.sum((0, 1))) would be read, and as an output written, behind its end."""
+    monkeypatch.setattr(dense, "_tensor", lambda *a, **kw: None)       # the tensors here are on the CPU
+    o = torch.zeros(5, 3, 64, requires_grad=True)
+    grad, = torch.autograd.grad((o.sum((0, 1)) * torch.ones(64)).sum(), o)
+    one = torch.zeros(64)
+    for t in (grad, one.expand(5, 3, 64), torch.zeros(7, 1, 1, 64)[2].expand(2, 3, 64)):
+        assert t.stride()[:2] == (0, 0)
+        with pytest.raises(ValueError, match="broadcast"):
+            dense._heads(t, "d_o")
+    # over one of them the strides say what they are; a dimension of one entry is not broadcast
+    assert dense._heads(torch.zeros(5, 1, 64).expand(5, 3, 64), "k") == (64, 0)
+    assert dense._heads(torch.zeros(1, 3, 64).expand(5, 3, 64), "k") == (0, 64)
+    assert dense._heads(one.expand(5, 1, 64), "k") == (0, 64)
+    assert dense._heads(one.expand(1, 3, 64), "k") == (192, 0)
+
+
+def test_attention_refuses_an_output_that_is_broadcast(lib):
+    for row, head in ((0, 64), (64, 0)):
+        p = att(o_row=row, o_head=head)
+        assert lib.bsa_attention_forward(C.byref(p), *[PTR] * 6, 2 * PTR, PTR, PTR, 1 << 40, None) == INVALID
+        assert "overlap" in lib.bsa_last_error().decode()

@@ -421,6 +421,32 @@ def test_attention_heads_and_rows_of_one():
         dense.attention_forward(q, k, k, cu1, cu.cpu())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_broadcast_tensors(dtype):
+    """Tensors broadcast over their rows or their heads give the bits of whole ones; over both they are refused."""
+    g, dt = gen(27), DT[dtype]
+    cu = packed([30, 45])
+    q, o_grad = normal(g, 75, 4, 64, dtype=dt), normal(g, 75, 1, 64, dtype=dt).expand(75, 4, 64)
+    k, v = normal(g, 75, 1, 64, dtype=dt).expand(75, 2, 64), normal(g, 1, 2, 64, dtype=dt).expand(75, 2, 64)
+    whole = lambda t: t.contiguous()
+    o, lse = dense.attention_forward(q, k, v, cu, causal=True)
+    o2, lse2 = dense.attention_forward(q, whole(k), whole(v), cu, causal=True)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    a = dense.attention_backward(q, k, v, o, lse, o_grad, cu, causal=True)
+    b = dense.attention_backward(q, whole(k), whole(v), o, lse, whole(o_grad), cu, causal=True)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    both_q, both_k = normal(g, 64, dtype=dt).expand(75, 4, 64), normal(g, 64, dtype=dt).expand(75, 2, 64)
+    k, v = whole(k), whole(v)
+    for ts in ((both_q, k, v), (q, both_k, v), (q, k, both_k)):
+        with pytest.raises(ValueError, match="broadcast"):
+            dense.attention_forward(*ts, cu)
+    with pytest.raises(ValueError, match="broadcast"):
+        dense.attention_forward(q, k, v, cu, o=both_q, lse=lse)
+    for ts in ((o, both_q), (both_q, o)):
+        with pytest.raises(ValueError, match="broadcast"):
+            dense.attention_backward(q, k, v, ts[0], lse, ts[1], cu)
+
+
 def test_attention_without_rows():
     q = torch.zeros(0, 2, 64, device="cuda", dtype=BF)
     k = torch.ones(9, 2, 64, device="cuda", dtype=BF)
