@@ -787,7 +787,8 @@ __global__ void __launch_bounds__((64 * Share<T, HD, SPLIT>::NW), (!SPLIT && HD 
   auto store = [&](int row, int c, f32x4 v) {
     if (row >= ext || (row >= rows && !a.zero_rest)) return;
     const RowAt at = packed_row(sq, hk, G, row);
-    store4((T*)p.dq + (at.t * a.heads + at.h) * HD + c, v, a.scale);
+    // (a row of no sequence summed products of its zeros: NaN beside a key that is not finite)
+    store4((T*)p.dq + (at.t * a.heads + at.h) * HD + c, row < rows ? v : f32x4{0.f, 0.f, 0.f, 0.f}, a.scale);
   };
   if constexpr (!SPLIT) {
 #pragma unroll

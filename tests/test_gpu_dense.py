@@ -369,6 +369,39 @@ def test_attention_values_that_are_not_finite_behind_the_causal_mask(lens, d, dt
             assert not fin[mark].any(), (name, value, out, fin[mark].sum().item())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens", [[100, 300], [100] * 130 + [300]])
+def test_attention_rows_in_no_sequence_beside_values_that_are_not_finite(lens, causal, d, dtype):
+    """Rows behind the last sequence share its last tile: a key of it with an infinity or NaN, which every
+    row of the sequence sees, leaves them 0."""
+    g, n, tail = gen(28), sum(lens), 20
+    first = n - lens[-1]                               # the last sequence's first row and key
+    cu = packed(lens)
+    q, do = normal(g, n + tail, 4, d, dtype=DT[dtype]), normal(g, n + tail, 4, d, dtype=DT[dtype])
+    k, v = normal(g, n + tail, 2, d, dtype=DT[dtype]), normal(g, n + tail, 2, d, dtype=DT[dtype])
+
+    def both(k, v):
+        o, lse = dense.attention_forward(q, k, v, cu, causal=causal)
+        return dict(dense.attention_backward(q, k, v, o, lse, do, cu, causal=causal), o=o, lse=lse.t())
+
+    want = both(k, v)
+    for name, value in (("k", math.nan), ("k", math.inf), ("v", math.nan), ("v", -math.inf)):
+        bad = dict(k=k, v=v)
+        bad[name] = bad[name].clone()
+        bad[name][first, 1, 3] = value
+        got = both(**bad)
+        for out in ("o", "lse", "dq", "dk", "dv"):
+            assert torch.equal(got[out][:first], want[out][:first]), (name, value, out)
+            rest = got[out][n:]
+            assert (rest == -math.inf).all() if out == "lse" else not rest.any(), (name, value, out)
+        # an infinite key has P = 0 where its score is -inf: by the formula column 3 alone, 0 times infinity, is then NaN
+        cols = slice(3, 4) if (name, value) == ("k", math.inf) else slice(None)
+        assert not got["dq"][first:n, 2:, cols].isfinite().any(), (name, value)
+        assert torch.equal(got["dq"][first:n, :2], want["dq"][first:n, :2]), (name, value)   # the other key head's
+
+
 @pytest.mark.parametrize("lk", [100, 3000])
 def test_attention_leaves_rows_behind_the_last_sequence(lk):
     g = gen(17)
