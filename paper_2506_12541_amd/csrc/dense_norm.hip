@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(NT) layernorm_fwd_kernel(const T* __restrict__
       }
     group_sum<L>(q, red);
     const float d = q[0] / (float)a.cols;
-    const float rs = 1.0f / sqrtf(fmaxf(q[1] / (float)a.cols - d * d, 0.f) + a.eps);
+    const float var = q[1] / (float)a.cols - d * d;
+    const float rs = 1.0f / sqrtf((var < 0.f ? 0.f : var) + a.eps);   // NaN stays (a row that is not finite)
     if (on) {
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(NT) layernorm_fwd_kernel(const T* __restrict__
         norm_store(y + row * a.ldy, l + L * t, a.cols, v[t]);
       }
       if (l == 0) {
-        mean[row] = mu + d;
+        mean[row] = fabsf(mu) < __builtin_huge_valf() ? mu + d : mu;   // infinite: d is NaN
         rstd[row] = rs;
       }
     }

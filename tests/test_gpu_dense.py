@@ -83,6 +83,21 @@ def test_layernorm_constant_rows_no_rows_and_values_that_are_not_finite():
     assert y.shape == (0, 48) and not got["dgain"].any() and not got["dbias"].any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [48, 333, 700, 5000, 20001])
+def test_layernorm_statistics_of_rows_that_are_not_finite(cols, dtype):
+    """As the formula gives them: the variance is NaN, the mean what the sum is."""
+    x = torch.full((6, cols), 2.0, dtype=DT[dtype], device="cuda")
+    x[1, 3] = math.nan
+    x[2, cols - 1] = math.inf
+    x[3, 0] = -math.inf
+    x[4, 0], x[4, 1] = math.inf, -math.inf
+    y, mean, rstd = dense.layernorm_forward(x, torch.ones(cols, device="cuda"))
+    assert rstd[1:5].isnan().all() and y[1:5].isnan().all() and not y[0].any() and not y[5].any()
+    assert mean[1].isnan() and mean[2] == math.inf and mean[3] == -math.inf and mean[4].isnan()
+    assert mean[0] == 2 and mean[5] == 2 and rstd[0] == rstd[5] and rstd[0].isfinite()
+
+
 def test_layernorm_backward_in_place():
     """The C entry point with dx on top of dy, and of x."""
     lib = _lib.load()
