@@ -1,6 +1,8 @@
 // C entry points of the dense operators: argument checks and launches. Declarations and
 // contracts: include/bsa.h.
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "dense.hpp"
@@ -36,6 +38,10 @@ bsa_status_t small_ws(const char* where, size_t need) {
 bool dtype_ok(int32_t d) { return d == BSA_F32 || d == BSA_BF16; }
 bool ld_ok(int64_t ld, int64_t cols) { return ld == 0 || ld >= cols; }
 long long ld_of(int64_t ld, int64_t cols) { return ld ? ld : cols; }
+// An output that is formed starts where one of the inputs does (NULL: not formed, not read).
+bool on_one(const void* out, std::initializer_list<const void*> inputs) {
+  return out && std::find(inputs.begin(), inputs.end(), out) != inputs.end();
+}
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 bsa_status_t check(const bsa_layernorm_t* p, bsa::NormArgs* a) {
@@ -172,7 +178,8 @@ bsa_status_t bsa_linear_forward(const bsa_linear_t* p, const void* x, const void
     bsa_status_t s = check(p, &a);
     if (s != BSA_OK || a.m == 0) return s;
     if (!x || !w || !y) return bad("x, w and y must be non-NULL");
-    if (y == x || y == w || y == pre) return bad("y may not alias x, w or pre");
+    if (on_one(y, {x, w, bias, pre})) return bad("y may not alias x, w, bias or pre");
+    if (on_one(pre, {x, w, bias, res})) return bad("pre may not alias an input");
     if (res == y && a.ldr != a.ldy) return bad("res may be y only with the same leading dimension");
     const size_t need = bsa::linear_fwd_ws_bytes(a);
     if (need && (!ws || ws_bytes < need)) return small_ws("affine map forward", need);
@@ -195,8 +202,9 @@ bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const voi
       if (a.act != bsa::kActNone && !pre) return bad("pre must be non-NULL for a map with an activation");
       if (dx && !w) return bad("w must be non-NULL for dx");
       if (dw && !x) return bad("x must be non-NULL for dw");
-      if (dx && (dx == dy || dx == pre || dx == x || dx == w)) return bad("dx may not alias an input");
     }
+    for (const void* g : {dx, dw, db})
+      if (on_one(g, {x, w, a.act == bsa::kActNone ? nullptr : pre, dy})) return bad("a gradient may not alias an input");
     const size_t need = bsa::linear_bwd_ws_bytes(a);
     if (need && (!ws || ws_bytes < need)) return small_ws("affine map backward", need);
     hipError_t e;
@@ -256,9 +264,8 @@ bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, con
     if (a.total_k > 0 && (!k || !v || !dk || !dv)) return bad("k, v, dk and dv must be non-NULL");
     for (const void* t : {q, k, v, o, d_o, (const void*)dq, (const void*)dk, (const void*)dv})
       if (!aligned(t, 16)) return bad("q, k, v, o, d_o, dq, dk and dv must be 16-byte aligned");
-    for (const void* g : {(const void*)dq, (const void*)dk, (const void*)dv})
-      for (const void* t : {q, k, v, o, d_o})
-        if (g && g == t) return bad("a gradient may not alias an input");
+    for (const void* g : {dq, dk, dv})
+      if (on_one(g, {q, k, v, o, d_o})) return bad("a gradient may not alias an input");
     const size_t need = bsa::attention_bwd_ws_bytes(a);
     if (need && (!ws || ws_bytes < need)) return small_ws("attention backward", need);
     if (need && !aligned(ws, 16)) return bad("ws must be 16-byte aligned");

@@ -162,3 +162,26 @@ def test_attention_refuses_an_output_that_is_broadcast(lib):
         p = att(o_row=row, o_head=head)
         assert lib.bsa_attention_forward(C.byref(p), *[PTR] * 6, 2 * PTR, PTR, PTR, 1 << 40, None) == INVALID
         assert "overlap" in lib.bsa_last_error().decode()
+
+
+def test_linear_refuses_outputs_on_its_inputs(lib):
+    """Gradients and the kept pre-activation are written while other workgroups still read the inputs."""
+    p, big = lin(m=4096, act=2), 1 << 40
+    x, w, pre, dy, dx, dw, db, ws = (i * PTR for i in range(1, 9))
+    back = lambda dx=dx, dw=dw, db=db: lib.bsa_linear_backward(C.byref(p), x, w, pre, dy, dx, dw, db, ws, 0, None)
+    for t in (x, w, pre, dy):
+        for kw in (dict(dx=t), dict(dw=t), dict(db=t), dict(dx=None, db=None, dw=t), dict(dx=None, dw=None, db=t)):
+            assert back(**kw) == INVALID and "alias" in lib.bsa_last_error().decode(), (t // PTR, kw)
+    assert back() == SMALL and back(dx=None) == SMALL and back(dw=None, db=None) == SMALL
+    q = lin(m=4096)                                     # without an activation pre is not read
+    assert lib.bsa_linear_backward(C.byref(q), x, w, pre, dy, pre, dw, db, ws, 0, None) == SMALL
+    assert lib.bsa_linear_backward(C.byref(q), x, w, None, dy, dx, dw, None, ws, 0, None) == SMALL
+    assert lib.bsa_linear_backward(C.byref(q), x, w, None, dy, dx, dy, None, ws, 0, None) == INVALID
+    r = lin(m=100, k=8192, act=1)                       # a split contraction: the workspace is found short at last
+    bias, res, y = 4 * PTR, 5 * PTR, 6 * PTR
+    fwd = lambda y, pre: lib.bsa_linear_forward(C.byref(r), x, w, bias, res, y, pre, ws, 0, None)
+    for t in (x, w, bias):
+        assert fwd(t, 7 * PTR) == INVALID and "alias" in lib.bsa_last_error().decode()
+    for t in (x, w, bias, res, y):
+        assert fwd(y, t) == INVALID and "alias" in lib.bsa_last_error().decode()
+    assert fwd(y, 7 * PTR) == SMALL and fwd(res, 7 * PTR) == SMALL and fwd(y, None) == SMALL
