@@ -331,8 +331,9 @@ bsa_status_t bsa_layernorm_backward(const bsa_layernorm_t* p, const void* x, con
 /* Affine map with an epilogue: z = x w^T + bias, y = act(z) + res, with x [m, k], w [n, k], y [m, n]. */
 typedef enum { BSA_ACT_NONE = 0, BSA_ACT_RELU = 1, BSA_ACT_GELU = 2 /* erf form */, BSA_ACT_SILU = 3 } bsa_act_t;
 typedef struct {
-  int64_t m;                            /* rows, 0 .. 2^31 - 1                          */
-  int32_t k, n;                         /* input and output channels, >= 1              */
+  int64_t m;                            /* rows, 0 .. 2^31 - 256                        */
+  int32_t k, n;                         /* input and output channels, 1 .. 2^24; x, y
+                                           and w have fewer than 2^24 tiles of 128 x 128 */
   int32_t dtype;                        /* bsa_dtype_t of every tensor                  */
   int32_t act;                          /* bsa_act_t                                    */
   int64_t ld_x, ld_w, ld_y, ld_res, ld_dy;  /* elements between rows (0: packed)        */
@@ -365,7 +366,8 @@ bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const voi
  * outside the tensors are pulled inside (nothing is read or written out of bounds), and then
  * the outputs are not defined. */
 typedef struct {
-  int32_t seqs;                         /* >= 1                                         */
+  int32_t seqs;                         /* 1 .. 2^22 (more: where the tiles of a launch,
+                                           seqs and one for every 16 rows, are < 2^24)  */
   int32_t heads, kv_heads;              /* kv_heads divides heads                       */
   int32_t head_dim;                     /* 32, 64 or 128                                */
   int64_t total_q, total_k;             /* rows of q and of k and v; total_q times

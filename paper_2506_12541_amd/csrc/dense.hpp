@@ -49,6 +49,8 @@ struct AttnArgs {
   long long q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, do_row, do_head;
   int group() const { return heads / kv_heads; }
 };
+bool attention_fwd_fits(const AttnArgs& a);   // the launches are within the limits of one
+bool attention_bwd_fits(const AttnArgs& a);
 size_t attention_fwd_ws_bytes(const AttnArgs& a);
 hipError_t launch_attention_fwd(const AttnArgs& a, const void* q, const void* k, const void* v, const int* cu_q,
                                 const int* cu_k, const int* used_k, void* o, float* lse, void* ws, hipStream_t st);

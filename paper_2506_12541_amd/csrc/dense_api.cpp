@@ -35,6 +35,8 @@ bsa_status_t small_ws(const char* where, size_t need) {
   return set_error(BSA_ERR_WORKSPACE_TOO_SMALL, std::string(where) + " workspace needs " + std::to_string(need) + " bytes");
 }
 
+constexpr const char* kTooManyTiles = "too many tiles for one launch (2^32 threads or more)";
+
 bool dtype_ok(int32_t d) { return d == BSA_F32 || d == BSA_BF16; }
 bool ld_ok(int64_t ld, int64_t cols) { return ld == 0 || ld >= cols; }
 long long ld_of(int64_t ld, int64_t cols) { return ld ? ld : cols; }
@@ -63,9 +65,11 @@ bsa_status_t check(const bsa_linear_t* p, bsa::LinearArgs* a) {
   if (p->m < 0 || p->m > INT32_MAX) return bad("m must be in [0, 2^31)");
   if (p->k < 1 || p->n < 1) return bad("k and n must be >= 1");
   if (p->k > (1 << 24) || p->n > (1 << 24)) return set_error(BSA_ERR_UNSUPPORTED, "k and n must be <= 2^24");
-  if (((p->m + 63) / 64) * (((p->n > p->k ? p->n : p->k) + 63) / 64) > INT32_MAX ||
-      (((int64_t)p->n + 63) / 64) * (((int64_t)p->k + 63) / 64) > INT32_MAX)
-    return set_error(BSA_ERR_UNSUPPORTED, "too many 64 x 64 tiles (2^31 or more)");
+  // 256 x 256 tiles have 512 threads, 128 x 128 tiles 256 (64 x 64 tiles are used where there are few)
+  const auto fits = [](int64_t M, int64_t N) {
+    return (M + 255) / 256 * ((N + 255) / 256) < 1 << 23 && (M + 127) / 128 * ((N + 127) / 128) < 1 << 24;
+  };
+  if (!fits(p->m, std::max(p->n, p->k)) || !fits(p->n, p->k)) return set_error(BSA_ERR_UNSUPPORTED, kTooManyTiles);
   if (!dtype_ok(p->dtype)) return bad("bad dtype");
   if (p->act < BSA_ACT_NONE || p->act > BSA_ACT_SILU) return bad("bad act");
   if (!ld_ok(p->ld_x, p->k) || !ld_ok(p->ld_w, p->k) || !ld_ok(p->ld_y, p->n) || !ld_ok(p->ld_res, p->n) ||
@@ -232,6 +236,7 @@ bsa_status_t bsa_attention_forward(const bsa_attention_t* p, const void* q, cons
     bsa::AttnArgs a;
     bsa_status_t s = check(p, &a);
     if (s != BSA_OK || a.total_q == 0) return s;
+    if (!bsa::attention_fwd_fits(a)) return set_error(BSA_ERR_UNSUPPORTED, kTooManyTiles);
     if (!q || !cu_q || !cu_k || !o || !lse) return bad("q, cu_q, cu_k, o and lse must be non-NULL");
     if (a.total_k > 0 && (!k || !v)) return bad("k and v must be non-NULL");
     if (o == q || o == k || o == v) return bad("o may not alias an input");
@@ -259,6 +264,7 @@ bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, con
     bsa::AttnArgs a;
     bsa_status_t s = check(p, &a);
     if (s != BSA_OK) return s;
+    if (!bsa::attention_bwd_fits(a)) return set_error(BSA_ERR_UNSUPPORTED, kTooManyTiles);
     if (!cu_q || !cu_k) return bad("cu_q and cu_k must be non-NULL");
     if (a.total_q > 0 && (!q || !o || !lse || !d_o || !dq)) return bad("q, o, lse, d_o and dq must be non-NULL");
     if (a.total_k > 0 && (!k || !v || !dk || !dv)) return bad("k, v, dk and dv must be non-NULL");

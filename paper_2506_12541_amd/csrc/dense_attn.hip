@@ -1015,16 +1015,29 @@ hipError_t attn_fwd(FwdP p, bool split, hipStream_t st) {
   return hipGetLastError();
 }
 
+// 16-row blocks of queries, and of keys, that a wave of the backward owns.
+constexpr int dq_blocks(int hd) { return hd == 128 ? 1 : 2; }
+constexpr int dkv_blocks(int hd, bool bf16) { return hd == 128 || !bf16 ? 1 : 2; }
+
 // The backward's passes SPLIT where their usual tiles would not give three workgroups to every
 // four CUs.
+bool dq_split(const AttnArgs& a) {
+  const int R = 16 * dq_blocks(a.hd) * kWaves;
+  return (a.total_q * a.group() + R - 1) / R * a.kv_heads < 192;
+}
+bool dkv_split(const AttnArgs& a) {
+  const int R = 16 * dkv_blocks(a.hd, a.bf16) * kWaves;
+  return (a.total_k + R - 1) / R * a.kv_heads < 192;
+}
+
 template <typename T, int HD>
 hipError_t attn_bwd(BwdP p, hipStream_t st) {
-  constexpr int QB = HD == 128 ? 1 : 2, KW = HD == 128 || sizeof(T) == 4 ? 1 : 2;
+  constexpr int QB = dq_blocks(HD), KW = dkv_blocks(HD, sizeof(T) == 2);
   constexpr int RQ = 16 * QB * kWaves, RK = 16 * KW * kWaves;
   const AttnArgs& a = p.a;
   if (a.total_q > 0) {
     auto grid = [&](int R) { return dim3(tile_slots(a.total_q, a.group(), R, a.seqs), a.kv_heads); };
-    if ((a.total_q * a.group() + RQ - 1) / RQ * a.kv_heads < 192)
+    if (dq_split(a))
       packed_dq_kernel<T, HD, 1, true><<<grid(16), 64 * Share<T, HD, true>::NW, 0, st>>>(p);
     else
       packed_dq_kernel<T, HD, QB, false><<<grid(RQ), 64 * kWaves, 0, st>>>(p);
@@ -1033,7 +1046,7 @@ hipError_t attn_bwd(BwdP p, hipStream_t st) {
   }
   if (a.total_k > 0) {
     auto grid = [&](int R) { return dim3(tile_slots(a.total_k, 1, R, a.seqs), a.kv_heads); };
-    if ((a.total_k + RK - 1) / RK * a.kv_heads < 192)
+    if (dkv_split(a))
       packed_dkv_kernel<T, HD, 1, true><<<grid(16), 64 * Share<T, HD, true>::NW, 0, st>>>(p);
     else
       packed_dkv_kernel<T, HD, KW, false><<<grid(RK), 64 * kWaves, 0, st>>>(p);
@@ -1051,6 +1064,15 @@ hipError_t attn_bwd(BwdP p, hipStream_t st) {
                               : FN<float, 32>(__VA_ARGS__)))
 
 }  // namespace
+
+// The grids in x times their 256 threads (64 Share::NW at most) stay below 2^32, where a launch's limit lies.
+bool attention_fwd_fits(const AttnArgs& a) {
+  return tile_slots(a.total_q, a.group(), fwd_plan(a).split ? 16 : 16 * kFwdQB * kWaves, a.seqs) < 1u << 24;
+}
+bool attention_bwd_fits(const AttnArgs& a) {
+  return tile_slots(a.total_q, a.group(), dq_split(a) ? 16 : 16 * dq_blocks(a.hd) * kWaves, a.seqs) < 1u << 24 &&
+         tile_slots(a.total_k, 1, dkv_split(a) ? 16 : 16 * dkv_blocks(a.hd, a.bf16) * kWaves, a.seqs) < 1u << 24;
+}
 
 size_t attention_fwd_ws_bytes(const AttnArgs& a) {
   const int s = fwd_plan(a).nsplit;

@@ -833,8 +833,7 @@ __global__ void __launch_bounds__(1024) db_sum_kernel(const float* __restrict__ 
 
 template <typename T>
 __global__ void __launch_bounds__(256) fill_zero_kernel(T* p, long long n) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = from_f32<T>(0.f);
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += 256LL * gridDim.x) p[i] = from_f32<T>(0.f);
 }
 
 // ---- host ----
@@ -980,7 +979,7 @@ hipError_t linear_fwd(const LinearArgs& a, const void* x, const void* w, const v
 
 template <typename T>
 hipError_t zero(T* p, long long n, hipStream_t st) {
-  fill_zero_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p, n);
+  fill_zero_kernel<T><<<(unsigned)std::min<long long>((n + 255) / 256, 1 << 16), 256, 0, st>>>(p, n);
   return hipGetLastError();
 }
 

@@ -185,3 +185,24 @@ def test_linear_refuses_outputs_on_its_inputs(lib):
     for t in (x, w, bias, res, y):
         assert fwd(y, t) == INVALID and "alias" in lib.bsa_last_error().decode()
     assert fwd(y, 7 * PTR) == SMALL and fwd(res, 7 * PTR) == SMALL and fwd(y, None) == SMALL
+
+
+def test_launches_past_their_limit_are_refused(lib):
+    """A grid times its threads has to stay below 2^32."""
+    for kw in (dict(m=(1 << 31) - 1, n=8, k=8), dict(m=(1 << 31) - 255, n=8, k=8), dict(m=1 << 26, n=64, k=1 << 13)):
+        p = lin(**kw)
+        assert lib.bsa_linear_sizes(C.byref(p), None, None) == UNSUPPORTED and "tiles" in lib.bsa_last_error().decode()
+    for kw in (dict(m=(1 << 31) - 256, n=8, k=8), dict(m=0, n=1 << 16, k=1 << 16), dict(m=1 << 20, n=1 << 10, k=1 << 10)):
+        assert lib.bsa_linear_sizes(C.byref(lin(**kw)), None, None) == 0
+    # single tokens (16-row tiles), then usual tiles; the checks of pointers come behind that of the grid
+    forward = lambda p: lib.bsa_attention_forward(C.byref(p), *[None] * 9, 0, None)
+    backward = lambda p: lib.bsa_attention_backward(C.byref(p), *[None] * 13, 0, None)
+    for kw in (dict(seqs=1 << 24), dict(seqs=1 << 23, heads=1, kv_heads=1, total_q=1 << 27, total_k=1 << 27)):
+        p = att(**kw)
+        assert forward(p) == UNSUPPORTED and "tiles" in lib.bsa_last_error().decode()
+    p = att(seqs=1 << 24)
+    assert backward(p) == UNSUPPORTED and "tiles" in lib.bsa_last_error().decode()
+    p = att(heads=1, kv_heads=1, head_dim=128, seqs=1 << 10, total_q=1 << 30, total_k=1 << 10)
+    assert forward(p) == INVALID and backward(p) == UNSUPPORTED
+    p = att(heads=1, kv_heads=1, seqs=1 << 22, total_q=1 << 27, total_k=1 << 27)
+    assert forward(p) == backward(p) == INVALID

@@ -210,6 +210,13 @@ def test_linear_no_rows_and_rows_that_are_not_finite():
         assert (y[0] == k).all() and y[1].isinf().all() and y[2].isnan().all() and (y[3:] == k).all()
 
 
+def test_linear_gradient_without_rows_of_a_large_weight():
+    """dw of 2^32 elements, more than a launch has threads."""
+    w = torch.empty(1 << 16, 1 << 16, dtype=BF, device="cuda")
+    got = dense.linear_backward(w[:0], w, w[:0], need_dx=False, bias=True)
+    assert not got["dw"].any() and not got["db"].any()
+
+
 def test_linear_float32_values_that_do_not_split():
     """Infinities, NaN and the largest float32 values go through the three-part products as through one."""
     big = torch.finfo(F32).max
