@@ -670,3 +670,43 @@ def test_streams():
         again, _ = dense.linear_forward(x, w, act="silu")
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want) and torch.equal(again, want)
+
+
+def test_calls_on_a_given_stream_wait_for_its_work():
+    """Inputs arrive on a stream behind queued work, and the calls are given that stream while another is current:
+    forward, backward and workspaces of each operator come behind it."""
+    g = gen(29)
+    real = dict(x=normal(g, 300, 4096, dtype=BF), dy=normal(g, 300, 4096, dtype=BF), gain=normal(g, 4096),
+                w=normal(g, 96, 4096, dtype=BF, scale=0.1), dz=normal(g, 300, 96, dtype=BF),
+                q=normal(g, 40, 4, 64, dtype=BF), k=normal(g, 3000, 2, 64, dtype=BF), do=normal(g, 40, 4, 64, dtype=BF),
+                cu_q=packed([17, 23]), cu_k=packed([2000, 1000]))
+
+    def calls(t, stream=None):
+        y, mean, rstd = dense.layernorm_forward(t["x"], t["gain"], stream=stream)
+        out = [y, *dense.layernorm_backward(t["x"], t["gain"], mean, rstd, t["dy"], stream=stream).values()]
+        z, pre = dense.linear_forward(t["x"], t["w"], act="gelu", save_pre=True, stream=stream)
+        out += [z, pre, *dense.linear_backward(t["x"], t["w"], t["dz"], pre, act="gelu", bias=True, stream=stream).values()]
+        a = t["q"], t["k"], t["k"]
+        o, lse = dense.attention_forward(*a, t["cu_q"], t["cu_k"], stream=stream)
+        return out + [o, lse, *dense.attention_backward(*a, o, lse, t["do"], t["cu_q"], t["cu_k"], stream=stream).values()]
+
+    want = calls(real)
+    side = torch.cuda.Stream()
+    late = {n: torch.zeros_like(t) for n, t in real.items()}
+    a = normal(g, 8192, 8192, dtype=BF)
+    b = torch.empty_like(a)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.mm(a, a, out=b)
+    calls(late, side)                       # memory for the stream's tensors
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(30):
+            torch.mm(a, a, out=b)
+        for n in real:
+            late[n].copy_(real[n])
+    got = calls(late, side)
+    assert not side.query()                 # the products are still running
+    torch.cuda.synchronize()
+    for i, (u, v) in enumerate(zip(got, want)):
+        assert torch.equal(u, v), i
