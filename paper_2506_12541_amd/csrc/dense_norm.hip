@@ -325,8 +325,10 @@ hipError_t norm_dispatch(int cols, F f) {
     if (v <= 1024) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
   }
   if (v <= 2048) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-  if (v <= 4096) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
-  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
+  if constexpr (sizeof(T) == 4) {   // bf16 rows end at 4096 vectors
+    if (v > 4096) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
+  }
+  return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
 }
 
 // Workgroups of the backward: one for up to four steps of its groups (about 1 us each, where the
