@@ -845,23 +845,34 @@ struct Plan {
   int T, S;
 };
 
-// bf16: 256 x 256 tiles (8 waves) where there are 192 of them, else 128 x 128 where there are 256,
-// else 64 x 64; float32: 128 x 128 where there are 512 of them, else 64 x 64. The contraction is
-// split, in powers of two, while the tiles leave CUs idle: each split writes and reads its sums
-// once more and takes a second launch, which 256 indices (512 of the largest tiles) pay for.
+// The contraction is split, in powers of two, while the tiles leave CUs idle: each split writes and reads
+// its sums once more and takes a second launch, which 256 indices (512 of the larger tiles) pay for.
+//
+// bf16, us with the one and the other tile:
+// - 256 x 256 (8 waves, one workgroup per CU) where there are 192 of them (3586 x 4096 x 4096, 240 tiles: 107, 128 x 128
+//   115; contraction 512: 23.7 and 23.6), or where the splits of a long contraction fill the CUs in one round (65536 rows,
+//   dW of 1024 x 1024: 137 and 236, 2048 x 2048: 483 and 836, with 8192 rows: 81 and 91, forward 81 and 76), or in two
+//   where 128 x 128 tiles, two to a CU, take two as well (dW of 2560 x 3584: 65536 rows 1631 and 1977, 24576 rows 622
+//   and 716, 16384 rows 430 and 391). Else they lose: 2048 x 2048 x 2048 43 and 24, 2560 columns (80 tiles) 62 and 31.
+// - 128 x 128 where there are 256 of them (2048 x 1024 x 2048: 14.9, 64 x 64 16.8), or where a contraction of 4096 and
+//   more is split over them (1280 x 4096 x 1792: 38 and 49; 2048, no split of 64 x 64: 1024 x 2048 x 1024: 18.6 and 12.2).
+// float32: 128 x 128 where there are 512 of them (2560 x 2048 -> 3584, 560 tiles: 286 and 286; 2304 x 3200, 450
+// tiles: 213, 128 x 64 193), else 64 rows fewer or both (product()).
 Plan plan_product(bool bf16, long long M, int N, long long K) {
   auto tiles = [&](int T) { return ((M + T - 1) / T) * ((N + T - 1) / T); };
-  Plan p{64, 1};
-  if (!bf16) {
-    if (tiles(128) >= 512) p.T = 128;
-  } else if (tiles(256) * std::max<long long>(K / 512, 1) >= 192 && tiles(256) >= 12) {
-    p.T = 256;
-  } else if (tiles(128) * std::max<long long>(K / 512, 1) >= 256) {
-    p.T = 128;
+  auto plan = [&](int T, int want) {
+    Plan p{T, 1};
+    while (tiles(T) * p.S < want && K / (2 * p.S) >= (T == 64 ? 256 : 512) && p.S < 64) p.S *= 2;
+    return p;
+  };
+  if (!bf16) return plan(tiles(128) >= 512 ? 128 : 64, 512);
+  if (tiles(256) >= 192) return Plan{256, 1};
+  if (K >= 16384 && tiles(256) >= 12) {
+    const Plan p = plan(256, 192);
+    if (tiles(256) * p.S <= 256 || (K >= 24576 && tiles(128) > 512)) return p;
   }
-  const long long want = p.T == 256 ? 192 : bf16 ? 256 : 512, least = p.T == 64 ? 256 : 512;
-  while (tiles(p.T) * p.S < want && K / (2 * p.S) >= least && p.S < 64) p.S *= 2;
-  return p;
+  if (tiles(128) >= 256 || (K >= 4096 && tiles(128) * (K / 512) >= 256)) return plan(128, 256);
+  return plan(64, 256);
 }
 
 size_t plan_bytes(const Plan& p, long long M, long long N) { return p.S > 1 ? sizeof(float) * (size_t)p.S * M * N : 0; }
@@ -911,15 +922,15 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
   }
   if (!dma) {
     const long long per = ((K + 31) / 32 + p.S - 1) / p.S;
-    // float32: 128 x 64 tiles split a quarter less, where there are enough of them (3586 x 512 -> 1024:
-    // 35 us, 64 x 64 tiles 42; 261 tiles of the odd map's dx: 65 us, 64 x 64 tiles 59)
-    const long long tall = (M + 127) / 128 * ntn;
+    // float32: 64 x 64 tiles lie three to a CU. While they do so in one round they are faster than 128 x 64 (2816 x 512
+    // -> 1024, 704 tiles: 28.0 us and 30.3; 1536 x 2048 -> 2048, 768: 90 and 95); beyond, those split a quarter less
+    // (3000 x 515 -> 1029, 799: 39.7 and 34.8; 2048 x 2048 -> 2048, 1024: 119 and 102).
     if (side == 128)
       product_kernel<T, TA, TB, 128, 128><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
-    else if (sizeof(T) == 2 || tall * p.S < 320)
+    else if (sizeof(T) == 2 || (long long)ntm * ntn * p.S <= 768)
       product_kernel<T, TA, TB, 64, 64><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
     else if constexpr (sizeof(T) == 4)
-      product_kernel<T, TA, TB, 128, 64><<<dim3((unsigned)tall, (unsigned)p.S), 256, 0, st>>>(a, b, K, ntn, per, o);
+      product_kernel<T, TA, TB, 128, 64><<<dim3((unsigned)((M + 127) / 128 * ntn), (unsigned)p.S), 256, 0, st>>>(a, b, K, ntn, per, o);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.S == 1) return e;
