@@ -164,8 +164,9 @@ __device__ __forceinline__ uint4 load_piece(const Mat<T>& m, long long r, int c)
 
 // A product's operands as bf16 tiles in LDS: bf16 tensors are copied; a float32 value enters as the
 // sum of three bf16 values (P = 3 planes), x1 = bf16(x), x2 = bf16(x - x1), x3 = bf16(x - x1 - x2),
-// which holds its 24 bits, and a product as the six of nine part products that reach 2^-24 of it
-// (x2 y3, x3 y2, x3 y3 are left out, 2^-24 at most in all), accumulated in float32. That is 6 bf16
+// which holds its 24 bits (of values below 2^-110: to 2^-134, half the smallest bf16 step), and a
+// product as the six of nine part products that reach 2^-24 of it (x2 y3, x3 y2, x3 y3 are left out,
+// 2^-24 at most in all), accumulated in float32. That is 6 bf16
 // matrix instructions where the f32 ones take 16 times a bf16 one.
 struct Parts {
   uint2 p[3];   // four values of each part

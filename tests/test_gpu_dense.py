@@ -239,6 +239,29 @@ def test_linear_float32_values_that_do_not_split():
         assert got["dw"][:, 3].isnan().all() and torch.equal(got["dw"][:, k - 1], torch.full((n,), math.inf, device="cuda"))
 
 
+@pytest.mark.parametrize("exponent", [-100, -112, -118, -126, -140])
+def test_linear_float32_small_values(exponent):
+    """The three bf16 parts of a value leave 2^-27 of it, or half the smallest bf16 step (2^-133) where it is small;
+    sums are float32 with its smallest step of 2^-149 (6 part products for each of k, half a step each)."""
+    g, m, k, n = gen(30), 300, 200, 130
+    x = (torch.randn(m, k, generator=g, dtype=torch.float64) * 2.0 ** exponent).to(F32).cuda()
+    w, dy = normal(g, n, k), normal(g, m, n)
+
+    def close(name, got, a, b):            # a b^T; a: large values, b: small ones
+        a, b = a.double().cpu(), b.double().cpu()
+        depth = a.shape[1]
+        size = a.abs() @ b.abs().t()
+        bound = (depth + 8) * ref.F * size + 2.0 ** -134 * a.abs().sum(1, keepdim=True) * (1 + 2.0 ** -8) + 6 * depth * 2.0 ** -150
+        ref.check(name, got, a @ b.t(), bound)
+
+    y, _ = dense.linear_forward(x, w)
+    close("y", y.t(), w, x)
+    close("dw", dense.linear_backward(x, w, dy, need_dx=False)["dw"], dy.t(), x.t())
+    close("y of few rows", dense.linear_forward(x[:9], w)[0].t(), w, x[:9])
+    zeros = torch.zeros(m, n, device="cuda")
+    close("dx", dense.linear_backward(zeros, w.t().contiguous(), x, need_dw=False)["dx"].t(), w, x)
+
+
 # ---- packed attention ----
 
 def packed(lens):
