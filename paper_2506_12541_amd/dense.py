@@ -286,8 +286,9 @@ def attention_forward(q, k, v, cu_q, cu_k=None, used_k=None, causal: bool = Fals
 
 def attention_backward(q, k, v, o, lse, d_o, cu_q, cu_k=None, used_k=None, causal: bool = False,
                        softmax_scale: float = 0.0, stream=None):
-    """Gradients of attention_forward given d_o (like o): dict(dq, dk, dv), contiguous, in q's type; dk and dv
-    are summed over a key head's query heads. Rows in no sequence and unused cache rows are 0."""
+    """Gradients of attention_forward given d_o (like o; one that is broadcast over rows and heads, as o.sum((0, 1))
+    gives, is passed as d_o.contiguous()): dict(dq, dk, dv), contiguous, in q's type; dk and dv are summed over a
+    key head's query heads. Rows in no sequence and unused cache rows are 0."""
     lib = _lib.load()
     p = _attention_params(q, k, v, cu_q, cu_k, used_k, causal, softmax_scale, True)
     cu_k = cu_q if cu_k is None else cu_k
