@@ -296,7 +296,8 @@ bsa_status_t bsa_block_backward(const bsa_params_t* p, int32_t ffn_dim, const bs
 /* ---- Dense operators beside the layer ----
  *
  * What a model has around the sparse layer: layer norms, affine maps with an activation or a
- * residual, and full attention over packed sequences. They follow the conventions above
+ * residual, gated maps, rotary positions with head norms, full attention over packed sequences, and
+ * a cache of 8 bits for it. They follow the conventions above
  * (device pointers of the current device, asynchronous on `stream` alone, caller-owned
  * buffers, host-side checks before any launch) and are deterministic. They take bf16 or
  * float32 tensors (dtype); every sum and statistic is float32 and a result is rounded once to
@@ -359,6 +360,67 @@ bsa_status_t bsa_linear_forward(const bsa_linear_t* p, const void* x, const void
 bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const void* w, const void* pre, const void* dy,
                                  void* dx, void* dw, void* db, void* ws, size_t ws_bytes, void* stream);
 
+/* Gated map: [g | u] = x w^T + bias, y = act(g) u, with x [m, k], w [2 n, k] (the n rows of the gate's map, then
+ * those of the other), bias [2 n], y [m, n]. Products as the affine map's. */
+typedef struct {
+  int64_t m;                            /* rows, 0 .. 2^31 - 256                        */
+  int32_t k, n;                         /* input and output channels, 1 .. 2^24 and 2^23; x, y
+                                           and w have fewer than 2^24 tiles of 128 x 128 */
+  int32_t dtype;                        /* bsa_dtype_t of every tensor                  */
+  int32_t act;                          /* bsa_act_t                                    */
+  int64_t ld_x, ld_w, ld_y, ld_dy;      /* elements between rows (0: packed)            */
+} bsa_gated_t;
+
+/* Validate p and report the workspaces (pointers may be NULL). */
+bsa_status_t bsa_gated_sizes(const bsa_gated_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes);
+
+/* bias and pre may be NULL. pre [m, 2 n] packed receives [g | u] for the backward, rounded to dtype. */
+bsa_status_t bsa_gated_forward(const bsa_gated_t* p, const void* x, const void* w, const void* bias, void* y, void* pre,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* With dz = [dy u act'(g) | dy act(g)]: dx = dz w [m, k], dw = dz^T x [2 n, k], db = sum of dz over the rows
+ * [2 n], all dtype, packed and overwritten; each may be NULL (not formed). pre: as filled by the forward.
+ * dz is rounded to dtype where it enters the products (not in db). */
+bsa_status_t bsa_gated_backward(const bsa_gated_t* p, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                                void* dw, void* db, void* ws, size_t ws_bytes, void* stream);
+
+/* Rotary positions of queries q [rows, heads, head_dim] and keys k [rows, kv_heads, head_dim], with the norm of
+ * each head in the same pass. With a gain [head_dim] (float32) n = x / sqrt(mean(x^2) + eps) gain, without (NULL)
+ * n = x. The first rot values of a head are rot / 2 pairs: (i, i + rot / 2), or with interleaved (2 i, 2 i + 1); pair
+ * i turns by t = position * freq[i], y = magnitude (n_a cos t - n_b sin t, n_a sin t + n_b cos t). The rest of
+ * n passes. positions [rows, axes]: axis a turns the pairs [a, a + 1) (rot / 2) / axes. Angles are formed and
+ * reduced in 64 bits (meant for |t| < 2^31), cosines and sines are float32, off by 2^-23 at most. */
+typedef enum { BSA_POS_I32 = 0, BSA_POS_F32 = 1 } bsa_pos_t;
+typedef struct {
+  int64_t rows;                         /* 0 .. 2^40                                    */
+  int32_t heads, kv_heads;              /* >= 1; kv_heads 0: no keys (their pointers are not read) */
+  int32_t head_dim;                     /* 2 .. 256                                     */
+  int32_t rot;                          /* even, 2 .. head_dim                          */
+  int32_t axes;                         /* 1 .. 4, divides rot / 2                      */
+  int32_t pos_type;                     /* bsa_pos_t                                    */
+  int32_t interleaved;                  /* 0 or 1                                       */
+  int32_t dtype;                        /* bsa_dtype_t of q, k, y and their gradients   */
+  float eps;                            /* > 0 (read with a gain)                       */
+  float magnitude;                      /* finite, > 0                                  */
+  /* elements between rows and between heads; both 0: packed. o: the outputs (y, or in the backward
+   * the gradients of q and k); d: dy */
+  int64_t q_row, q_head, k_row, k_head, oq_row, oq_head, ok_row, ok_head, dq_row, dq_head, dk_row, dk_head;
+} bsa_rotary_t;
+
+/* Validate p and report the backward workspace (ws_bwd_bytes may be NULL). */
+bsa_status_t bsa_rotary_sizes(const bsa_rotary_t* p, size_t* ws_bwd_bytes);
+
+/* freq [rot / 2] float64. y_q may be q and y_k may be k (same strides). */
+bsa_status_t bsa_rotary_forward(const bsa_rotary_t* p, const void* q, const void* k, const void* positions, const double* freq,
+                                const float* gain_q, const float* gain_k, void* y_q, void* y_k, void* stream);
+
+/* dq and dk (dtype), dgain_q and dgain_k [head_dim] float32 (each may be NULL: not formed), given dy_q and dy_k. q is
+ * read only with gain_q, k only with gain_k (else they may be NULL), as they were before the forward. dq may
+ * be dy_q or q, dk may be dy_k or k (same strides). */
+bsa_status_t bsa_rotary_backward(const bsa_rotary_t* p, const void* q, const void* k, const void* positions, const double* freq,
+                                 const float* gain_q, const float* gain_k, const void* dy_q, const void* dy_k, void* dq,
+                                 void* dk, float* dgain_q, float* dgain_k, void* ws, size_t ws_bytes, void* stream);
+
 /* Full attention over packed sequences with grouped heads. Sequence s has the query rows
  * [cu_q[s], cu_q[s+1]) and the key rows [cu_k[s], cu_k[s] + l), l = used_k[s] (a cache that is
  * filled so far) or, with used_k NULL, cu_k[s+1] - cu_k[s]. Query head h reads key head
@@ -406,6 +468,44 @@ bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, con
                                     const int32_t* cu_k, const int32_t* used_k, void* dq, void* dk, void* dv, void* ws,
                                     size_t ws_bytes, void* stream);
 
+/* Cache of 8 bits. A cache holds keys, and values, as e4m3 bytes [total_k, kv_heads, head_dim] and an exponent
+ * code for each row and key head [kv_heads, total_k]: a byte stands for its e4m3 value times 2^(code - 127). A row
+ * of a head is written with the smallest exponent code - 127 in [-64, 63] at which its largest magnitude is at
+ * most 448 times the scale (values past 448 2^63 are cut to it), each value rounded to nearest even, which is
+ * the only rounding. Infinities and NaN are written as NaN and take no part in the scale.
+ * Sequence s owns the cache rows [cu_k[s], cu_k[s+1]), of which the first l = used_k[s] are in use (NULL: all).
+ * Its n = cu_q[s+1] - cu_q[s] rows of k and v [rows, kv_heads, head_dim] are the last n of those l; rows that would
+ * lie before the sequence's first are not written, and are read as 0. The arrays of offsets are as
+ * bsa_attention_forward takes them. */
+typedef struct {
+  int32_t seqs;                         /* 1 .. 2^24                                    */
+  int32_t kv_heads;                     /* 1 .. 65535                                   */
+  int32_t head_dim;                     /* 32, 64 or 128                                */
+  int32_t dtype;                        /* bsa_dtype_t of k and v                       */
+  int64_t rows, total_k;                /* rows of k and v, and of the cache; <= 2^30   */
+  /* elements between rows and between heads of k and v, bytes between those of the cache's keys (ck) and
+   * values (cv); multiples of 16 bytes, like the tensors' addresses; both 0: packed */
+  int64_t k_row, k_head, v_row, v_head, ck_row, ck_head, cv_row, cv_head;
+} bsa_cache_t;
+
+/* New rows into the cache. exp_k and exp_v: the exponent codes. */
+bsa_status_t bsa_cache_write(const bsa_cache_t* p, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k,
+                             const int32_t* used_k, void* cache_k, void* cache_v, uint8_t* exp_k, uint8_t* exp_v, void* stream);
+
+/* Rows back from the cache: the values their bytes stand for, exactly; rows in no sequence are 0. */
+bsa_status_t bsa_cache_read(const bsa_cache_t* p, const void* cache_k, const void* cache_v, const uint8_t* exp_k,
+                            const uint8_t* exp_v, const int32_t* cu_q, const int32_t* cu_k, const int32_t* used_k, void* k,
+                            void* v, void* stream);
+
+/* bsa_attention_forward with the cache for k and v: o = softmax(scale q K^T) V with the values that the bytes stand
+ * for. Everything else is as there, p's k and v strides being those of the cache in bytes; there is no backward.
+ * bf16 queries: probabilities are rounded to bf16 where they enter the product with V. float32 queries, and their
+ * probabilities, enter the products as three bf16 parts (within 2^-24 of themselves). */
+bsa_status_t bsa_cache_attention_sizes(const bsa_attention_t* p, size_t* ws_bytes);
+bsa_status_t bsa_cache_attention_forward(const bsa_attention_t* p, const void* q, const void* cache_k, const void* cache_v,
+                                         const uint8_t* exp_k, const uint8_t* exp_v, const int32_t* cu_q, const int32_t* cu_k,
+                                         const int32_t* used_k, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- Measurement support (not part of the layer's computation) ---- */
 
 /* on = 1: start recording, clearing earlier records; on = 0: stop and clear. While on,
@@ -415,7 +515,8 @@ bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, con
  * "bwd.dq_slc", "bwd.kv_ball", "bwd.kv_cmp", "bwd.mlp", "bwd.slc_csr", "bwd.slc_kv", and
  * for the block "blk.norm", "blk.gemm" (activation products), "blk.wgrad" (weight
  * gradients), "blk.elem" (SwiGLU, casts, layout changes). Each dense operator's call is one
- * phase: "norm.fwd", "norm.bwd", "linear.fwd", "linear.bwd", "attn.fwd", "attn.bwd".
+ * phase: "norm.fwd", "norm.bwd", "linear.fwd", "linear.bwd", "gated.fwd", "gated.bwd",
+ * "rotary.fwd", "rotary.bwd", "attn.fwd", "attn.bwd", "cache.write", "cache.read", "cache.attn".
  * Host-side bookkeeping only; no device memory is allocated. */
 bsa_status_t bsa_timing_enable(int32_t on);
 

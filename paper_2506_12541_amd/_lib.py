@@ -12,6 +12,7 @@ LIB_PATH = os.path.join(HERE, "libbsa.so")
 
 BSA_OK, BSA_ERR_INVALID_ARGUMENT, BSA_ERR_UNSUPPORTED, BSA_ERR_WORKSPACE_TOO_SMALL, BSA_ERR_HIP = range(5)
 BSA_F32, BSA_BF16 = 0, 1
+BSA_POS_I32, BSA_POS_F32 = 0, 1
 BSA_POOL_MLP, BSA_POOL_MEAN = 0, 1
 BSA_QC_MEAN, BSA_QC_MLP = 0, 1
 
@@ -76,6 +77,25 @@ class bsa_attention_t(C.Structure):
                                  "do_row", "do_head")]
 
 
+class bsa_gated_t(C.Structure):
+    _fields_ = [("m", C.c_int64), ("k", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32)] + [
+        (n, C.c_int64) for n in ("ld_x", "ld_w", "ld_y", "ld_dy")]
+
+
+class bsa_rotary_t(C.Structure):
+    _fields_ = [("rows", C.c_int64)] + [(n, C.c_int32) for n in ("heads", "kv_heads", "head_dim", "rot", "axes", "pos_type",
+                                                                 "interleaved", "dtype")] + [
+        ("eps", C.c_float), ("magnitude", C.c_float)] + [
+        (n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "oq_row", "oq_head", "ok_row", "ok_head",
+                                 "dq_row", "dq_head", "dk_row", "dk_head")]
+
+
+class bsa_cache_t(C.Structure):
+    _fields_ = [("seqs", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)] + [
+        (n, C.c_int64) for n in ("rows", "total_k", "k_row", "k_head", "v_row", "v_head", "ck_row", "ck_head",
+                                 "cv_row", "cv_head")]
+
+
 _SIGS = {
     "bsa_status_string": (C.c_char_p, [C.c_int]),
     "bsa_last_error": (C.c_char_p, []),
@@ -119,6 +139,16 @@ _SIGS = {
     "bsa_linear_sizes": (C.c_int, [C.POINTER(bsa_linear_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "bsa_linear_forward": (C.c_int, [C.POINTER(bsa_linear_t)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]),
     "bsa_linear_backward": (C.c_int, [C.POINTER(bsa_linear_t)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "bsa_gated_sizes": (C.c_int, [C.POINTER(bsa_gated_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "bsa_gated_forward": (C.c_int, [C.POINTER(bsa_gated_t)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]),
+    "bsa_gated_backward": (C.c_int, [C.POINTER(bsa_gated_t)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "bsa_rotary_sizes": (C.c_int, [C.POINTER(bsa_rotary_t), C.POINTER(C.c_size_t)]),
+    "bsa_rotary_forward": (C.c_int, [C.POINTER(bsa_rotary_t)] + [C.c_void_p] * 9),
+    "bsa_rotary_backward": (C.c_int, [C.POINTER(bsa_rotary_t)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]),
+    "bsa_cache_write": (C.c_int, [C.POINTER(bsa_cache_t)] + [C.c_void_p] * 10),
+    "bsa_cache_read": (C.c_int, [C.POINTER(bsa_cache_t)] + [C.c_void_p] * 10),
+    "bsa_cache_attention_sizes": (C.c_int, [C.POINTER(bsa_attention_t), C.POINTER(C.c_size_t)]),
+    "bsa_cache_attention_forward": (C.c_int, [C.POINTER(bsa_attention_t)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]),
     "bsa_attention_sizes": (C.c_int, [C.POINTER(bsa_attention_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "bsa_attention_forward": (C.c_int, [C.POINTER(bsa_attention_t)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]),
     "bsa_attention_backward": (C.c_int, [C.POINTER(bsa_attention_t)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]),

@@ -80,6 +80,91 @@ bsa_status_t check(const bsa_linear_t* p, bsa::LinearArgs* a) {
   return BSA_OK;
 }
 
+bsa_status_t check(const bsa_gated_t* p, bsa::GatedArgs* a) {
+  if (!p) return bad("params is NULL");
+  if (p->n < 1) return bad("k and n must be >= 1");
+  if (p->n > (1 << 23)) return set_error(BSA_ERR_UNSUPPORTED, "n must be <= 2^23");
+  if (p->act < BSA_ACT_NONE || p->act > BSA_ACT_SILU) return bad("bad act");
+  if (!ld_ok(p->ld_y, p->n) || !ld_ok(p->ld_dy, p->n)) return bad("leading dimensions must be 0 or at least the row's length");
+  // its products are those of a map to 2 n channels
+  const bsa_linear_t both{p->m, p->k, 2 * p->n, p->dtype, BSA_ACT_NONE, p->ld_x, p->ld_w, 0, 0, 0};
+  bsa::LinearArgs l;
+  const bsa_status_t s = check(&both, &l);
+  if (s != BSA_OK) return s;
+  *a = bsa::GatedArgs{p->m, p->k, p->n, l.bf16, p->act, l.ldx, l.ldw, ld_of(p->ld_y, p->n), ld_of(p->ld_dy, p->n)};
+  return BSA_OK;
+}
+
+// Strides of a [rows, heads, cols] tensor: both 0 is packed; whole multiples of `unit`.
+bool strides_ok(long long* row, long long* head, int heads, int cols, int unit) {
+  if (*row == 0 && *head == 0) {
+    *head = cols;
+    *row = (long long)heads * cols;
+  }
+  return *row >= 0 && *head >= 0 && *row % unit == 0 && *head % unit == 0;
+}
+// An output's rows and heads do not overlap.
+bool apart(long long rows, long long row, int heads, long long head, int cols) {
+  const long long all_rows = (rows - 1) * row + cols, all_heads = (heads - 1) * head + cols;
+  return ((heads == 1 || head >= cols) && (rows <= 1 || row >= all_heads)) ||
+         ((rows <= 1 || row >= cols) && (heads == 1 || head >= all_rows));
+}
+// An output may be the input itself where their strides are one.
+bool on_other_strides(const void* out, long long row, long long head, const void* in, long long in_row, long long in_head) {
+  return out && out == in && (row != in_row || head != in_head);
+}
+
+bsa_status_t check(const bsa_rotary_t* p, bsa::RotaryArgs* a) {
+  if (!p) return bad("params is NULL");
+  if (p->rows < 0 || p->rows > ((int64_t)1 << 40)) return bad("rows must be in [0, 2^40]");
+  if (p->heads < 1 || p->kv_heads < 0) return bad("heads must be >= 1 and kv_heads >= 0");
+  if (p->heads > 65535 || p->kv_heads > 65535) return set_error(BSA_ERR_UNSUPPORTED, "heads must be <= 65535");
+  if (p->head_dim < 2) return bad("head_dim must be >= 2");
+  if (p->head_dim > bsa::kRotMaxDim) return set_error(BSA_ERR_UNSUPPORTED, "head_dim must be <= 256");
+  if (p->rot < 2 || p->rot > p->head_dim || p->rot % 2 != 0) return bad("rot must be even and in [2, head_dim]");
+  if (p->axes < 1 || p->axes > 4 || p->rot / 2 % p->axes != 0) return bad("axes must be in [1, 4] and divide rot / 2");
+  if (p->pos_type != BSA_POS_I32 && p->pos_type != BSA_POS_F32) return bad("bad pos_type");
+  if (p->interleaved != 0 && p->interleaved != 1) return bad("interleaved must be 0/1");
+  if (!dtype_ok(p->dtype)) return bad("bad dtype");
+  if (!(p->eps > 0.0f) || std::isinf(p->eps)) return bad("eps must be finite and > 0");
+  if (!(p->magnitude > 0.0f) || std::isinf(p->magnitude)) return bad("magnitude must be finite and > 0");
+  *a = bsa::RotaryArgs{p->rows, p->heads, p->kv_heads, p->head_dim, p->rot, p->axes, p->pos_type == BSA_POS_F32,
+                       p->interleaved != 0, p->dtype == BSA_BF16, p->eps, p->magnitude,
+                       p->q_row, p->q_head, p->k_row, p->k_head, p->oq_row, p->oq_head, p->ok_row, p->ok_head,
+                       p->dq_row, p->dq_head, p->dk_row, p->dk_head};
+  const struct { long long *row, *head; int heads; } st[6] = {{&a->q_row, &a->q_head, p->heads},   {&a->k_row, &a->k_head, p->kv_heads},
+                                                              {&a->oq_row, &a->oq_head, p->heads}, {&a->ok_row, &a->ok_head, p->kv_heads},
+                                                              {&a->dq_row, &a->dq_head, p->heads}, {&a->dk_row, &a->dk_head, p->kv_heads}};
+  for (const auto& t : st)
+    if (!strides_ok(t.row, t.head, t.heads, p->head_dim, 1)) return bad("strides must be >= 0");
+  if (!apart(p->rows, a->oq_row, p->heads, a->oq_head, p->head_dim) ||
+      (p->kv_heads && !apart(p->rows, a->ok_row, p->kv_heads, a->ok_head, p->head_dim)))
+    return bad("an output's rows and heads may not overlap");
+  return BSA_OK;
+}
+
+bsa_status_t check(const bsa_cache_t* p, bsa::CacheArgs* a) {
+  if (!p) return bad("params is NULL");
+  if (p->seqs < 1) return bad("seqs must be >= 1");
+  if (p->kv_heads < 1) return bad("kv_heads must be >= 1");
+  if (p->kv_heads > 65535 || p->seqs > (1 << 24)) return set_error(BSA_ERR_UNSUPPORTED, "kv_heads must be <= 65535, seqs <= 2^24");
+  if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128)
+    return set_error(BSA_ERR_UNSUPPORTED, "head_dim must be 32, 64 or 128");
+  if (p->rows < 0 || p->total_k < 0) return bad("rows and total_k must be >= 0");
+  if (p->rows > ((int64_t)1 << 30) || p->total_k > ((int64_t)1 << 30))
+    return set_error(BSA_ERR_UNSUPPORTED, "rows and total_k must be <= 2^30");
+  if (!dtype_ok(p->dtype)) return bad("bad dtype");
+  *a = bsa::CacheArgs{p->seqs, p->kv_heads, p->head_dim, p->rows, p->total_k, p->dtype == BSA_BF16, p->k_row, p->k_head,
+                      p->v_row, p->v_head, p->ck_row, p->ck_head, p->cv_row, p->cv_head};
+  const int e = p->dtype == BSA_BF16 ? 8 : 4;   // elements of 16 bytes
+  if (!strides_ok(&a->k_row, &a->k_head, p->kv_heads, p->head_dim, e) || !strides_ok(&a->v_row, &a->v_head, p->kv_heads, p->head_dim, e) ||
+      !strides_ok(&a->ck_row, &a->ck_head, p->kv_heads, p->head_dim, 16) || !strides_ok(&a->cv_row, &a->cv_head, p->kv_heads, p->head_dim, 16))
+    return bad("strides must be >= 0 and multiples of 16 bytes");
+  if (!apart(p->total_k, a->ck_row, p->kv_heads, a->ck_head, p->head_dim) || !apart(p->total_k, a->cv_row, p->kv_heads, a->cv_head, p->head_dim))
+    return bad("the cache's rows and heads may not overlap");
+  return BSA_OK;
+}
+
 bsa_status_t check(const bsa_attention_t* p, bsa::AttnArgs* a) {
   if (!p) return bad("params is NULL");
   if (p->seqs < 1) return bad("seqs must be >= 1");
@@ -105,15 +190,19 @@ bsa_status_t check(const bsa_attention_t* p, bsa::AttnArgs* a) {
                                                               {&a->v_row, &a->v_head, p->kv_heads},
                                                               {&a->o_row, &a->o_head, p->heads},
                                                               {&a->do_row, &a->do_head, p->heads}};
-  for (const auto& s : st) {
-    if (*s.row == 0 && *s.head == 0) {
-      *s.head = p->head_dim;
-      *s.row = (long long)s.heads * p->head_dim;
-    }
-    if (*s.row < 0 || *s.head < 0 || *s.row % e != 0 || *s.head % e != 0)
-      return bad("strides must be >= 0 and multiples of 16 bytes");
-  }
+  for (const auto& s : st)
+    if (!strides_ok(s.row, s.head, s.heads, p->head_dim, e)) return bad("strides must be >= 0 and multiples of 16 bytes");
   return BSA_OK;
+}
+
+// The strides of k and v are bytes of the cache.
+bsa_status_t check_cache(const bsa_attention_t* p, bsa::AttnArgs* a) {
+  const bsa_status_t s = check(p, a);
+  if (s != BSA_OK) return s;
+  a->k_row = p->k_row, a->k_head = p->k_head, a->v_row = p->v_row, a->v_head = p->v_head;
+  if (!strides_ok(&a->k_row, &a->k_head, a->kv_heads, a->hd, 16) || !strides_ok(&a->v_row, &a->v_head, a->kv_heads, a->hd, 16))
+    return bad("strides of the cache must be multiples of 16 bytes");
+  return s;
 }
 
 }  // namespace
@@ -218,6 +307,116 @@ bsa_status_t bsa_linear_backward(const bsa_linear_t* p, const void* x, const voi
   });
 }
 
+bsa_status_t bsa_gated_sizes(const bsa_gated_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes) {
+  return entry([&] {
+    bsa::GatedArgs a;
+    const bsa_status_t s = check(p, &a);
+    if (s != BSA_OK) return s;
+    if (ws_fwd_bytes) *ws_fwd_bytes = bsa::gated_fwd_ws_bytes(a);
+    if (ws_bwd_bytes) *ws_bwd_bytes = bsa::gated_bwd_ws_bytes(a);
+    return s;
+  });
+}
+
+bsa_status_t bsa_gated_forward(const bsa_gated_t* p, const void* x, const void* w, const void* bias, void* y, void* pre,
+                               void* ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    bsa::GatedArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK || a.m == 0) return s;
+    if (!x || !w || !y) return bad("x, w and y must be non-NULL");
+    if (on_one(y, {x, w, bias, pre})) return bad("y may not alias x, w, bias or pre");
+    if (on_one(pre, {x, w, bias})) return bad("pre may not alias an input");
+    const size_t need = bsa::gated_fwd_ws_bytes(a);
+    if (need && (!ws || ws_bytes < need)) return small_ws("gated map forward", need);
+    hipError_t e;
+    BSA_PHASE("gated.fwd", (hipStream_t)stream, e = bsa::launch_gated_fwd(a, x, w, bias, y, pre, ws, (hipStream_t)stream));
+    return launched(e, "bsa_gated_forward");
+  });
+}
+
+bsa_status_t bsa_gated_backward(const bsa_gated_t* p, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                                void* dw, void* db, void* ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    bsa::GatedArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK) return s;
+    if (!dx && !dw && !db) return BSA_OK;
+    if (a.m > 0) {
+      if (!dy || !pre) return bad("dy and pre must be non-NULL");
+      if (dx && !w) return bad("w must be non-NULL for dx");
+      if (dw && !x) return bad("x must be non-NULL for dw");
+    }
+    for (const void* g : {dx, dw, db})
+      if (on_one(g, {x, w, pre, dy})) return bad("a gradient may not alias an input");
+    const size_t need = bsa::gated_bwd_ws_bytes(a);
+    if (need && (!ws || ws_bytes < need)) return small_ws("gated map backward", need);
+    hipError_t e;
+    BSA_PHASE("gated.bwd", (hipStream_t)stream,
+              e = bsa::launch_gated_bwd(a, x, w, pre, dy, dx, dw, db, ws, (hipStream_t)stream));
+    return launched(e, "bsa_gated_backward");
+  });
+}
+
+bsa_status_t bsa_rotary_sizes(const bsa_rotary_t* p, size_t* ws_bwd_bytes) {
+  return entry([&] {
+    bsa::RotaryArgs a;
+    const bsa_status_t s = check(p, &a);
+    if (s == BSA_OK && ws_bwd_bytes) *ws_bwd_bytes = bsa::rotary_bwd_ws_bytes(a);
+    return s;
+  });
+}
+
+bsa_status_t bsa_rotary_forward(const bsa_rotary_t* p, const void* q, const void* k, const void* positions, const double* freq,
+                                const float* gain_q, const float* gain_k, void* y_q, void* y_k, void* stream) {
+  return entry([&] {
+    bsa::RotaryArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK || a.rows == 0) return s;
+    if (!q || !positions || !freq || !y_q) return bad("q, positions, freq and y_q must be non-NULL");
+    if (a.kv_heads && (!k || !y_k)) return bad("k and y_k must be non-NULL with key heads");
+    if (y_q == y_k || (a.kv_heads && (y_q == k || y_k == q))) return bad("y_q and y_k may only be q and k");
+    if (on_other_strides(y_q, a.oq_row, a.oq_head, q, a.q_row, a.q_head) ||
+        on_other_strides(y_k, a.ok_row, a.ok_head, k, a.k_row, a.k_head))
+      return bad("an output may be its input only with the same strides");
+    hipError_t e;
+    BSA_PHASE("rotary.fwd", (hipStream_t)stream,
+              e = bsa::launch_rotary_fwd(a, q, k, positions, freq, gain_q, gain_k, y_q, y_k, (hipStream_t)stream));
+    return launched(e, "bsa_rotary_forward");
+  });
+}
+
+bsa_status_t bsa_rotary_backward(const bsa_rotary_t* p, const void* q, const void* k, const void* positions, const double* freq,
+                                 const float* gain_q, const float* gain_k, const void* dy_q, const void* dy_k, void* dq,
+                                 void* dk, float* dgain_q, float* dgain_k, void* ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    bsa::RotaryArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK) return s;
+    if (a.kv_heads == 0) k = dy_k = gain_k = nullptr, dk = dgain_k = nullptr;
+    if ((dgain_q && !gain_q) || (dgain_k && !gain_k)) return bad("a gain's gradient needs the gain");
+    if (a.rows > 0) {
+      if (!positions || !freq || !dy_q || !dq) return bad("positions, freq, dy_q and dq must be non-NULL");
+      if (a.kv_heads && (!dy_k || !dk)) return bad("dy_k and dk must be non-NULL with key heads");
+      if ((gain_q && !q) || (gain_k && !k)) return bad("q and k must be non-NULL with their gains");
+      if (dq == dk || (a.kv_heads && (dq == k || dq == dy_k || dk == q || dk == dy_q)))
+        return bad("dq may only be q or dy_q, dk only k or dy_k");
+      if (on_other_strides(dq, a.oq_row, a.oq_head, gain_q ? q : nullptr, a.q_row, a.q_head) ||
+          on_other_strides(dq, a.oq_row, a.oq_head, dy_q, a.dq_row, a.dq_head) ||
+          on_other_strides(dk, a.ok_row, a.ok_head, gain_k ? k : nullptr, a.k_row, a.k_head) ||
+          on_other_strides(dk, a.ok_row, a.ok_head, dy_k, a.dk_row, a.dk_head))
+        return bad("a gradient may be an input only with the same strides");
+    }
+    const size_t need = gain_q || gain_k ? bsa::rotary_bwd_ws_bytes(a) : 0;
+    if (need && (!ws || ws_bytes < need)) return small_ws("rotary backward", need);
+    hipError_t e;
+    BSA_PHASE("rotary.bwd", (hipStream_t)stream,
+              e = bsa::launch_rotary_bwd(a, q, k, positions, freq, gain_q, gain_k, dy_q, dy_k, dq, dk, dgain_q, dgain_k, ws,
+                                         (hipStream_t)stream));
+    return launched(e, "bsa_rotary_backward");
+  });
+}
+
 bsa_status_t bsa_attention_sizes(const bsa_attention_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes) {
   return entry([&] {
     bsa::AttnArgs a;
@@ -240,10 +439,7 @@ bsa_status_t bsa_attention_forward(const bsa_attention_t* p, const void* q, cons
     if (!q || !cu_q || !cu_k || !o || !lse) return bad("q, cu_q, cu_k, o and lse must be non-NULL");
     if (a.total_k > 0 && (!k || !v)) return bad("k and v must be non-NULL");
     if (o == q || o == k || o == v) return bad("o may not alias an input");
-    const long long d = a.hd, rows = (a.total_q - 1) * a.o_row + d, heads = (a.heads - 1) * a.o_head + d;
-    if (!((a.heads == 1 || a.o_head >= d) && (a.total_q == 1 || a.o_row >= heads)) &&
-        !((a.total_q == 1 || a.o_row >= d) && (a.heads == 1 || a.o_head >= rows)))
-      return bad("o's rows and heads may not overlap");
+    if (!apart(a.total_q, a.o_row, a.heads, a.o_head, a.hd)) return bad("o's rows and heads may not overlap");
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16))
       return bad("q, k, v and o must be 16-byte aligned");
     const size_t need = bsa::attention_fwd_ws_bytes(a);
@@ -279,6 +475,78 @@ bsa_status_t bsa_attention_backward(const bsa_attention_t* p, const void* q, con
     BSA_PHASE("attn.bwd", (hipStream_t)stream,
               e = bsa::launch_attention_bwd(a, q, k, v, o, lse, d_o, cu_q, cu_k, used_k, dq, dk, dv, ws, (hipStream_t)stream));
     return launched(e, "bsa_attention_backward");
+  });
+}
+
+bsa_status_t bsa_cache_write(const bsa_cache_t* p, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_k,
+                             const int32_t* used_k, void* cache_k, void* cache_v, uint8_t* exp_k, uint8_t* exp_v, void* stream) {
+  return entry([&] {
+    bsa::CacheArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK || a.rows == 0 || a.total_k == 0) return s;
+    if (!k || !v || !cu_q || !cu_k || !cache_k || !cache_v || !exp_k || !exp_v) return bad("every pointer but used_k must be non-NULL");
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache_k, 16) || !aligned(cache_v, 16))
+      return bad("k, v and the cache must be 16-byte aligned");
+    if (on_one(cache_k, {k, v, cache_v}) || on_one(cache_v, {k, v}) || exp_k == exp_v) return bad("the cache may not alias an input or itself");
+    hipError_t e;
+    BSA_PHASE("cache.write", (hipStream_t)stream,
+              e = bsa::launch_cache_write(a, k, v, cu_q, cu_k, used_k, cache_k, cache_v, exp_k, exp_v, (hipStream_t)stream));
+    return launched(e, "bsa_cache_write");
+  });
+}
+
+bsa_status_t bsa_cache_read(const bsa_cache_t* p, const void* cache_k, const void* cache_v, const uint8_t* exp_k,
+                            const uint8_t* exp_v, const int32_t* cu_q, const int32_t* cu_k, const int32_t* used_k, void* k,
+                            void* v, void* stream) {
+  return entry([&] {
+    bsa::CacheArgs a;
+    bsa_status_t s = check(p, &a);
+    if (s != BSA_OK || a.rows == 0) return s;
+    if (!k || !v || !cu_q || !cu_k) return bad("k, v, cu_q and cu_k must be non-NULL");
+    if (a.total_k > 0 && (!cache_k || !cache_v || !exp_k || !exp_v)) return bad("the cache must be non-NULL");
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache_k, 16) || !aligned(cache_v, 16))
+      return bad("k, v and the cache must be 16-byte aligned");
+    if (on_one(k, {cache_k, cache_v, v}) || on_one(v, {cache_k, cache_v})) return bad("k and v may not alias the cache or each other");
+    if (!apart(a.rows, a.k_row, a.kv_heads, a.k_head, a.hd) || !apart(a.rows, a.v_row, a.kv_heads, a.v_head, a.hd))
+      return bad("rows and heads of k and v may not overlap");
+    hipError_t e;
+    BSA_PHASE("cache.read", (hipStream_t)stream,
+              e = bsa::launch_cache_read(a, cache_k, cache_v, exp_k, exp_v, cu_q, cu_k, used_k, k, v, (hipStream_t)stream));
+    return launched(e, "bsa_cache_read");
+  });
+}
+
+bsa_status_t bsa_cache_attention_sizes(const bsa_attention_t* p, size_t* ws_bytes) {
+  return entry([&] {
+    bsa::AttnArgs a;
+    const bsa_status_t s = check_cache(p, &a);
+    if (s == BSA_OK && ws_bytes) *ws_bytes = bsa::cache_attention_ws_bytes(a);
+    return s;
+  });
+}
+
+bsa_status_t bsa_cache_attention_forward(const bsa_attention_t* p, const void* q, const void* cache_k, const void* cache_v,
+                                         const uint8_t* exp_k, const uint8_t* exp_v, const int32_t* cu_q, const int32_t* cu_k,
+                                         const int32_t* used_k, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    bsa::AttnArgs a;
+    bsa_status_t s = check_cache(p, &a);
+    if (s != BSA_OK || a.total_q == 0) return s;
+    if (!bsa::cache_attention_fits(a)) return set_error(BSA_ERR_UNSUPPORTED, kTooManyTiles);
+    if (!q || !cu_q || !cu_k || !o || !lse) return bad("q, cu_q, cu_k, o and lse must be non-NULL");
+    if (a.total_k > 0 && (!cache_k || !cache_v || !exp_k || !exp_v)) return bad("the cache must be non-NULL");
+    if (on_one(o, {q, cache_k, cache_v})) return bad("o may not alias an input");
+    if (!apart(a.total_q, a.o_row, a.heads, a.o_head, a.hd)) return bad("o's rows and heads may not overlap");
+    if (!aligned(q, 16) || !aligned(cache_k, 16) || !aligned(cache_v, 16) || !aligned(o, 16))
+      return bad("q, the cache and o must be 16-byte aligned");
+    const size_t need = bsa::cache_attention_ws_bytes(a);
+    if (need && (!ws || ws_bytes < need)) return small_ws("cache attention", need);
+    if (need && !aligned(ws, 16)) return bad("ws must be 16-byte aligned");
+    hipError_t e;
+    BSA_PHASE("cache.attn", (hipStream_t)stream,
+              e = bsa::launch_cache_attention(a, q, cache_k, cache_v, exp_k, exp_v, cu_q, cu_k, used_k, o, lse, ws,
+                                              (hipStream_t)stream));
+    return launched(e, "bsa_cache_attention_forward");
   });
 }
 
