@@ -31,6 +31,24 @@ _CODES = {torch.bfloat16: BSA_BF16, torch.float32: BSA_F32}
 _HERE = contextlib.nullcontext()
 
 
+# Parameter records of calls whose arguments have passed the checks, by all that the checks read of them (shapes, strides,
+# types, devices, numbers; never addresses or values). The calls of a serving step are as short on the GPU as their
+# host path is long: with it a rotary_forward of 32 tokens takes 8 us of the host, without 14.
+_checked = {}
+
+
+def _remember(key, record):
+    if len(_checked) >= 4096:      # shapes that keep changing: start over
+        _checked.clear()
+    _checked[key] = record
+    return record
+
+
+def _fresh(t):
+    """A contiguous tensor of t's shape, type and device."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -359,20 +377,34 @@ def rotary_forward(q, k, positions, freq, gain_q=None, gain_k=None, eps: float =
     or float32, or [rows, axes] with each axis turning its own run of the pairs. Strided views of a fused
     projection are fine. Returns (y_q, y_k), which may be given: q and k themselves too."""
     lib = _lib.load()
-    p = _rotary_params(q, k, positions, freq, gain_q, gain_k, eps, interleaved, magnitude)
-    dev, dt = q.device, q.dtype
-    p.q_row, p.q_head = _any_heads(q, "q", dt, dev)
-    if k is not None:
-        p.k_row, p.k_head = _any_heads(k, "k", dt, dev)
-    elif y_k is not None:
-        raise ValueError("y_k needs k")
-    if y_q is not None:
-        p.oq_row, p.oq_head = _any_heads(y_q, "y_q", dt, dev, q.shape)
-    if y_k is not None:
-        p.ok_row, p.ok_head = _any_heads(y_k, "y_k", dt, dev, k.shape)
+    try:
+        key = ("rotary_forward", q.shape, q.stride(), q.dtype, q.device,
+               None if k is None else (k.shape, k.stride(), k.dtype, k.device), positions.shape, positions.stride(),
+               positions.dtype, positions.device, freq.shape, freq.stride(), freq.dtype, freq.device,
+               None if gain_q is None else (gain_q.shape, gain_q.stride(), gain_q.dtype, gain_q.device),
+               None if gain_k is None else (gain_k.shape, gain_k.stride(), gain_k.dtype, gain_k.device), eps, interleaved,
+               magnitude, None if y_q is None else (y_q.shape, y_q.stride(), y_q.dtype, y_q.device),
+               None if y_k is None else (y_k.shape, y_k.stride(), y_k.dtype, y_k.device))
+        p = _checked.get(key)
+    except (AttributeError, TypeError):      # no tensors: the checks say so
+        key = p = None
+    if p is None:
+        p = _rotary_params(q, k, positions, freq, gain_q, gain_k, eps, interleaved, magnitude)
+        dev, dt = q.device, q.dtype
+        p.q_row, p.q_head = _any_heads(q, "q", dt, dev)
+        if k is not None:
+            p.k_row, p.k_head = _any_heads(k, "k", dt, dev)
+        elif y_k is not None:
+            raise ValueError("y_k needs k")
+        if y_q is not None:
+            p.oq_row, p.oq_head = _any_heads(y_q, "y_q", dt, dev, q.shape)
+        if y_k is not None:
+            p.ok_row, p.ok_head = _any_heads(y_k, "y_k", dt, dev, k.shape)
+        _remember(key, p)
+    dev = q.device
     with _on(dev, stream):
-        y_q = torch.empty(q.shape, dtype=dt, device=dev) if y_q is None else y_q
-        y_k = torch.empty(k.shape, dtype=dt, device=dev) if y_k is None and k is not None else y_k
+        y_q = _fresh(q) if y_q is None else y_q
+        y_k = _fresh(k) if y_k is None and k is not None else y_k
         check(lib.bsa_rotary_forward(C.byref(p), q.data_ptr(), _ptr(k), positions.data_ptr(), freq.data_ptr(), _ptr(gain_q),
                                      _ptr(gain_k), y_q.data_ptr(), _ptr(y_k), _queue(dev)), "bsa_rotary_forward")
     return y_q, y_k
@@ -563,6 +595,17 @@ def _cache_strides(cache, dev):
     return ck + cv
 
 
+def _cache_key(cache):
+    k, v, ke, ve = cache
+    return (k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device, ke.shape, ke.stride(), ke.dtype,
+            ke.device, ve.shape, ve.stride(), ve.dtype, ve.device)
+
+
+def _offsets_key(cu_q, cu_k, used_k):
+    return (cu_q.shape, cu_q.stride(), cu_q.dtype, cu_q.device, cu_k.shape, cu_k.stride(), cu_k.dtype, cu_k.device,
+            None if used_k is None else (used_k.shape, used_k.stride(), used_k.dtype, used_k.device))
+
+
 def _offsets(cu_q, cu_k, used_k, dev):
     _tensor(cu_q, "cu_q", torch.int32, dev)
     if cu_q.dim() != 1 or cu_q.numel() < 2 or not cu_q.is_contiguous():
@@ -579,15 +622,23 @@ def cache_write(cache, k, v, cu_q, cu_k, used_k=None, stream=None):
     last of the used_k[s] rows in use behind its first row cu_k[s] (used_k None: of all up to cu_k[s+1]), where
     cache_attention_forward with the same offsets finds them. Other rows keep what they held."""
     lib = _lib.load()
-    k_row, k_head = _heads(k, "k")
-    dev, dt = k.device, k.dtype
-    v_row, v_head = _heads(v, "v", dt, dev, k.shape)
-    strides = _cache_strides(cache, dev)
-    rows, kv, d = cache.k.shape
-    if k.shape[1:] != cache.k.shape[1:]:
-        raise ValueError(f"k must have {kv} heads of {d}, got {tuple(k.shape)}")
-    p = _lib.bsa_cache_t(_offsets(cu_q, cu_k, used_k, dev), kv, d, _CODES[dt], k.shape[0], rows, k_row, k_head, v_row, v_head,
-                         *strides)
+    try:
+        key = ("cache_write", k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device, _cache_key(cache),
+               _offsets_key(cu_q, cu_k, used_k))
+        p = _checked.get(key)
+    except (AttributeError, TypeError):
+        key = p = None
+    if p is None:
+        k_row, k_head = _heads(k, "k")
+        dev, dt = k.device, k.dtype
+        v_row, v_head = _heads(v, "v", dt, dev, k.shape)
+        strides = _cache_strides(cache, dev)
+        rows, kv, d = cache.k.shape
+        if k.shape[1:] != cache.k.shape[1:]:
+            raise ValueError(f"k must have {kv} heads of {d}, got {tuple(k.shape)}")
+        p = _remember(key, _lib.bsa_cache_t(_offsets(cu_q, cu_k, used_k, dev), kv, d, _CODES[dt], k.shape[0], rows, k_row,
+                                            k_head, v_row, v_head, *strides))
+    dev = k.device
     with _on(dev, stream):
         check(lib.bsa_cache_write(C.byref(p), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(used_k),
                                   cache.k.data_ptr(), cache.v.data_ptr(), cache.k_exp.data_ptr(), cache.v_exp.data_ptr(),
@@ -599,17 +650,25 @@ def cache_read(cache, rows: int, cu_q, cu_k, used_k=None, dtype=torch.bfloat16, 
     (bfloat16 or float32; exact in both). Rows in no sequence are 0. With cu_q the running sum of used_k: all that
     the caches hold."""
     lib = _lib.load()
-    if dtype not in _CODES:
-        raise ValueError(f"dtype must be bfloat16 or float32, got {dtype}")
-    if rows < 0:
-        raise ValueError("rows must be >= 0")
-    _tensor(cache.k, "cache.k", torch.float8_e4m3fn)
+    try:
+        key = ("cache_read", rows, dtype, _cache_key(cache), _offsets_key(cu_q, cu_k, used_k))
+        p = _checked.get(key)
+    except (AttributeError, TypeError):
+        key = p = None
+    if p is None:
+        if dtype not in _CODES:
+            raise ValueError(f"dtype must be bfloat16 or float32, got {dtype}")
+        if rows < 0:
+            raise ValueError("rows must be >= 0")
+        _tensor(cache.k, "cache.k", torch.float8_e4m3fn)
+        dev = cache.k.device
+        strides = _cache_strides(cache, dev)
+        total, kv, d = cache.k.shape
+        p = _remember(key, _lib.bsa_cache_t(_offsets(cu_q, cu_k, used_k, dev), kv, d, _CODES[dtype], rows, total, 0, 0, 0, 0,
+                                            *strides))
     dev = cache.k.device
-    strides = _cache_strides(cache, dev)
-    total, kv, d = cache.k.shape
-    p = _lib.bsa_cache_t(_offsets(cu_q, cu_k, used_k, dev), kv, d, _CODES[dtype], rows, total, 0, 0, 0, 0, *strides)
     with _on(dev, stream):
-        k = torch.empty((rows, kv, d), dtype=dtype, device=dev)
+        k = torch.empty((rows, p.kv_heads, p.head_dim), dtype=dtype, device=dev)
         v = torch.empty_like(k)
         check(lib.bsa_cache_read(C.byref(p), cache.k.data_ptr(), cache.v.data_ptr(), cache.k_exp.data_ptr(),
                                  cache.v_exp.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _ptr(used_k), k.data_ptr(),
@@ -623,27 +682,38 @@ def cache_attention_forward(q, cache, cu_q, cu_k, used_k=None, causal: bool = Fa
     lib = _lib.load()
     if (o is None) != (lse is None):
         raise ValueError("pass both o and lse, or neither")
-    q_row, q_head = _heads(q, "q")
-    dev, dt = q.device, q.dtype
-    tq, h, d = q.shape
-    strides = _cache_strides(cache, dev)
-    rows, kv, _ = cache.k.shape
-    if cache.k.shape[2] != d or kv == 0:
-        raise ValueError(f"the cache must have head_dim {d} and at least one head, got {tuple(cache.k.shape)}")
-    p = _lib.bsa_attention_t(_offsets(cu_q, cu_k, used_k, dev), h, kv, d, tq, rows, int(bool(causal)), _CODES[dt],
-                             softmax_scale, int(o is None), q_row, q_head, *strides, 0, 0, 0, 0)
-    if o is not None:
-        p.o_row, p.o_head = _heads(o, "o", dt, dev, q.shape)
-        _shaped(lse, "lse", (h, tq), torch.float32, dev)
-    need = C.c_size_t()
-    check(lib.bsa_cache_attention_sizes(C.byref(p), C.byref(need)), "bsa_cache_attention_sizes")
+    try:
+        key = ("cache_attention_forward", q.shape, q.stride(), q.dtype, q.device, _cache_key(cache),
+               _offsets_key(cu_q, cu_k, used_k), causal, softmax_scale,
+               None if o is None else (o.shape, o.stride(), o.dtype, o.device, lse.shape, lse.stride(), lse.dtype, lse.device))
+        record = _checked.get(key)
+    except (AttributeError, TypeError):
+        key = record = None
+    if record is None:
+        q_row, q_head = _heads(q, "q")
+        dev, dt = q.device, q.dtype
+        tq, h, d = q.shape
+        strides = _cache_strides(cache, dev)
+        rows, kv, _ = cache.k.shape
+        if cache.k.shape[2] != d or kv == 0:
+            raise ValueError(f"the cache must have head_dim {d} and at least one head, got {tuple(cache.k.shape)}")
+        p = _lib.bsa_attention_t(_offsets(cu_q, cu_k, used_k, dev), h, kv, d, tq, rows, int(bool(causal)), _CODES[dt],
+                                 softmax_scale, int(o is None), q_row, q_head, *strides, 0, 0, 0, 0)
+        if o is not None:
+            p.o_row, p.o_head = _heads(o, "o", dt, dev, q.shape)
+            _shaped(lse, "lse", (h, tq), torch.float32, dev)
+        need = C.c_size_t()
+        check(lib.bsa_cache_attention_sizes(C.byref(p), C.byref(need)), "bsa_cache_attention_sizes")
+        record = _remember(key, (p, need.value))
+    p, need = record
+    dev = q.device
     with _on(dev, stream):
-        ws = _workspace(need.value, dev)
+        ws = _workspace(need, dev)
         if o is None:
-            o = torch.empty(q.shape, dtype=dt, device=dev)
-            lse = torch.empty((h, tq), dtype=torch.float32, device=dev)
+            o = _fresh(q)
+            lse = torch.empty((p.heads, p.total_q), dtype=torch.float32, device=dev)
         check(lib.bsa_cache_attention_forward(C.byref(p), q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(),
                                               cache.k_exp.data_ptr(), cache.v_exp.data_ptr(), cu_q.data_ptr(),
-                                              cu_k.data_ptr(), _ptr(used_k), o.data_ptr(), lse.data_ptr(), _ptr(ws),
-                                              need.value, _queue(dev)), "bsa_cache_attention_forward")
+                                              cu_k.data_ptr(), _ptr(used_k), o.data_ptr(), lse.data_ptr(), _ptr(ws), need,
+                                              _queue(dev)), "bsa_cache_attention_forward")
     return o, lse
