@@ -44,6 +44,10 @@ def _remember(key, record):
     return record
 
 
+def _signature(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
+
+
 def _fresh(t):
     """A contiguous tensor of t's shape, type and device."""
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
@@ -377,14 +381,10 @@ def rotary_forward(q, k, positions, freq, gain_q=None, gain_k=None, eps: float =
     or float32, or [rows, axes] with each axis turning its own run of the pairs. Strided views of a fused
     projection are fine. Returns (y_q, y_k), which may be given: q and k themselves too."""
     lib = _lib.load()
+    sig = _signature
     try:
-        key = ("rotary_forward", q.shape, q.stride(), q.dtype, q.device,
-               None if k is None else (k.shape, k.stride(), k.dtype, k.device), positions.shape, positions.stride(),
-               positions.dtype, positions.device, freq.shape, freq.stride(), freq.dtype, freq.device,
-               None if gain_q is None else (gain_q.shape, gain_q.stride(), gain_q.dtype, gain_q.device),
-               None if gain_k is None else (gain_k.shape, gain_k.stride(), gain_k.dtype, gain_k.device), eps, interleaved,
-               magnitude, None if y_q is None else (y_q.shape, y_q.stride(), y_q.dtype, y_q.device),
-               None if y_k is None else (y_k.shape, y_k.stride(), y_k.dtype, y_k.device))
+        key = ("rotary_forward", sig(q), sig(k), sig(positions), sig(freq), sig(gain_q), sig(gain_k), eps, interleaved,
+               magnitude, sig(y_q), sig(y_k))
         p = _checked.get(key)
     except (AttributeError, TypeError):      # no tensors: the checks say so
         key = p = None
@@ -416,38 +416,49 @@ def rotary_backward(dy_q, dy_k, positions, freq, q=None, k=None, gain_q=None, ga
     the forward is needed with gain_q (gain_k). dq and dk may be given: views of a fused gradient, or dy_q and
     dy_k themselves."""
     lib = _lib.load()
-    p = _rotary_params(dy_q, dy_k, positions, freq, gain_q, gain_k, eps, interleaved, magnitude)
-    dev, dt = dy_q.device, dy_q.dtype
-    p.dq_row, p.dq_head = _any_heads(dy_q, "dy_q", dt, dev)
-    if dy_k is not None:
-        p.dk_row, p.dk_head = _any_heads(dy_k, "dy_k", dt, dev)
-    elif dk is not None:
-        raise ValueError("dk needs dy_k")
-    if gain_q is not None:
-        if q is None:
-            raise ValueError("q is needed with gain_q")
-        p.q_row, p.q_head = _any_heads(q, "q", dt, dev, dy_q.shape)
-    if gain_k is not None:
-        if k is None:
-            raise ValueError("k is needed with gain_k")
-        p.k_row, p.k_head = _any_heads(k, "k", dt, dev, dy_k.shape)
-    if dq is not None:
-        p.oq_row, p.oq_head = _any_heads(dq, "dq", dt, dev, dy_q.shape)
-    if dk is not None:
-        p.ok_row, p.ok_head = _any_heads(dk, "dk", dt, dev, dy_k.shape)
-    need = C.c_size_t()
-    if gain_q is not None or gain_k is not None:
-        check(lib.bsa_rotary_sizes(C.byref(p), C.byref(need)), "bsa_rotary_sizes")
+    sig = _signature
+    try:
+        key = ("rotary_backward", sig(dy_q), sig(dy_k), sig(positions), sig(freq), sig(q), sig(k), sig(gain_q), sig(gain_k), eps,
+               interleaved, magnitude, sig(dq), sig(dk))
+        record = _checked.get(key)
+    except (AttributeError, TypeError, ValueError):
+        key = record = None
+    if record is None:
+        p = _rotary_params(dy_q, dy_k, positions, freq, gain_q, gain_k, eps, interleaved, magnitude)
+        dev, dt = dy_q.device, dy_q.dtype
+        p.dq_row, p.dq_head = _any_heads(dy_q, "dy_q", dt, dev)
+        if dy_k is not None:
+            p.dk_row, p.dk_head = _any_heads(dy_k, "dy_k", dt, dev)
+        elif dk is not None:
+            raise ValueError("dk needs dy_k")
+        if gain_q is not None:
+            if q is None:
+                raise ValueError("q is needed with gain_q")
+            p.q_row, p.q_head = _any_heads(q, "q", dt, dev, dy_q.shape)
+        if gain_k is not None:
+            if k is None:
+                raise ValueError("k is needed with gain_k")
+            p.k_row, p.k_head = _any_heads(k, "k", dt, dev, dy_k.shape)
+        if dq is not None:
+            p.oq_row, p.oq_head = _any_heads(dq, "dq", dt, dev, dy_q.shape)
+        if dk is not None:
+            p.ok_row, p.ok_head = _any_heads(dk, "dk", dt, dev, dy_k.shape)
+        need = C.c_size_t()
+        if gain_q is not None or gain_k is not None:
+            check(lib.bsa_rotary_sizes(C.byref(p), C.byref(need)), "bsa_rotary_sizes")
+        record = _remember(key, (p, need.value))
+    p, need = record
+    dev = dy_q.device
     with _on(dev, stream):
-        ws = _workspace(need.value, dev)
-        dq = torch.empty(dy_q.shape, dtype=dt, device=dev) if dq is None else dq
-        dk = torch.empty(dy_k.shape, dtype=dt, device=dev) if dk is None and dy_k is not None else dk
+        ws = _workspace(need, dev)
+        dq = _fresh(dy_q) if dq is None else dq
+        dk = _fresh(dy_k) if dk is None and dy_k is not None else dk
         dgain_q = None if gain_q is None else torch.empty_like(gain_q)
         dgain_k = None if gain_k is None else torch.empty_like(gain_k)
         check(lib.bsa_rotary_backward(C.byref(p), None if gain_q is None else q.data_ptr(),
                                       None if gain_k is None else k.data_ptr(), positions.data_ptr(), freq.data_ptr(),
                                       _ptr(gain_q), _ptr(gain_k), dy_q.data_ptr(), _ptr(dy_k), dq.data_ptr(), _ptr(dk),
-                                      _ptr(dgain_q), _ptr(dgain_k), _ptr(ws), need.value, _queue(dev)),
+                                      _ptr(dgain_q), _ptr(dgain_k), _ptr(ws), need, _queue(dev)),
               "bsa_rotary_backward")
     return dict(dq=dq, dk=dk, dgain_q=dgain_q, dgain_k=dgain_k)
 
@@ -595,17 +606,6 @@ def _cache_strides(cache, dev):
     return ck + cv
 
 
-def _cache_key(cache):
-    k, v, ke, ve = cache
-    return (k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device, ke.shape, ke.stride(), ke.dtype,
-            ke.device, ve.shape, ve.stride(), ve.dtype, ve.device)
-
-
-def _offsets_key(cu_q, cu_k, used_k):
-    return (cu_q.shape, cu_q.stride(), cu_q.dtype, cu_q.device, cu_k.shape, cu_k.stride(), cu_k.dtype, cu_k.device,
-            None if used_k is None else (used_k.shape, used_k.stride(), used_k.dtype, used_k.device))
-
-
 def _offsets(cu_q, cu_k, used_k, dev):
     _tensor(cu_q, "cu_q", torch.int32, dev)
     if cu_q.dim() != 1 or cu_q.numel() < 2 or not cu_q.is_contiguous():
@@ -617,16 +617,21 @@ def _offsets(cu_q, cu_k, used_k, dev):
     return seqs
 
 
+def _call_key(name, cache, cu_q, cu_k, used_k, *more):
+    sig = _signature
+    k, v, k_exp, v_exp = cache
+    return name, sig(k), sig(v), sig(k_exp), sig(v_exp), sig(cu_q), sig(cu_k), sig(used_k), more
+
+
 def cache_write(cache, k, v, cu_q, cu_k, used_k=None, stream=None):
     """Quantises new rows k, v [rows, kv_heads, d] into the cache: those of sequence s, [cu_q[s], cu_q[s+1]), become the
     last of the used_k[s] rows in use behind its first row cu_k[s] (used_k None: of all up to cu_k[s+1]), where
     cache_attention_forward with the same offsets finds them. Other rows keep what they held."""
     lib = _lib.load()
     try:
-        key = ("cache_write", k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device, _cache_key(cache),
-               _offsets_key(cu_q, cu_k, used_k))
+        key = _call_key("cache_write", cache, cu_q, cu_k, used_k, _signature(k), _signature(v))
         p = _checked.get(key)
-    except (AttributeError, TypeError):
+    except (AttributeError, TypeError, ValueError):
         key = p = None
     if p is None:
         k_row, k_head = _heads(k, "k")
@@ -651,9 +656,9 @@ def cache_read(cache, rows: int, cu_q, cu_k, used_k=None, dtype=torch.bfloat16, 
     the caches hold."""
     lib = _lib.load()
     try:
-        key = ("cache_read", rows, dtype, _cache_key(cache), _offsets_key(cu_q, cu_k, used_k))
+        key = _call_key("cache_read", cache, cu_q, cu_k, used_k, rows, dtype)
         p = _checked.get(key)
-    except (AttributeError, TypeError):
+    except (AttributeError, TypeError, ValueError):
         key = p = None
     if p is None:
         if dtype not in _CODES:
@@ -683,11 +688,10 @@ def cache_attention_forward(q, cache, cu_q, cu_k, used_k=None, causal: bool = Fa
     if (o is None) != (lse is None):
         raise ValueError("pass both o and lse, or neither")
     try:
-        key = ("cache_attention_forward", q.shape, q.stride(), q.dtype, q.device, _cache_key(cache),
-               _offsets_key(cu_q, cu_k, used_k), causal, softmax_scale,
-               None if o is None else (o.shape, o.stride(), o.dtype, o.device, lse.shape, lse.stride(), lse.dtype, lse.device))
+        key = _call_key("cache_attention_forward", cache, cu_q, cu_k, used_k, _signature(q), causal, softmax_scale, _signature(o),
+                        _signature(lse))
         record = _checked.get(key)
-    except (AttributeError, TypeError):
+    except (AttributeError, TypeError, ValueError):
         key = record = None
     if record is None:
         q_row, q_head = _heads(q, "q")
