@@ -3,7 +3,8 @@
 //   db = sum dz.
 // The forward is one product whose workgroups hold the same columns of both maps, so g and u meet in
 // registers (dense_product.hpp) and only y is written (and, for the backward, [g | u]). The backward's two
-// products are the affine map's over the 2n columns of dz.
+// products are the affine map's over the 2n columns of dz. float32 operands of large products are split into
+// their bf16 parts once, in a pass before (planes, below).
 // Bound by the matrix cores from a few hundred rows on, below by the weight's bytes.
 #include "dense_product.hpp"
 
@@ -66,6 +67,282 @@ __global__ void __launch_bounds__(256) gated_dz_kernel(const T* __restrict__ dy,
   }
 }
 
+// ---- float32: operands split into their parts once ----
+//
+// A float32 value enters a product as three bf16 parts (dense_product.hpp). Formed in the product's tiles, the parts
+// of a value are formed again for every tile of the other side; with 64 x 64 tiles, which odd middle sizes end up with,
+// that takes longer than multiplying. Here a pass before writes them as three bf16 matrices ("planes", [3][rows][cols], both
+// rounded up to 32 with zeros, so that no tile of the contraction is partial), and the product loads its tiles
+// straight into LDS. A value past the largest bf16 is cut there and its rest is in the other parts; infinities, whose
+// parts would meet zeros, are noted (flags) and send every tile through parts_plain.
+
+constexpr long long up32(long long x) { return (x + 31) / 32 * 32; }
+
+__device__ __forceinline__ void split3(float x, bf16_t (&p)[3], bool& inf) {
+  const float top = 3.3895314e38f;     // the largest bf16 value
+  const bool endless = fabsf(x) == __builtin_huge_valf();
+  inf |= endless;
+  float x1 = bf2f(f2bf(x));
+  if (fabsf(x1) > top && !endless) x1 = copysignf(top, x);
+  const float r = endless ? 0.f : x - x1, x2 = bf2f(f2bf(r));
+  p[0] = f2bf(x1);
+  p[1] = f2bf(x2);
+  p[2] = f2bf(r - x2);
+}
+
+struct Planes {
+  const float* src;
+  long long ld, rows;
+  int cols;
+  bf16_t* to;          // [3][up32(rows)][up32(cols)]
+  int* flags;          // one for each workgroup: it met an infinity
+};
+constexpr int kSplitBlocks = 512;
+
+// Two matrices (blockIdx.y), four columns to a thread.
+__global__ void __launch_bounds__(256) split_planes_kernel(Planes p0, Planes p1) {
+  const Planes p = blockIdx.y ? p1 : p0;
+  const long long R = up32(p.rows), plane = R * up32(p.cols);
+  const int C4 = (int)(up32(p.cols) / 4);
+  bool inf = false;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < R * C4; i += 256LL * kSplitBlocks) {
+    const long long r = i / C4;
+    const int c = (int)(i - r * C4) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < p.rows) {
+      const float* s = p.src + r * p.ld + c;
+      if (c + 4 <= p.cols) {
+        load4u(s, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (c + e < p.cols) v[e] = s[e];
+      }
+    }
+    bf16_t q[4][3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split3(v[e], q[e], inf);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      *reinterpret_cast<ushort4*>(p.to + k * plane + r * 4 * C4 + c) = make_ushort4(q[0][k], q[1][k], q[2][k], q[3][k]);
+  }
+  const int any = __syncthreads_or(inf);
+  if (threadIdx.x == 0) p.flags[blockIdx.x] = any;
+}
+
+// A matrix of planes: Mat of the first, elements to the next.
+struct PlaneMat {
+  Mat<bf16_t> m;
+  long long plane;
+  __device__ __forceinline__ float at(long long r, long long c) const {
+    const bf16_t* p = m.p + r * m.ld + c;
+    return bf2f(p[0]) + (bf2f(p[plane]) + bf2f(p[2 * plane]));
+  }
+};
+
+// Accumulators of a wave tile by f32 matrix instructions from the sums of the parts, which are the values.
+template <bool TA, bool TB, bool G, int FI, int FJ>
+__device__ __forceinline__ void parts_plain(const PlaneMat& a, const PlaneMat& b, long long m0, long long n0, long long k0,
+                                            long long k1, int lane, f32x4 (&acc)[FI][FJ]) {
+  const int r = lane & 15, j = lane >> 4;
+  auto at = [](const PlaneMat& m, bool tr, long long o, long long k) {
+    const bool in = tr ? o < m.m.cols : o < m.m.rows;
+    return in ? (tr ? m.at(k, o) : m.at(o, k)) : 0.f;
+  };
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int jj = 0; jj < FJ; ++jj) acc[i][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (long long k = k0; k < k1; k += 4) {     // k1 - k0: a multiple of 32
+    float x[FI], y[FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i) x[i] = at(a, TA, m0 + 16 * i + r, k + j);
+#pragma unroll
+    for (int i = 0; i < FJ; ++i) y[i] = at(b, TB, stored_row<G>(b.m, n0 + 16 * i + r), k + j);
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int jj = 0; jj < FJ; ++jj) acc[i][jj] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[jj], x[i], acc[i][jj], 0, 0, 0);
+  }
+}
+
+// 128 x 128 tiles of 2 x 4 waves, contraction tiles of 32 in a ring of three LDS stages of 48 KB: one workgroup to a CU,
+// two waves to a SIMD (4 waves of 64 x 64 read less from LDS, but nothing runs while one waits).
+template <bool TA, bool TB, bool G>
+__global__ void __launch_bounds__(512) parts_kernel(PlaneMat a, PlaneMat b, int nkt, int ntm, int ntn, int kt_per,
+                                                       const int* fa, int nfa, const int* fb, int nfb, Epi<float> o) {
+  constexpr int BT = 128, BK = 32, FI = 4, FJ = 2, TILE = BT * BK;
+  // a stage is an array of its own: reads of one stage do not wait for loads into another
+  __shared__ __attribute__((aligned(1024))) bf16_t st0[2][3][TILE], st1[2][3][TILE], st2[2][3][TILE];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wid >> 2, wn = wid & 3;
+  // XCDs take contiguous runs of tiles, in bands of 8 tile rows walked column by column (product_dma_kernel)
+  const int nt = ntm * ntn;
+  int id = blockIdx.x;
+  if ((nt & 7) == 0) id = (id & 7) * (nt >> 3) + (id >> 3);
+  const int band = id / (8 * ntn), in = id - band * 8 * ntn, bh = min(8, ntm - 8 * band);
+  const int tm = 8 * band + in % bh, tn = in / bh;
+  const long long m0 = (long long)tm * BT, n0 = (long long)tn * BT;
+  const int kt0 = min((int)blockIdx.y * kt_per, nkt), kt1 = min(kt0 + kt_per, nkt);
+  DmaTile<TA, TA != TB, TA ? BK : BT, TA ? BT : BK, 8> la;
+  DmaTile<TB, TA != TB, TB ? BK : BT, TB ? BT : BK, 8, G> lb;
+  la.init(a.m, m0, wid, lane);
+  lb.init(b.m, n0, wid, lane);
+  constexpr int PER = 3 * (decltype(la)::NU + decltype(lb)::NU);
+  typedef bf16_t Stage[2][3][TILE];
+  auto issue = [&](int kt, Stage& st, int k) __attribute__((always_inline)) {
+    la.issue(st[0][k], a.m, (long long)kt * BK, wid, 2 * k * a.plane);
+    lb.issue(st[1][k], b.m, (long long)kt * BK, wid, 2 * k * b.plane);
+  };
+  f32x4 acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 af[3][FI], bf[3][FJ];
+  auto read_a = [&](const Stage& st, int k) __attribute__((always_inline)) {
+    Frags<TA, TA != TB, BK, BT, FI>::read(st[0][k], wm * 64, 0, lane, af[k]);
+  };
+  auto read_b = [&](const Stage& st, int k) __attribute__((always_inline)) {
+    Frags<TB, TA != TB, BK, BT, FJ>::read(st[1][k], wn * 32, 0, lane, bf[k]);
+  };
+  auto multiply = [&](int ka, int kb) {
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bf[kb][j], af[ka][i], acc[i][j]);
+  };
+  // tile t lies in stage c; the one before c is free
+  auto step = [&](int t, const Stage& c, Stage& free) __attribute__((always_inline)) {
+    // tile t has landed once at most the tile issued after it is in flight
+    if (t + 1 < kt1)
+      vm_wait<PER>();
+    else
+      vm_drain();
+    lds_barrier();     // every wave's loads of tile t are visible, and it has its fragments of t - 1
+    // the small part products first; the next loads between the products, so that no wave queues for all of them
+    const bool more = t + 2 < kt1;
+    read_a(c, 2);
+    read_b(c, 0);
+    multiply(2, 0);
+    if (more) issue(t + 2, free, 0);
+    read_a(c, 0);
+    read_b(c, 2);
+    multiply(0, 2);
+    if (more) issue(t + 2, free, 1);
+    read_a(c, 1);
+    read_b(c, 1);
+    multiply(1, 1);
+    if (more) issue(t + 2, free, 2);
+    multiply(1, 0);
+    multiply(0, 1);
+    multiply(0, 0);
+    lgkm_drain();
+  };
+  for (int u = 0; u < 2; ++u)
+    if (kt0 + u < kt1)
+      for (int k = 0; k < 3; ++k) issue(kt0 + u, u ? st1 : st0, k);
+  for (int kt = kt0; kt < kt1; kt += 3) {
+    step(kt, st0, st2);
+    if (kt + 1 < kt1) step(kt + 1, st1, st0);
+    if (kt + 2 < kt1) step(kt + 2, st2, st1);
+  }
+  int odd = 0;
+  for (int i = threadIdx.x; i < nfa; i += 512) odd |= fa[i];
+  for (int i = threadIdx.x; i < nfb; i += 512) odd |= fb[i];
+  if (__syncthreads_or(odd))
+    parts_plain<TA, TB, G, FI, FJ>(a, b, m0 + wm * 64, n0 + wn * 32, (long long)kt0 * BK, (long long)kt1 * BK, lane, acc);
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {
+    const long long m = m0 + wm * 64 + 16 * i + (lane & 15);
+#pragma unroll
+    for (int j = 0; j < FJ; j += G ? 2 : 1) {
+      const int n = (int)n0 + wn * 32 + 16 * j + 4 * (lane >> 4);
+      float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+      if constexpr (G) {
+        float u[4] = {acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
+        gated_store4(o, m, gated_col(n), v, u, blockIdx.y);
+      } else {
+        epi_store4(o, m, n, v, blockIdx.y);
+      }
+    }
+  }
+}
+
+// dz as planes [3][up32(m)][up32(2n)] and its partial column sums; otherwise as gated_dz_kernel. The last
+// workgroups also clear the rows and columns behind dz. flags: one for each workgroup.
+__global__ void __launch_bounds__(256) gated_dz_planes_kernel(const float* __restrict__ dy, long long lddy,
+                                                              const float* __restrict__ pre, int act, long long m, int n,
+                                                              long long rpg, bf16_t* __restrict__ dz, float* __restrict__ part,
+                                                              int* __restrict__ flags) {
+  __shared__ float red[8][2][132];
+  const long long R = up32(m), C = up32(2LL * n), plane = R * C;
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5, c = (blockIdx.x * 32 + cx) * 4;
+  const long long r0 = blockIdx.y * rpg, r1 = r0 + rpg < m ? r0 + rpg : m;
+  bool inf = false;
+  float s[2][4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[0][e] = s[1][e] = 0.f;
+  if (c < n) {
+    const Mat<float> my{dy, lddy, m, n}, mg{pre, 2LL * n, m, n}, mu{pre + n, 2LL * n, m, n};
+#pragma unroll 2
+    for (long long r = r0 + ry; r < r1; r += 8) {
+      float y[4], v[2][4];
+      unpack16<float>(load_piece(my, r, c), y);
+      unpack16<float>(load_piece(mg, r, c), v[0]);
+      unpack16<float>(load_piece(mu, r, c), v[1]);
+      bf16_t q[2][4][3];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = v[0][e];
+        const float dg = y[e] * v[1][e] * act_slope<float>(z, act), du = y[e] * act_fwd<float>(z, act);
+        s[0][e] += dg;
+        s[1][e] += du;
+        split3(dg, q[0][e], inf);
+        split3(du, q[1][e], inf);
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16_t* const p = dz + k * plane + r * C + h * n + c;
+          const ushort4 w = make_ushort4(q[h][0][k], q[h][1][k], q[h][2][k], q[h][3][k]);
+          if (c + 4 <= n) {
+            __builtin_memcpy(p, &w, 8);
+          } else {
+            p[0] = w.x;
+            if (c + 1 < n) p[1] = w.y;
+            if (c + 2 < n) p[2] = w.z;
+          }
+        }
+    }
+  }
+  if (blockIdx.x == 0) {       // the columns behind, of this workgroup's rows
+    const int w = (int)(C - 2 * n);
+    for (long long i = threadIdx.x; i < (r1 - r0) * w; i += 256)
+      for (int k = 0; k < 3; ++k) dz[k * plane + (r0 + i / w) * C + 2 * n + i % w] = 0;
+  }
+  if (blockIdx.y == gridDim.y - 1) {   // the rows behind
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < (R - m) * C; i += 256LL * gridDim.x)
+      for (int k = 0; k < 3; ++k) dz[k * plane + m * C + i] = 0;
+  }
+  const int any = __syncthreads_or(inf);
+  if (threadIdx.x == 0) flags[blockIdx.y * gridDim.x + blockIdx.x] = any;
+  if (!part) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[ry][h][cx * 4 + e] = s[h][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 256; i += 256) {
+    const int h = i / 128, x = i % 128;
+    float v = red[0][h][x];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += red[k][h][x];
+    const int col = blockIdx.x * 128 + x;
+    if (col < n) part[(long long)blockIdx.y * 2 * n + h * n + col] = v;
+  }
+}
+
 // ---- host ----
 
 // The forward's product has 2n columns.
@@ -73,10 +350,35 @@ Plan fwd_plan(const GatedArgs& a) { return plan_product(a.bf16, a.m, 2 * a.n, a.
 
 LinearArgs rows_of(const GatedArgs& a) { return LinearArgs{a.m, a.k, 2 * a.n, a.bf16, kActNone, a.ldx, a.ldw, 0, 0, 2LL * a.n}; }
 
+// Whether float32 products go through planes: where both sides of a product have several tiles that share them, and
+// the forward's one product is long enough for the pass before it. us (forward, backward) by planes and without:
+// 3586 x 515 -> 2 x 1029: 66, 168 and 78, 260; 2000 x 2048 -> 2 x 2048: 195, 385 and 218, 503; 1000 x 8192 -> 2 x 600: 152, 265 and
+// 178, 357; 1024 x 1024 -> 2 x 1024: 40, 84 and 38, 99; 2048 x 512 -> 2 x 1024: 38, 87 and 33, 101; 300 x 4096 -> 2 x 4096: 218,
+// 378 and 176, 436; 20000 x 256 -> 2 x 256: 56, 134 and 60, 129; 65536 x 64 -> 2 x 1024: 275, 728 and 313, 677.
+bool bwd_planes(const GatedArgs& a) {
+  return !a.bf16 && a.m >= 768 && a.n >= 512 && a.k >= 256 && a.k <= (1 << 22) && a.n <= (1 << 21);
+}
+bool fwd_planes(const GatedArgs& a) { return bwd_planes(a) && a.m * a.n >= (3LL << 29) / a.k; }
+size_t planes_bytes(long long rows, long long cols) { return align256(3 * sizeof(bf16_t) * (size_t)(up32(rows) * up32(cols))); }
+
+// Splits of the contraction: as many as end first, in units of 0.1 us, at 1.2 us a tile of 128 x 128 x 32 on each of 256
+// CUs, 4 us a workgroup, and the splits' sums written and read at 4 TB/s behind another launch of 4 us.
+int planes_splits(long long M, long long N, long long K, int outs) {
+  const long long tiles = (M + 127) / 128 * ((N * outs + 127) / 128), nkt = (K + 31) / 32;
+  long long best = 0, pick = 1;
+  for (long long S = 1; S <= 16 && S <= nkt; ++S) {
+    const long long t = (tiles * S + 255) / 256 * ((nkt + S - 1) / S * 12 + 40) + (S > 1 ? 40 + S * M * N * outs / 50000 : 0);
+    if (S == 1 || t < best) best = t, pick = S;
+  }
+  return (int)pick;
+}
+
 struct GatedBwdWs {
   size_t dz, dbp, rest, total;
+  size_t w, x, flags;        // planes of w and x, and the flags of w, x and dz
   int P;
   long long rpg;
+  int Sx, Sw;                // splits of dx and dw
 };
 GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
   GatedBwdWs L{};
@@ -90,11 +392,111 @@ GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
   L.P = (int)(L.rpg ? (a.m + L.rpg - 1) / L.rpg : 1);
   size_t off = 0;
   auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
-  L.dz = put(esz * (size_t)a.m * 2 * a.n);
   L.dbp = put(sizeof(float) * (size_t)L.P * 2 * a.n);
-  L.rest = put(linear_bwd_ws_bytes(rows_of(a)));
+  if (bwd_planes(a)) {
+    L.dz = put(planes_bytes(a.m, 2LL * a.n));
+    L.w = put(planes_bytes(2LL * a.n, a.k));
+    L.x = put(planes_bytes(a.m, a.k));
+    L.flags = put(sizeof(int) * (2 * kSplitBlocks + (size_t)gx * L.P));
+    L.Sx = planes_splits(a.m, a.k, 2LL * a.n, 1);
+    L.Sw = planes_splits(2LL * a.n, a.k, a.m, 1);
+    auto part = [](int S, long long M, long long N) { return S > 1 ? sizeof(float) * (size_t)S * M * N : 0; };
+    L.rest = put(std::max(part(L.Sx, a.m, a.k), part(L.Sw, 2LL * a.n, a.k)));
+  } else {
+    L.dz = put(esz * (size_t)a.m * 2 * a.n);
+    L.rest = put(linear_bwd_ws_bytes(rows_of(a)));
+  }
   L.total = off;
   return L;
+}
+
+Planes planes_of(const float* src, long long ld, long long rows, int cols, void* to, int* flags) {
+  return Planes{src, ld, rows, cols, (bf16_t*)to, flags};
+}
+// The planes as an operand. In column form the zeros behind a row are columns of it.
+PlaneMat plane_mat(const void* p, long long rows, long long cols, bool column) {
+  const long long C = up32(cols), R = up32(rows);
+  return PlaneMat{Mat<bf16_t>{(const bf16_t*)p, C, column ? R : rows, (int)C}, R * C};
+}
+
+// C = A B^T of planes; S > 1: partial sums in part, joined by split_sum_kernel
+template <bool TA, bool TB, bool G>
+hipError_t parts_product(const PlaneMat& a, const PlaneMat& b, long long M, int N, long long K, int S, float* part, const int* fa,
+                         int nfa, const int* fb, int nfb, Epi<float> o, hipStream_t st) {
+  o.part = S > 1 ? part : nullptr;
+  const int nkt = (int)(up32(K) / 32), ntm = (int)((M + 127) / 128), ntn = G ? (N + 63) / 64 : (N + 127) / 128;
+  parts_kernel<TA, TB, G><<<dim3((unsigned)((long long)ntm * ntn), (unsigned)S), 512, 0, st>>>(a, b, nkt, ntm, ntn, (nkt + S - 1) / S,
+                                                                                               fa, nfa, fb, nfb, o);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || S == 1) return e;
+  o.part = nullptr;
+  const long long n4 = M * ((N + 3) / 4);
+  split_sum_kernel<float, G ? 2 : 1><<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(part, S, o);
+  return hipGetLastError();
+}
+
+struct GatedFwdWs {
+  size_t x, w, flags, part, total;
+  int S;
+};
+GatedFwdWs gated_fwd_layout(const GatedArgs& a) {
+  GatedFwdWs L{};
+  size_t off = 0;
+  auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
+  if (fwd_planes(a)) {
+    L.S = planes_splits(a.m, a.n, a.k, 2);
+    L.x = put(planes_bytes(a.m, a.k));
+    L.w = put(planes_bytes(2LL * a.n, a.k));
+    L.flags = put(sizeof(int) * 2 * kSplitBlocks);
+    L.part = put(L.S > 1 ? sizeof(float) * (size_t)L.S * a.m * 2 * a.n : 0);
+  } else if (!few_rows_ok(a.m, a.k)) {
+    L.part = put(plan_bytes(fwd_plan(a), a.m, 2LL * a.n));
+  }
+  L.total = off;
+  return L;
+}
+
+hipError_t split_two(const Planes& p, const Planes& q, hipStream_t st) {
+  split_planes_kernel<<<dim3(kSplitBlocks, 2), 256, 0, st>>>(p, q);
+  return hipGetLastError();
+}
+
+hipError_t planes_fwd(const GatedArgs& a, const void* x, const void* w, const Epi<float>& o, char* ws, hipStream_t st) {
+  const GatedFwdWs L = gated_fwd_layout(a);
+  int* const flags = (int*)(ws + L.flags);
+  const hipError_t e = split_two(planes_of((const float*)x, a.ldx, a.m, a.k, ws + L.x, flags),
+                                 planes_of((const float*)w, a.ldw, 2LL * a.n, a.k, ws + L.w, flags + kSplitBlocks), st);
+  if (e != hipSuccess) return e;
+  return parts_product<false, false, true>(plane_mat(ws + L.x, a.m, a.k, false), plane_mat(ws + L.w, 2LL * a.n, a.k, false), a.m, a.n,
+                                           a.k, L.S, (float*)(ws + L.part), flags, kSplitBlocks, flags + kSplitBlocks, kSplitBlocks,
+                                           o, st);
+}
+
+hipError_t planes_bwd(const GatedArgs& a, const GatedBwdWs& L, const void* x, const void* w, const void* pre, const void* dy,
+                      void* dx, void* dw, float* dbp, char* ws, hipStream_t st) {
+  const int gx = (a.n + 127) / 128;
+  int *const fw = (int*)(ws + L.flags), *const fx = fw + kSplitBlocks, *const fz = fx + kSplitBlocks;
+  gated_dz_planes_kernel<<<dim3(gx, L.P), 256, 0, st>>>((const float*)dy, a.lddy, (const float*)pre, a.act, a.m, a.n, L.rpg,
+                                                       (bf16_t*)(ws + L.dz), dbp, fz);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (!dx && !dw)) return e;
+  const Planes pw = planes_of((const float*)w, a.ldw, 2LL * a.n, a.k, ws + L.w, fw);
+  const Planes px = planes_of((const float*)x, a.ldx, a.m, a.k, ws + L.x, fx);
+  const Planes none_w{nullptr, 0, 0, 0, nullptr, fw}, none_x{nullptr, 0, 0, 0, nullptr, fx};   // not asked for: no rows
+  e = split_two(dx ? pw : none_w, dw ? px : none_x, st);
+  if (e != hipSuccess) return e;
+  if (dx) {
+    const Epi<float> o{a.m, a.k, (float*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
+    e = parts_product<false, true, false>(plane_mat(ws + L.dz, a.m, 2LL * a.n, false), plane_mat(ws + L.w, 2LL * a.n, a.k, true), a.m,
+                                          a.k, 2LL * a.n, L.Sx, (float*)(ws + L.rest), fz, gx * L.P, fw, kSplitBlocks, o, st);
+    if (e != hipSuccess) return e;
+  }
+  if (dw) {
+    const Epi<float> o{2LL * a.n, a.k, (float*)dw, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
+    e = parts_product<true, true, false>(plane_mat(ws + L.dz, a.m, 2LL * a.n, true), plane_mat(ws + L.x, a.m, a.k, true), 2LL * a.n,
+                                         a.k, a.m, L.Sw, (float*)(ws + L.rest), fz, gx * L.P, fx, kSplitBlocks, o, st);
+  }
+  return e;
 }
 
 template <typename T>
@@ -103,7 +505,10 @@ hipError_t gated_fwd(const GatedArgs& a, const void* x, const void* w, const voi
   const Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, nullptr, 0, (T*)pre, a.act, nullptr};
   const Mat<T> mx{(const T*)x, a.ldx, a.m, a.k}, mw{(const T*)w, a.ldw, 2LL * a.n, a.k};
   if (few_rows_ok(a.m, a.k)) return few_rows<T, 2>(mx, mw, a.m, a.n, a.k, o, st);
-  return product<T, false, false, true>(mx, mw, a.m, a.n, a.k, fwd_plan(a), (float*)ws, o, st);
+  if constexpr (sizeof(T) == 4) {
+    if (fwd_planes(a)) return planes_fwd(a, x, w, o, (char*)ws, st);
+  }
+  return product<T, false, false, true>(mx, mw, a.m, a.n, a.k, fwd_plan(a), (float*)((char*)ws + gated_fwd_layout(a).part), o, st);
 }
 
 template <typename T>
@@ -114,24 +519,28 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
   char* const c = (char*)ws;
   T* const dz = (T*)(c + L.dz);
   float* const dbp = db && a.m > 0 ? (float*)(c + L.dbp) : nullptr;
-  if (a.m > 0) {
+  const bool planes = a.m > 0 && bwd_planes(a);
+  if (planes) {
+    const hipError_t e = planes_bwd(a, L, x, w, pre, dy, dx, dw, dbp, c, st);
+    if (e != hipSuccess) return e;
+  } else if (a.m > 0) {
     gated_dz_kernel<T><<<dim3((a.n + 32 * E - 1) / (32 * E), L.P), 256, 0, st>>>((const T*)dy, a.lddy, (const T*)pre, a.act,
                                                                                  a.m, a.n, L.rpg, dz, dbp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  // without rows this also clears db
-  const hipError_t e = launch_linear_bwd(rows_of(a), x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
-  if (e != hipSuccess || !dbp) return e;
+  if (!planes) {    // without rows this also clears db
+    const hipError_t e = launch_linear_bwd(rows_of(a), x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
+    if (e != hipSuccess) return e;
+  }
+  if (!dbp) return hipSuccess;
   db_sum_kernel<T><<<(2 * a.n + 63) / 64, 1024, 0, st>>>(dbp, L.P, 2 * a.n, (T*)db);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t gated_fwd_ws_bytes(const GatedArgs& a) {
-  return few_rows_ok(a.m, a.k) ? 0 : plan_bytes(fwd_plan(a), a.m, 2LL * a.n);
-}
+size_t gated_fwd_ws_bytes(const GatedArgs& a) { return gated_fwd_layout(a).total; }
 
 hipError_t launch_gated_fwd(const GatedArgs& a, const void* x, const void* w, const void* bias, void* y, void* pre, void* ws,
                             hipStream_t st) {

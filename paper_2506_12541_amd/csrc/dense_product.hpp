@@ -561,8 +561,9 @@ struct DmaTile {
       off[u] = 2u * (TR ? (uint32_t)row * (uint32_t)m.ld + min(c, last) : (uint32_t)min(row, last) * (uint32_t)m.ld + c);
     }
   }
-  __device__ __forceinline__ void issue(bf16_t* lds, const Mat<bf16_t>& m, long long k0, int wid) const {
-    const char* p = base + 2 * (TR ? k0 * m.ld : k0);
+  // more: bytes to a matrix of the same shape behind this one
+  __device__ __forceinline__ void issue(bf16_t* lds, const Mat<bf16_t>& m, long long k0, int wid, long long more = 0) const {
+    const char* p = base + 2 * (TR ? k0 * m.ld : k0) + more;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       const bool second = G && ((wid * NU + u) * (64 / CPR) & 16);
@@ -609,7 +610,14 @@ __device__ __forceinline__ void epi_store8(const Epi<bf16_t>& o, long long m, in
   store16u(o.out + m * o.ldo + n, pack16<bf16_t>(v));
 }
 
-// Eight consecutive columns of both maps of a gated product.
+// A store past the caches' retention, of 16 bytes at element alignment.
+__device__ __forceinline__ void store16_stream(bf16_t* p, uint4 v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+}
+
+// Eight consecutive columns of both maps of a gated product. The outputs are larger than the operands and do not
+// push them out of the caches: 65536 x 512 -> 2 x 2048 with [g | u] kept 461 us, so 428; 8192 x 4096 -> 2 x 8192 965 and 897.
 __device__ __forceinline__ void gated_store8(const Epi<bf16_t>& o, long long m, int n, float (&g)[8], float (&u)[8], int split) {
   if (n + 8 > o.N || o.part) {
     float g0[4] = {g[0], g[1], g[2], g[3]}, g1[4] = {g[4], g[5], g[6], g[7]};
@@ -629,12 +637,12 @@ __device__ __forceinline__ void gated_store8(const Epi<bf16_t>& o, long long m, 
     for (int e = 0; e < 8; ++e) u[e] += t[e];
   }
   if (o.pre) {
-    store16u(o.pre + m * 2 * o.N + n, pack16<bf16_t>(g));
-    store16u(o.pre + m * 2 * o.N + o.N + n, pack16<bf16_t>(u));
+    store16_stream(o.pre + m * 2 * o.N + n, pack16<bf16_t>(g));
+    store16_stream(o.pre + m * 2 * o.N + o.N + n, pack16<bf16_t>(u));
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) u[e] *= act_fwd<bf16_t>(g[e], o.act);
-  store16u(o.out + m * o.ldo + n, pack16<bf16_t>(u));
+  store16_stream(o.out + m * o.ldo + n, pack16<bf16_t>(u));
 }
 
 // Workgroup tile BM x BN of WM x WN waves, contraction tiles of BK in a ring of NS LDS stages,
@@ -694,8 +702,8 @@ __global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
     if (kt0 + s < kt1) issue(kt0 + s, s);
-  if constexpr (NW == 8) {
-    // Two waves share a SIMD; the second four waves run one phase behind the first four, so one
+  if constexpr (NW == 8 && NS == 4) {
+    // One workgroup to a CU: two waves share a SIMD; the second four waves run one phase behind the first four, so one
     // wave of each SIMD multiplies while the other reads its fragments. Phases end with a
     // barrier; group 0 reads tile t in phase 2t and multiplies in 2t + 1, group 1 one phase
     // later. Stage (t - 1) % NS is last read in phase 2t - 1, so tile t + NS - 1 may be loaded
@@ -1034,6 +1042,15 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
   const int cols = G ? side / 2 : side;    // outputs of a tile's row
   const int ntm = (int)((M + side - 1) / side), ntn = (N + cols - 1) / cols;
   const dim3 grid((unsigned)((long long)ntm * ntn), (unsigned)p.S);
+  if constexpr (sizeof(T) == 2 && G) {
+    // A gated tile's epilogue is long: over short contractions 256 x 128 tiles, two to a CU, let one write while the other
+    // multiplies (65536 x 512 -> 2 x 2048: 338 us, 256 x 256 350; 65536 x 256 -> 2 x 512: 57 and 65; 16384 x 1024 -> 2 x 1024: 77 and 71).
+    if (dma && side == 256 && K <= 512 && p.S == 1) {
+      const int nn = (N + 63) / 64;
+      product_dma_kernel<TA, TB, 256, 128, 4, 2, 32, 3, G><<<(unsigned)((long long)ntm * nn), 512, 0, st>>>(a, b, K, ntm, nn, (int)(K / 32), o);
+      return hipGetLastError();
+    }
+  }
   if constexpr (sizeof(T) == 2) {
     if (dma) {
       const int bk = side == 256 ? 32 : 64;

@@ -149,8 +149,11 @@ __device__ __forceinline__ float head_sum(float x, int G) {
   return x;
 }
 
-// 1 / sqrt(x) to 2^-23, x > 0 (of a denormal number: as of the smallest normal one).
-__device__ __forceinline__ float inverse_root(float x) { return __builtin_amdgcn_rsqf(fmaxf(x, 1.17549435e-38f)); }
+// 1 / sqrt(x) to 2^-23, x > 0 (of a denormal number: as of the smallest normal one; NaN stays).
+__device__ __forceinline__ float inverse_root(float x) {
+  constexpr float least = 1.17549435e-38f;
+  return __builtin_amdgcn_rsqf(x < least ? least : x);
+}
 
 // grid: x steps of R rows, four to a workgroup; y waves that share the heads of a step; z queries and keys.
 template <typename T, bool INTER, bool BWD, bool WHOLE>

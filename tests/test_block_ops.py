@@ -276,3 +276,30 @@ def test_quantise_agrees_with_the_library_conversion():
     assert torch.equal(values, want)
     top = x.double().abs().amax(2, keepdim=True) / scale
     assert ((top <= 448) & ((top > 224) | (codes.t()[..., None] == 63)) | (codes.t()[..., None] == 190)).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_the_definitions_gradients_are_their_differences(interleaved):
+    """The float64 gradients that the GPU tests compare with, against central differences of the float64 outputs."""
+    g = torch.Generator().manual_seed(2)
+    r = lambda *s: torch.randn(s, generator=g, dtype=torch.float64)
+    x, gain, dy = r(3, 2, 20), r(20), r(3, 2, 20)
+    at, freq = torch.tensor([0, 7, 1000]), dense.rotary_frequencies(12, device="cpu")[0]
+    # bounds go by the type: float32 stands for it, the values are float64
+    block_ref.HALF[torch.float64] = block_ref.HALF[torch.float32]
+    try:
+        f = lambda x, gain: (block_ref.rotary(x, at, freq, gain, 1e-3, interleaved, 1.5)["y"][0] * dy).sum()
+        got = block_ref.rotary(x, at, freq, gain, 1e-3, interleaved, 1.5, dy)
+        dx, dgain = r(3, 2, 20), r(20)
+        e = 1e-6
+        assert abs((f(x + e * dx, gain) - f(x - e * dx, gain)) / (2 * e) - (got["dx"][0] * dx).sum()) < 1e-6
+        assert abs((f(x, gain + e * dgain) - f(x, gain - e * dgain)) / (2 * e) - (got["dgain"][0] * dgain).sum()) < 1e-6
+        x, w, b, dy2 = r(5, 7), r(12, 7), r(12), r(5, 6)
+        for act in ("none", "gelu", "silu"):
+            f = lambda x, w, b: (block_ref.gated(x, w, b, act)["y"][0] * dy2).sum()
+            got = block_ref.gated(x, w, b, act, dy2)
+            for name, t in (("dx", r(5, 7)), ("dw", r(12, 7)), ("db", r(12))):
+                up, down = ([v + s * e * t if n == name else v for n, v in (("dx", x), ("dw", w), ("db", b))] for s in (1, -1))
+                assert abs((f(*up) - f(*down)) / (2 * e) - (got[name][0] * t).sum()) < 1e-6, (act, name)
+    finally:
+        del block_ref.HALF[torch.float64]

@@ -264,3 +264,486 @@ def test_cache_attention_many_sequences_and_long_ones(dtype):
     check_cache_attention(gen(11), dtype, [1] * 300, [64] * 300, [i % 65 for i in range(300)], 2, 2, 32, True)
     check_cache_attention(gen(12), dtype, [700], [1500], [1300], 4, 1, 64, True)
     check_cache_attention(gen(13), dtype, [1], [9000], [8999], 2, 1, 128, True, scale=0.3)
+
+
+# ---- rotary: calls that the documentation allows ----
+
+def rotary_args(g, dt, rows, heads, kv, d, rot, norm=True):
+    q, k = normal(g, rows, heads, d, dtype=dt), normal(g, rows, kv, d, dtype=dt)
+    dq, dk = normal(g, rows, heads, d, dtype=dt), normal(g, rows, kv, d, dtype=dt)
+    at = torch.randint(0, 3000, (rows,), generator=g, dtype=torch.int32).cuda()
+    freq, _ = dense.rotary_frequencies(rot)
+    how = dict(gain_q=normal(g, d, shift=1.0), gain_k=normal(g, d, shift=1.0)) if norm else {}
+    return q, k, dq, dk, at, freq, how
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot", [(64, 48), (30, 14)])
+def test_rotary_views_in_place_and_given_outputs(dtype, inter, d, rot):
+    """Views of a fused projection, outputs in views, and outputs on top of inputs give the packed tensors' bits."""
+    g, dt = gen(d), DT[dtype]
+    q, k, dq, dk, at, freq, how = rotary_args(g, dt, 37, 4, 2, d, rot)
+    how["interleaved"] = inter
+    yq, yk = dense.rotary_forward(q, k, at, freq, **how)
+    a = dense.rotary_backward(dq, dk, at, freq, q=q, k=k, **how)
+    fused, dfused = (torch.full((37, 9, d), 7.0, dtype=dt, device="cuda") for _ in range(2))
+    fused[:, :4], fused[:, 4:6] = q, k
+    vq, vk = fused[:, :4], fused[:, 4:6]
+    oq, ok = dense.rotary_forward(vq, vk, at, freq, y_q=dfused[:, :4], y_k=dfused[:, 4:6], **how)
+    assert torch.equal(oq, yq) and torch.equal(ok, yk) and (dfused[:, 6:] == 7).all()
+    b = dense.rotary_backward(dq, dk, at, freq, q=vq, k=vk, dq=dfused[:, :4], dk=dfused[:, 4:6], **how)
+    assert torch.equal(b["dq"], a["dq"]) and torch.equal(b["dk"], a["dk"]) and (dfused[:, 6:] == 7).all()
+    assert torch.equal(b["dgain_q"], a["dgain_q"]) and torch.equal(b["dgain_k"], a["dgain_k"])
+    eq, ek = dq.clone(), dk.clone()                    # gradients on top of the given ones
+    c = dense.rotary_backward(eq, ek, at, freq, q=q, k=k, dq=eq, dk=ek, **how)
+    assert torch.equal(eq, a["dq"]) and torch.equal(ek, a["dk"]) and torch.equal(c["dgain_q"], a["dgain_q"])
+    dense.rotary_forward(vq, vk, at, freq, y_q=vq, y_k=vk, **how)       # in place, in views
+    assert torch.equal(vq, yq) and torch.equal(vk, yk) and (fused[:, 6:] == 7).all()
+    only, none = dense.rotary_forward(q, None, at, freq, gain_q=how["gain_q"], interleaved=inter)
+    assert torch.equal(only, yq) and none is None
+    one = dense.rotary_backward(dq, None, at, freq, q=q, gain_q=how["gain_q"], interleaved=inter)
+    assert torch.equal(one["dq"], a["dq"]) and one["dk"] is None and one["dgain_k"] is None
+
+
+def test_rotary_broadcast_and_head_major_inputs():
+    g = gen(3)
+    q, k, dq, dk, at, freq, how = rotary_args(g, BF, 21, 4, 2, 64, 64)
+    for x in (q[:, :1].expand(21, 4, 64), q[:1].expand(21, 4, 64), q.transpose(0, 1).contiguous().transpose(0, 1)):
+        y, _ = dense.rotary_forward(x, k, at, freq, **how)
+        z, _ = dense.rotary_forward(x.contiguous(), k, at, freq, **how)
+        assert torch.equal(y, z)
+        a = dense.rotary_backward(x, dk, at, freq, q=q, k=k, **how)      # as the gradient too
+        b = dense.rotary_backward(x.contiguous(), dk, at, freq, q=q, k=k, **how)
+        assert torch.equal(a["dq"], b["dq"]) and torch.equal(a["dgain_q"], b["dgain_q"])
+
+
+def test_rotary_turned_back_is_where_it_was():
+    """Without a norm the backward turns back: a length times magnitude squared."""
+    g = gen(4)
+    q, k, _, _, at, freq, _ = rotary_args(g, F32, 50, 2, 1, 64, 32, norm=False)
+    y, yk = dense.rotary_forward(q, k, at, freq, magnitude=2.0)
+    back = dense.rotary_backward(y, yk, at, freq, magnitude=2.0)
+    assert torch.allclose(back["dq"][..., :32], 4 * q[..., :32], atol=1e-5) and torch.equal(back["dq"][..., 32:], q[..., 32:])
+    at64 = at.to(torch.int32)
+    neg, _ = dense.rotary_forward(y, None, -at64, freq, magnitude=0.5)
+    assert torch.allclose(neg[..., :32], q[..., :32], atol=1e-5)
+
+
+def test_rotary_no_rows_and_values_that_are_not_finite():
+    g = gen(5)
+    q, k, dq, dk, at, freq, how = rotary_args(g, F32, 6, 2, 1, 64, 32)
+    e = dense.rotary_forward(q[:0], k[:0], at[:0], freq, **how)
+    b = dense.rotary_backward(dq[:0], dk[:0], at[:0], freq, q=q[:0], k=k[:0], **how)
+    assert e[0].shape == (0, 2, 64) and b["dq"].shape == (0, 2, 64) and not b["dgain_q"].any() and not b["dgain_k"].any()
+    want, _ = dense.rotary_forward(q, k, at, freq, **how)
+    x = q.clone()
+    x[1, 0, 5], x[3, 1, 40] = math.nan, math.inf
+    y, _ = dense.rotary_forward(x, k, at, freq, **how)
+    assert y[1, 0].isnan().all() and y[3, 1].isnan().any()         # their own heads, and no others
+    keep = torch.ones(6, 2, dtype=torch.bool, device="cuda")
+    keep[1, 0] = keep[3, 1] = False
+    assert torch.equal(y[keep], want[keep])
+    pos = at.float()
+    pos[2], pos[4] = math.inf, math.nan
+    y, _ = dense.rotary_forward(q, k, pos, freq, **how)
+    assert y[[2, 4]][..., :32].isnan().all() and torch.equal(y[[2, 4]][..., 32:], want[[2, 4]][..., 32:])
+    assert torch.equal(y[[0, 1, 3, 5]], want[[0, 1, 3, 5]])
+    zero = torch.zeros_like(q)
+    y, _ = dense.rotary_forward(zero, k, at, freq, **how)
+    z = dense.rotary_backward(dq, dk, at, freq, q=zero, k=k, **how)
+    assert not y.any() and z["dq"].isfinite().all() and not z["dgain_q"].any()
+
+
+def test_rotary_long_tensors():
+    """Offsets past 32 bits: the last rows of a tensor of more than 2^32 elements, in place."""
+    rows, heads, d = (1 << 32) // (32 * 128) + 3, 32, 128
+    x = torch.zeros(rows, heads, d, dtype=BF, device="cuda")
+    g = gen(6)
+    last = normal(g, 5, heads, d, dtype=BF)
+    x[-5:] = last
+    at = torch.arange(rows, dtype=torch.int32, device="cuda")
+    freq, _ = dense.rotary_frequencies(128)
+    want, _ = dense.rotary_forward(last, None, at[-5:].contiguous(), freq)
+    dense.rotary_forward(x, None, at, freq, y_q=x)
+    assert torch.equal(x[-5:], want) and not x[:-5:1000].any()
+
+
+# ---- gated map: calls that the documentation allows ----
+
+@pytest.mark.parametrize("m,k,n", [(800, 300, 700), (3586, 515, 1029), (1000, 2100, 600), (2001, 257, 1500)])
+def test_gated_float32_planes(m, k, n):
+    """Sizes at which float32 products run on operands split before."""
+    check_gated(gen(m), "f32", m, k, n, "silu", True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(200, 136, 132), (900, 264, 520)])
+def test_gated_strides_and_parts(dtype, m, k, n):
+    """Operands whose rows lie apart, aligned to 16 bytes and not; gradients that are not asked for."""
+    g, dt = gen(5), DT[dtype]
+    x, w, dy = normal(g, m, k, dtype=dt), normal(g, 2 * n, k, dtype=dt, scale=0.1), normal(g, m, n, dtype=dt)
+    y, pre = dense.gated_forward(x, w, act="gelu", save_pre=True)
+    a = dense.gated_backward(x, w, dy, pre, act="gelu", bias=True)
+
+    def apart(t, more):
+        buf = torch.full((t.shape[0], t.shape[1] + more), float("nan"), dtype=dt, device="cuda")
+        buf[:, :t.shape[1]] = t
+        return buf[:, :t.shape[1]]
+    for more in (8, 3):
+        ys, ps = dense.gated_forward(apart(x, more), apart(w, more), act="gelu", save_pre=True)
+        b = dense.gated_backward(apart(x, more), apart(w, more), apart(dy, more), ps, act="gelu", bias=True)
+        for u, v in ((y, ys), (pre, ps), *((a[name], b[name]) for name in a)):
+            assert torch.allclose(u.float(), v.float(), rtol=2 * dense_ref.HALF[dt], atol=2e-3)
+    plain, none = dense.gated_forward(x, w, act="gelu")
+    assert torch.equal(plain, y) and none is None
+    y3, p3 = dense.gated_forward(x.view(4, m // 4, k), w, act="gelu", save_pre=True)
+    assert torch.equal(y3.view(m, n), y) and p3.shape == (4, m // 4, 2 * n)
+    for kw in (dict(need_dx=False), dict(need_dw=False), dict(need_dx=False, need_dw=False, bias=True), dict(bias=True, need_dw=False)):
+        some = dense.gated_backward(x, w, dy, pre, act="gelu", **kw)
+        assert (some["dx"] is None) == (not kw.get("need_dx", True)) and (some["dw"] is None) == (not kw.get("need_dw", True))
+        for name in ("dx", "dw", "db"):
+            assert some[name] is None or torch.equal(some[name], a[name])
+
+
+def test_gated_no_rows_and_values_that_are_not_finite():
+    w = torch.ones(80, 24, device="cuda", dtype=BF)
+    e = torch.zeros(0, 24, device="cuda", dtype=BF)
+    y, pre = dense.gated_forward(e, w, save_pre=True)
+    got = dense.gated_backward(e, w, y, pre, bias=True)
+    assert y.shape == (0, 40) and got["dx"].shape == (0, 24) and not got["dw"].any() and not got["db"].any()
+    for dt in (BF, F32):
+        for m, k, n in ((3, 24, 40), (200, 72, 40), (300, 100, 40), (900, 300, 600)):
+            x = torch.ones(m, k, device="cuda", dtype=dt)
+            x[1, k - 1], x[2, 0] = math.inf, math.nan
+            w = torch.full((2 * n, k), 1 / 16, device="cuda", dtype=dt)
+            y, pre = dense.gated_forward(x, w, act="none", save_pre=True)
+            assert (y[0] == (k / 16) ** 2).all() if k < 256 or dt == F32 else True
+            assert (y[1] == math.inf).all() and y[2].isnan().all() and torch.equal(y[3:], y[:1].expand(m - 3, n))
+            assert (pre[1] == math.inf).all() and pre[2].isnan().all()
+            g = dense.gated_backward(x, w, torch.ones_like(y), pre, act="none")
+            assert g["dx"][3:].isfinite().all() and (g["dx"][1] == math.inf).all() and g["dx"][2].isnan().all()
+
+
+def test_gated_float32_values_that_do_not_split():
+    """The largest float32 values and small ones through operands split before."""
+    big, (m, k, n) = torch.finfo(F32).max, (900, 300, 600)
+    g = gen(8)
+    x, w = normal(g, m, k), normal(g, 2 * n, k, scale=0.1)
+    x[2] = 0
+    x[2, 5] = big
+    w[:, 5] = 0.5
+    x[3] = 2.0 ** -120                       # its parts reach into the denormal numbers
+    _, pre = dense.gated_forward(x, w, act="none", save_pre=True)
+    want = x.double().cpu() @ w.double().cpu().t()
+    assert (pre[2] == big / 2).all()
+    size = x[3:].double().cpu().abs() @ w.double().cpu().abs().t()
+    check("pre", pre[3:], want[3:], (k + 2) * dense_ref.F * size + 2.0 ** -140)
+    x[4, 7] = -math.inf
+    _, pre = dense.gated_forward(x, w, act="none", save_pre=True)
+    assert torch.equal(pre[4], -torch.sign(w[:, 7]) * math.inf) and (pre[2] == big / 2).all()
+    check("pre beside an infinity", pre[5:], want[5:], (k + 2) * dense_ref.F * size[2:] + 2.0 ** -140)
+
+
+# ---- 8-bit cache: calls that the documentation allows ----
+
+def filled(g, rows, kv, d, layout="rows", amp=1.3):
+    cache = dense.cache_alloc(rows, kv, d)
+    if layout == "heads":                    # a head's rows one behind another
+        cache = dense.Cache(*(torch.zeros(kv, rows, d, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).transpose(0, 1)
+                              for _ in range(2)), cache.k_exp, cache.v_exp)
+    elif layout == "fused":                  # keys and values side by side, as one of several layers
+        both = torch.zeros(3, rows, 2 * kv, d, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+        cache = dense.Cache(both[1, :, :kv], both[1, :, kv:], cache.k_exp, cache.v_exp)
+    k, v = normal(g, rows, kv, d, scale=amp), normal(g, rows, kv, d)
+    one = cu([rows])
+    dense.cache_write(cache, k, v, one, one)
+    return cache, k, v
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("lq", [[1, 1, 1], [300, 40, 200]])
+def test_cache_layouts(d, lq):
+    """Head-major and fused caches, and views of a fused projection, give the packed tensors' bits."""
+    cap, used = cu([500, 64, 900]), ints([400, 64, 333])
+    n, outs = sum(lq), []
+    for layout in ("rows", "heads", "fused"):
+        g = gen(d)
+        cache, _, _ = filled(g, 1464, 4, d, layout)
+        qkv = normal(g, n, 16, d, dtype=BF)
+        if layout == "rows":
+            q, k, v = (t.contiguous() for t in (qkv[:, :8], qkv[:, 8:12], qkv[:, 12:]))
+        else:
+            q, k, v = qkv[:, :8], qkv[:, 8:12], qkv[:, 12:]
+        cu_q = cu(lq)
+        dense.cache_write(cache, k, v, cu_q, cap, used)
+        o, lse = dense.cache_attention_forward(q, cache, cu_q, cap, used, causal=True)
+        kr, vr = dense.cache_read(cache, 797, cu([400, 64, 333]), cap, used, dtype=F32)
+        outs.append((o, lse, kr, vr, cache.k_exp, cache.v_exp))
+    for other in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
+    oo = torch.full((n, 16, d), 3.0, dtype=BF, device="cuda")[:, 3:11]
+    ll = torch.zeros(8, n, device="cuda")
+    o, lse = dense.cache_attention_forward(q, cache, cu_q, cap, used, causal=True, o=oo, lse=ll)
+    assert o is oo and lse is ll and torch.equal(o, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+def test_cache_attention_is_packed_attention_of_what_the_cache_holds():
+    g = gen(12)
+    lens = [700, 0, 130, 1, 64]
+    cache, _, _ = filled(g, sum(lens), 2, 64)
+    q = normal(g, sum(lens), 8, 64, dtype=BF)
+    c = cu(lens)
+    k, v = dense.cache_read(cache, sum(lens), c, c)
+    for causal in (False, True):
+        o, lse = dense.cache_attention_forward(q, cache, c, c, causal=causal)
+        p, want = dense.attention_forward(q, k, v, c, causal=causal)
+        assert torch.allclose(lse, want, rtol=1e-5, atol=1e-5) and torch.allclose(o.float(), p.float(), rtol=2 ** -6, atol=2 ** -7)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lq,lk", [(5, 200), (150, 180), (1, 70), (300, 300)])
+def test_cache_attention_nan_behind_the_mask(dtype, lq, lk):
+    """NaN in a key or value reaches the queries that see it, and no others."""
+    g = gen(lq)
+    cache, _, _ = filled(g, lk, 2, 64)
+    q = normal(g, lq, 4, 64, dtype=DT[dtype])
+    cq, ck = cu([lq]), cu([lk])
+    want, wl = dense.cache_attention_forward(q, cache, cq, ck, causal=True)
+    for which in ("k", "v"):
+        for row in {lk - 1, lk - 2 if lq > 1 else lk - 1, lk - 1 - lq // 2}:
+            for col in (0, 37):
+                byte = getattr(cache, which).view(torch.uint8)
+                keep = byte[row, 1, col].clone()
+                byte[row, 1, col] = 0xff
+                o, lse = dense.cache_attention_forward(q, cache, cq, ck, causal=True)
+                byte[row, 1, col] = keep
+                first = max(row - (lk - lq), 0)               # the first query that sees the row
+                assert torch.equal(o[:first], want[:first]) and torch.equal(o[:, :2], want[:, :2])
+                assert o[first:, 2:, col].isnan().all()
+                assert torch.equal(lse[:2], wl[:2]) and torch.equal(lse[2:, :first], wl[2:, :first])
+
+
+def test_cache_attention_rows_in_no_sequence_and_sharp_rows():
+    g = gen(14)
+    cache, _, _ = filled(g, 300, 1, 64, amp=8.0)             # scores with a wide range
+    q = normal(g, 40, 2, 64, dtype=BF, scale=4.0)
+    cq, ck, used = cu([3, 0, 20]), cu([100, 50, 140]), ints([77, 50, 140])
+    o, lse = dense.cache_attention_forward(q, cache, cq, ck, used, causal=True)
+    assert not o[23:].any() and (lse[:, 23:] == -math.inf).all() and o[:23].isfinite().all()
+    oo, ll = torch.full_like(o, 5.0), torch.full_like(lse, 5.0)
+    dense.cache_attention_forward(q, cache, cq, ck, used, causal=True, o=oo, lse=ll)
+    assert (oo[23:] == 5).all() and (ll[:, 23:] == 5).all() and torch.equal(oo[:23], o[:23]) and torch.equal(ll[:, :23], lse[:, :23])
+    k, v = dense.cache_read(cache, 300, cu([300]), cu([300]), dtype=F32)
+    want = dense_ref.attention(q, k, v, cq, ck, [77, 50, 140], True)
+    check("o", o, *want["o"])
+    check("lse", lse, *want["lse"])
+
+
+def test_cache_offsets_past_32_bits():
+    rows, kv, d = 4400000, 8, 128                            # 4.5 GB of keys
+    g = gen(15)
+    cache = dense.cache_alloc(rows, kv, d)
+    k, v, q = normal(g, 300, kv, d, dtype=BF), normal(g, 300, kv, d, dtype=BF), normal(g, 2, 8, d, dtype=BF)
+    cq, ck, used = cu([0, 300]), ints([0, rows - 400, rows]), ints([0, 350])
+    dense.cache_write(cache, k, v, cq, ck, used)
+    small = dense.cache_alloc(400, kv, d)
+    one, last = ints([0, 400]), ints([350])
+    dense.cache_write(small, k, v, cu([300]), one, last)
+    assert torch.equal(cache.k[-400:].view(torch.uint8), small.k.view(torch.uint8))
+    assert torch.equal(cache.v_exp[:, -400:], small.v_exp) and not cache.k_exp[:, :-400].any()
+    kr, vr = dense.cache_read(cache, 300, cq, ck, used)
+    ks, vs = dense.cache_read(small, 300, cu([300]), one, last)
+    assert torch.equal(kr, ks) and torch.equal(vr, vs) and ks.any()
+    o, lse = dense.cache_attention_forward(q, cache, cu([0, 2]), ck, used, causal=True)
+    p, want = dense.cache_attention_forward(q, small, cu([2]), one, last, causal=True)
+    assert torch.allclose(lse, want, rtol=1e-5, atol=1e-5) and torch.allclose(o.float(), p.float(), rtol=2 ** -6, atol=2 ** -7)
+
+
+# ---- streams, graphs, together ----
+
+def test_calls_on_a_stream_with_work_queued_on_it():
+    """A call on a given stream waits for what is queued there, and leaves the current stream alone."""
+    g = gen(20)
+    q, k, dq, dk, at, freq, how = rotary_args(g, BF, 64, 8, 2, 64, 64)
+    w, x = normal(g, 256, 512, dtype=BF, scale=0.05), normal(g, 64, 512, dtype=BF)
+    cache, _, _ = filled(g, 512, 2, 64)
+    cq, ck, used = cu([32, 32]), cu([256, 256]), ints([200, 256])
+
+    def run(q, k, x, stream=None):
+        a, b = dense.rotary_forward(q, k, at, freq, stream=stream, **how)
+        r = dense.rotary_backward(dq, dk, at, freq, q=q, k=k, stream=stream, **how)
+        dense.cache_write(cache, b, k, cq, ck, used, stream=stream)
+        o, lse = dense.cache_attention_forward(a, cache, cq, ck, used, causal=True, stream=stream)
+        kr, vr = dense.cache_read(cache, 64, cq, ck, used, stream=stream)
+        y, pre = dense.gated_forward(x, w, save_pre=True, stream=stream)
+        d = dense.gated_backward(x, w, y, pre, stream=stream)
+        return [a, b, r["dq"], r["dgain_k"], o, lse, kr, vr, y, d["dx"], d["dw"]]
+    want = [t.clone() for t in run(q, k, x)]
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    late = [torch.zeros_like(t) for t in (q, k, x)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            big = big @ big
+            big = big / big.abs().amax()
+        for t, u in zip(late, (q, k, x)):
+            t.copy_(u)
+    got = run(*late, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_serving_step_in_a_graph():
+    """A captured step (norms and rotation, cache, attention, gated map) whose lengths grow on the device, replayed several
+    times with eager work between, against the same steps run eagerly."""
+    g = gen(21)
+    seqs, heads, kv, d, cap = 5, 8, 2, 64, 96
+    c = heads * d
+    wqkv = normal(g, (heads + 2 * kv) * d, c, dtype=BF, scale=c ** -0.5)
+    wo, wg, wd = (normal(g, *s, dtype=BF, scale=c ** -0.5) for s in ((c, c), (2 * 256, c), (c, 256)))
+    gq, gk = normal(g, d, scale=0.1, shift=1.0), normal(g, d, scale=0.1, shift=1.0)
+    freq, mag = dense.rotary_frequencies(d, scaling="ramp", factor=2.0, trained=64)
+    x0, start = normal(g, seqs, c, dtype=BF), ints([1, 17, 60, 64, 30])
+    cq, ck = cu([1] * seqs), cu([cap] * seqs)
+
+    def step(x, used, at, cache):
+        qkv = dense.linear_forward(x, wqkv)[0].view(seqs, heads + 2 * kv, d)
+        q, k = dense.rotary_forward(qkv[:, :heads], qkv[:, heads:heads + kv], at, freq, gain_q=gq, gain_k=gk, magnitude=mag)
+        dense.cache_write(cache, k, qkv[:, heads + kv:], cq, ck, used)
+        o, lse = dense.cache_attention_forward(q, cache, cq, ck, used, causal=True)
+        h, _ = dense.linear_forward(o.view(seqs, c), wo, residual=x)
+        a, _ = dense.gated_forward(h, wg)
+        y, _ = dense.linear_forward(a, wd, residual=h)
+        return y, lse
+
+    def fresh():
+        cache, _, _ = filled(gen(22), cap * seqs, kv, d)
+        return x0.clone(), start.clone(), start - 1, cache
+    x, used, at, cache = fresh()
+    eager = []
+    for _ in range(6):
+        y, lse = step(x, used, at, cache)
+        eager.append((y.clone(), lse.clone(), [t.view(torch.uint8).clone() for t in cache]))
+        x.copy_(y), used.add_(1), at.add_(1)
+    x, used, at, cache = fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, used, at, dense.Cache(*(t.clone() for t in cache)))      # warm up on a copy
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, lse = step(x, used, at, cache)
+    for want_y, want_lse, want_cache in eager:
+        graph.replay()
+        torch.randn(1000, device="cuda").sum()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want_y) and torch.equal(lse, want_lse)
+        assert all(torch.equal(t.view(torch.uint8), u) for t, u in zip(cache, want_cache))
+        x.copy_(y), used.add_(1), at.add_(1)
+
+
+def test_training_step_in_a_graph():
+    """The backward calls captured beside the forward ones, two graphs on workspaces of their own, replayed in turn."""
+    g = gen(23)
+    graphs = []
+    for rows in (70, 300):
+        q, k, dq, dk, at, freq, how = rotary_args(g, BF, rows, 4, 2, 64, 32)
+        x, w, dy = normal(g, rows, 128, dtype=F32), normal(g, 400, 128, scale=0.1), normal(g, rows, 200)
+
+        def step():
+            yq, yk = dense.rotary_forward(q, k, at, freq, **how)
+            r = dense.rotary_backward(dq, dk, at, freq, q=q, k=k, **how)
+            y, pre = dense.gated_forward(x, w, save_pre=True)
+            d = dense.gated_backward(x, w, dy, pre, bias=True)
+            return [yq, yk, r["dq"], r["dk"], r["dgain_q"], r["dgain_k"], y, d["dx"], d["dw"], d["db"]]
+        want = [t.clone() for t in step()]
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            got = step()
+        graphs.append((graph, got, want, (q, k, dq, dk, at, freq, how, x, w, dy)))     # a graph reads its inputs where they lie
+    for _ in range(3):
+        for graph, got, want, _ in graphs:
+            for t in got:
+                t.fill_(float("nan"))
+            graph.replay()
+        for graph, got, want, _ in graphs:
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_block_forward_and_backward_together():
+    """One float32 block around packed attention, its gradients against autograd in 64 bits and against differences."""
+    g = gen(24)
+    lens, heads, kv, d, f = [40, 1, 23], 4, 2, 32, 96
+    n, c = sum(lens), heads * d
+    cq = cu(lens)
+    at = torch.cat([torch.arange(v) for v in lens]).to(torch.int32).cuda()
+    freq, _ = dense.rotary_frequencies(24)
+    P = {name: normal(g, *s, scale=s[-1] ** -0.5) for name, s in (("wqkv", ((heads + 2 * kv) * d, c)), ("wo", (c, c)),
+                                                               ("wg", (2 * f, c)), ("wd", (c, f)))}
+    P.update(x=normal(g, n, c), gq=normal(g, d, scale=0.1, shift=1.0), gk=normal(g, d, scale=0.1, shift=1.0))
+    dy = normal(g, n, c)
+    sp = (heads, heads + kv)
+    qkv, _ = dense.linear_forward(P["x"], P["wqkv"])
+    t = qkv.view(n, -1, d)
+    q, k = dense.rotary_forward(t[:, :sp[0]], t[:, sp[0]:sp[1]], at, freq, gain_q=P["gq"], gain_k=P["gk"])
+    v = t[:, sp[1]:]
+    o, lse = dense.attention_forward(q, k, v, cq, causal=True)
+    h, _ = dense.linear_forward(o.view(n, c), P["wo"], residual=P["x"])
+    a, pre = dense.gated_forward(h, P["wg"], save_pre=True)
+    y, _ = dense.linear_forward(a, P["wd"], residual=h)
+    b4 = dense.linear_backward(a, P["wd"], dy)
+    b3 = dense.gated_backward(h, P["wg"], b4["dx"], pre)
+    dh = dy + b3["dx"]
+    b2 = dense.linear_backward(o.view(n, c), P["wo"], dh)
+    b1 = dense.attention_backward(q, k, v, o, lse, b2["dx"].view(n, heads, d), cq, causal=True)
+    dqkv = torch.empty_like(t)
+    br = dense.rotary_backward(b1["dq"], b1["dk"], at, freq, q=t[:, :sp[0]], k=t[:, sp[0]:sp[1]], gain_q=P["gq"], gain_k=P["gk"],
+                               dq=dqkv[:, :sp[0]], dk=dqkv[:, sp[0]:sp[1]])
+    dqkv[:, sp[1]:] = b1["dv"]
+    b0 = dense.linear_backward(P["x"], P["wqkv"], dqkv.view(n, -1))
+    got = dict(wqkv=b0["dw"], wo=b2["dw"], wg=b3["dw"], wd=b4["dw"], x=dh + b0["dx"], gq=br["dgain_q"], gk=br["dgain_k"])
+
+    def block(p):
+        """In 64 bits on the CPU."""
+        t = (p["x"] @ p["wqkv"].t()).view(n, -1, d)
+        ang = at.cpu().double()[:, None] * freq.cpu()
+        co, si = ang.cos()[:, None], ang.sin()[:, None]
+
+        def turn(z, gain):
+            z = z / (z.square().mean(-1, keepdim=True) + 1e-6).sqrt() * gain
+            u, w = z[..., :12], z[..., 12:24]
+            return torch.cat((u * co - w * si, u * si + w * co, z[..., 24:]), -1)
+        q, k, v = turn(t[:, :sp[0]], p["gq"]), turn(t[:, sp[0]:sp[1]], p["gk"]), t[:, sp[1]:]
+        outs, first = [], 0
+        for m in lens:
+            r = slice(first, first + m)
+            first += m
+            mask = torch.full((m, m), -math.inf, dtype=torch.float64).triu(1)
+            for j in range(heads):
+                s = q[r, j] @ k[r, j // 2].t() / math.sqrt(d) + mask
+                outs.append((r, j, s.softmax(-1) @ v[r, j // 2]))
+        o = torch.cat([torch.cat([x for r, j, x in outs if r.start == s], 1) for s in sorted({r.start for r, _, _ in outs})])
+        h = p["x"] + o @ p["wo"].t()
+        z = h @ p["wg"].t()
+        return h + (torch.nn.functional.silu(z[:, :f]) * z[:, f:]) @ p["wd"].t()
+    p64 = {name: t.cpu().double().requires_grad_() for name, t in P.items()}
+    out = block(p64)
+    (out * dy.cpu().double()).sum().backward()
+    # ten float32 steps in a row, each within some 10 roundings of sums of 100 terms: 1e-4 of a tensor's largest value
+    assert (y.cpu().double() - out).abs().max() <= 1e-4 * out.abs().max()
+    for name, t in p64.items():
+        assert (got[name].cpu().double() - t.grad).abs().max() <= 1e-4 * t.grad.abs().max(), name
+    with torch.no_grad():                     # differences along one direction of every tensor
+        for name in P:
+            step = torch.randn(P[name].shape, generator=g).double()
+            e = 1e-5
+            up, down = ({**p64, name: p64[name] + s * e * step} for s in (1, -1))
+            slope = ((block(up) - block(down)) * dy.cpu().double()).sum() / (2 * e)
+            have = (got[name].cpu().double() * step).sum()
+            scale = (got[name].cpu().double() * step).abs().sum()
+            assert (slope - have).abs() <= 1e-4 * scale, name
