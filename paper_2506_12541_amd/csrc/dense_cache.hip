@@ -370,7 +370,10 @@ __device__ __forceinline__ int clear_bytes(uint8_t* t, int lane) {
 }
 
 // Many rows: as packed_fwd_kernel of dense_attn.hip, the tiles of keys and values converted to bf16 as they are
-// stored in LDS, once for the workgroup.
+// stored in LDS, once for the workgroup. Bound by the matrix cores and the exponentials beside them: two waves share a
+// SIMD (one register more than 256 leaves one: chunks of 200 to 1024 rows against 1024 to 8192, 252 us, so 173), and the one
+// that multiplies goes first (166). 4 x 1024 rows against 8192, 32 heads of 128: 586 us, 880 TFLOP/s; packed_fwd_kernel on bf16
+// caches 542.
 template <typename T, int HD, int QB>
 __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP cp) {
   constexpr int NW = kWaves, KT = 64, KB = KT / 16, NCH = HD / 32, DB = HD / 16, R = 16 * QB * NW, P = parts_of<T>();
@@ -427,6 +430,7 @@ __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP c
     const bool more = t0 + KT < k_hi;
     if (more) load(t0 + KT);
     f32x4 s[QB][KB];
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -438,6 +442,7 @@ __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP c
           for (int x = P - 1; x >= 0; --x)      // the small parts first
             s[qb][kb] = mma(kf, qf[qb][c][x], c == 0 && x == P - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qb][kb]);
       }
+    __builtin_amdgcn_s_setprio(0);
     bf16x8 pf[QB][KB / 2][P];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -478,6 +483,7 @@ __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP c
         to_parts<P>(v8, pf[qb][kp]);
       }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -488,6 +494,7 @@ __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP c
 #pragma unroll
           for (int x = P - 1; x >= 0; --x) o[qb][db] = mma(vf, pf[qb][kp][x], o[qb][db]);
       }
+    __builtin_amdgcn_s_setprio(0);
     if (more) {     // the tile before this one has been read by every wave (the barrier)
       kt.store(kn, wid, lane);
       vt.store(vn, wid, lane);
@@ -898,7 +905,7 @@ hipError_t launch_cache_attention(const AttnArgs& a, const void* q, const void* 
   const FwdPlan f = cache_plan(a);
   CacheFwdP p{FwdP{a, q, ck, cv, SeqArgs{cu_q, cu_k, used_k, a.seqs, a.total_q, a.total_k}, group_of(a), o, lse,
                    a.scale * kLog2e, f.nsplit, nullptr, nullptr},
-              ek, ev, (int)((a.total_k / a.seqs + f.nsplit - 1) / f.nsplit + 63) / 64 * 64};
+              ek, ev, std::max((int)((a.total_k / a.seqs + f.nsplit - 1) / f.nsplit + 63) / 64 * 64, 64)};
   if (f.nsplit > 1) {
     p.f.part = (float*)ws;
     p.f.ml = (float2*)((char*)ws + align256((size_t)f.nsplit * a.total_q * a.heads * a.hd * sizeof(float)));

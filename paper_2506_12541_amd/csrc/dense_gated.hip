@@ -356,7 +356,9 @@ LinearArgs rows_of(const GatedArgs& a) { return LinearArgs{a.m, a.k, 2 * a.n, a.
 // 178, 357; 1024 x 1024 -> 2 x 1024: 40, 84 and 38, 99; 2048 x 512 -> 2 x 1024: 38, 87 and 33, 101; 300 x 4096 -> 2 x 4096: 218,
 // 378 and 176, 436; 20000 x 256 -> 2 x 256: 56, 134 and 60, 129; 65536 x 64 -> 2 x 1024: 275, 728 and 313, 677.
 bool bwd_planes(const GatedArgs& a) {
-  return !a.bf16 && a.m >= 768 && a.n >= 512 && a.k >= 256 && a.k <= (1 << 22) && a.n <= (1 << 21);
+  const long long most = 1LL << 35;     // launches of fewer than 2^23 workgroups
+  return !a.bf16 && a.m >= 768 && a.n >= 512 && a.k >= 256 && a.k <= (1 << 22) && a.n <= (1 << 21) && a.m * a.n <= most &&
+         a.m * a.k <= most && (long long)a.n * a.k <= most;
 }
 bool fwd_planes(const GatedArgs& a) { return bwd_planes(a) && a.m * a.n >= (3LL << 29) / a.k; }
 size_t planes_bytes(long long rows, long long cols) { return align256(3 * sizeof(bf16_t) * (size_t)(up32(rows) * up32(cols))); }

@@ -1045,8 +1045,8 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
   if constexpr (sizeof(T) == 2 && G) {
     // A gated tile's epilogue is long: over short contractions 256 x 128 tiles, two to a CU, let one write while the other
     // multiplies (65536 x 512 -> 2 x 2048: 338 us, 256 x 256 350; 65536 x 256 -> 2 x 512: 57 and 65; 16384 x 1024 -> 2 x 1024: 77 and 71).
-    if (dma && side == 256 && K <= 512 && p.S == 1) {
-      const int nn = (N + 63) / 64;
+    const int nn = (N + 63) / 64;
+    if (dma && side == 256 && K <= 512 && p.S == 1 && (long long)ntm * nn < 1 << 23) {
       product_dma_kernel<TA, TB, 256, 128, 4, 2, 32, 3, G><<<(unsigned)((long long)ntm * nn), 512, 0, st>>>(a, b, K, ntm, nn, (int)(K / 32), o);
       return hipGetLastError();
     }

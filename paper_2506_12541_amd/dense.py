@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
+import operator
 from typing import NamedTuple
 
 import torch
@@ -32,7 +33,7 @@ _HERE = contextlib.nullcontext()
 
 
 # Parameter records of calls whose arguments have passed the checks, by all that the checks read of them (shapes, strides,
-# types, devices, numbers; never addresses or values). The calls of a serving step are as short on the GPU as their
+# types, devices, plain numbers; never addresses or values of tensors). The calls of a serving step are as short on the GPU as their
 # host path is long: with it a rotary_forward of 32 tokens takes 8 us of the host, without 14.
 _checked = {}
 
@@ -382,6 +383,7 @@ def rotary_forward(q, k, positions, freq, gain_q=None, gain_k=None, eps: float =
     projection are fine. Returns (y_q, y_k), which may be given: q and k themselves too."""
     lib = _lib.load()
     sig = _signature
+    eps, interleaved, magnitude = float(eps), bool(interleaved), float(magnitude)
     try:
         key = ("rotary_forward", sig(q), sig(k), sig(positions), sig(freq), sig(gain_q), sig(gain_k), eps, interleaved,
                magnitude, sig(y_q), sig(y_k))
@@ -417,6 +419,7 @@ def rotary_backward(dy_q, dy_k, positions, freq, q=None, k=None, gain_q=None, ga
     dy_k themselves."""
     lib = _lib.load()
     sig = _signature
+    eps, interleaved, magnitude = float(eps), bool(interleaved), float(magnitude)
     try:
         key = ("rotary_backward", sig(dy_q), sig(dy_k), sig(positions), sig(freq), sig(q), sig(k), sig(gain_q), sig(gain_k), eps,
                interleaved, magnitude, sig(dq), sig(dk))
@@ -655,6 +658,7 @@ def cache_read(cache, rows: int, cu_q, cu_k, used_k=None, dtype=torch.bfloat16, 
     (bfloat16 or float32; exact in both). Rows in no sequence are 0. With cu_q the running sum of used_k: all that
     the caches hold."""
     lib = _lib.load()
+    rows = operator.index(rows)
     try:
         key = _call_key("cache_read", cache, cu_q, cu_k, used_k, rows, dtype)
         p = _checked.get(key)
@@ -687,6 +691,7 @@ def cache_attention_forward(q, cache, cu_q, cu_k, used_k=None, causal: bool = Fa
     lib = _lib.load()
     if (o is None) != (lse is None):
         raise ValueError("pass both o and lse, or neither")
+    causal, softmax_scale = bool(causal), float(softmax_scale)
     try:
         key = _call_key("cache_attention_forward", cache, cu_q, cu_k, used_k, _signature(q), causal, softmax_scale, _signature(o),
                         _signature(lse))
@@ -701,7 +706,7 @@ def cache_attention_forward(q, cache, cu_q, cu_k, used_k=None, causal: bool = Fa
         rows, kv, _ = cache.k.shape
         if cache.k.shape[2] != d or kv == 0:
             raise ValueError(f"the cache must have head_dim {d} and at least one head, got {tuple(cache.k.shape)}")
-        p = _lib.bsa_attention_t(_offsets(cu_q, cu_k, used_k, dev), h, kv, d, tq, rows, int(bool(causal)), _CODES[dt],
+        p = _lib.bsa_attention_t(_offsets(cu_q, cu_k, used_k, dev), h, kv, d, tq, rows, int(causal), _CODES[dt],
                                  softmax_scale, int(o is None), q_row, q_head, *strides, 0, 0, 0, 0)
         if o is not None:
             p.o_row, p.o_head = _heads(o, "o", dt, dev, q.shape)

@@ -747,3 +747,26 @@ def test_block_forward_and_backward_together():
             have = (got[name].cpu().double() * step).sum()
             scale = (got[name].cpu().double() * step).abs().sum()
             assert (slope - have).abs() <= 1e-4 * scale, name
+
+
+def test_numbers_given_as_tensors_are_read_at_each_call():
+    """Calls remember checked arguments by shapes and numbers: a tensor that stands for a number counts by its value."""
+    g = gen(30)
+    q, k, _, _, at, freq, _ = rotary_args(g, F32, 5, 2, 1, 32, 32, norm=False)
+    scale = torch.tensor(1.0)
+    a, _ = dense.rotary_forward(q, k, at, freq, magnitude=scale)
+    scale.fill_(2.0)
+    b, _ = dense.rotary_forward(q, k, at, freq, magnitude=scale)
+    assert torch.equal(b, 2 * a)
+    cache, _, _ = filled(g, 64, 1, 32)
+    rows, c = torch.tensor(64), cu([64])
+    assert dense.cache_read(cache, rows, c, c)[0].shape[0] == 64
+    rows.fill_(7)
+    assert dense.cache_read(cache, rows, cu([7]), cu([64]), ints([7]))[0].shape[0] == 7
+
+
+def test_cache_attention_more_sequences_than_rows():
+    g = gen(31)
+    check_cache_attention(g, "bf16", [1] * 6, [1, 0, 0, 2, 0, 0], None, 2, 1, 32, True)
+    check_cache_attention(g, "bf16", [2] * 70, [0, 1] * 35, None, 2, 2, 32, True)
+    check_cache_attention(g, "bf16", [3, 2], [0, 0], None, 2, 2, 64, False)
