@@ -166,32 +166,34 @@ __device__ __forceinline__ void parts_plain(const PlaneMat& a, const PlaneMat& b
   }
 }
 
-// 128 x 128 tiles of 2 x 4 waves, contraction tiles of 32 in a ring of three LDS stages of 48 KB: one workgroup to a CU,
-// two waves to a SIMD (4 waves of 64 x 64 read less from LDS, but nothing runs while one waits).
-template <bool TA, bool TB, bool G>
-__global__ void __launch_bounds__(512) parts_kernel(PlaneMat a, PlaneMat b, int nkt, int ntm, int ntn, int kt_per,
+// BM x 128 tiles of 8 waves, contraction tiles of 32: BM = 256, waves of 64 x 64 and two LDS stages of 72 KB, or BM = 128,
+// waves of 64 x 32 (more LDS reads for a product) and three stages of 48 KB. One workgroup to a CU, two waves to a SIMD
+// (4 waves of 64 x 64 on 128 x 128 tiles read less, but nothing runs while one waits: 14 % slower). 16384 x 1024 -> 2 x 2048: 713 us
+// with 256 rows (193 TFLOP/s), 767 with 128; 3586 x 515 -> 2 x 1029: 57 and 62 of the forward's 61 and 67.
+template <bool TA, bool TB, bool G, int BM>
+__global__ void __launch_bounds__(512, 2) parts_kernel(PlaneMat a, PlaneMat b, int nkt, int ntm, int ntn, int kt_per,
                                                        const int* fa, int nfa, const int* fb, int nfb, Epi<float> o) {
-  constexpr int BT = 128, BK = 32, FI = 4, FJ = 2, TILE = BT * BK;
+  constexpr int BN = 128, BK = 32, NS = BM == 256 ? 2 : 3, WN = BM == 256 ? 2 : 4, FI = 4, FJ = 8 / WN;
+  constexpr int AT = BM * BK, BT = BN * BK;
   // a stage is an array of its own: reads of one stage do not wait for loads into another
-  __shared__ __attribute__((aligned(1024))) bf16_t st0[2][3][TILE], st1[2][3][TILE], st2[2][3][TILE];
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wid >> 2, wn = wid & 3;
+  __shared__ __attribute__((aligned(1024))) bf16_t st0[3 * (AT + BT)], st1[3 * (AT + BT)], st2[NS == 3 ? 3 * (AT + BT) : 8];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wid / WN, wn = wid % WN;
   // XCDs take contiguous runs of tiles, in bands of 8 tile rows walked column by column (product_dma_kernel)
   const int nt = ntm * ntn;
   int id = blockIdx.x;
   if ((nt & 7) == 0) id = (id & 7) * (nt >> 3) + (id >> 3);
   const int band = id / (8 * ntn), in = id - band * 8 * ntn, bh = min(8, ntm - 8 * band);
   const int tm = 8 * band + in % bh, tn = in / bh;
-  const long long m0 = (long long)tm * BT, n0 = (long long)tn * BT;
+  const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
   const int kt0 = min((int)blockIdx.y * kt_per, nkt), kt1 = min(kt0 + kt_per, nkt);
-  DmaTile<TA, TA != TB, TA ? BK : BT, TA ? BT : BK, 8> la;
-  DmaTile<TB, TA != TB, TB ? BK : BT, TB ? BT : BK, 8, G> lb;
+  DmaTile<TA, TA != TB, TA ? BK : BM, TA ? BM : BK, 8> la;
+  DmaTile<TB, TA != TB, TB ? BK : BN, TB ? BN : BK, 8, G> lb;
   la.init(a.m, m0, wid, lane);
   lb.init(b.m, n0, wid, lane);
   constexpr int PER = 3 * (decltype(la)::NU + decltype(lb)::NU);
-  typedef bf16_t Stage[2][3][TILE];
-  auto issue = [&](int kt, Stage& st, int k) __attribute__((always_inline)) {
-    la.issue(st[0][k], a.m, (long long)kt * BK, wid, 2 * k * a.plane);
-    lb.issue(st[1][k], b.m, (long long)kt * BK, wid, 2 * k * b.plane);
+  auto issue = [&](int kt, bf16_t* st, int k) __attribute__((always_inline)) {
+    la.issue(st + k * AT, a.m, (long long)kt * BK, wid, 2 * k * a.plane);
+    lb.issue(st + 3 * AT + k * BT, b.m, (long long)kt * BK, wid, 2 * k * b.plane);
   };
   f32x4 acc[FI][FJ];
 #pragma unroll
@@ -199,11 +201,11 @@ __global__ void __launch_bounds__(512) parts_kernel(PlaneMat a, PlaneMat b, int 
 #pragma unroll
     for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   bf16x8 af[3][FI], bf[3][FJ];
-  auto read_a = [&](const Stage& st, int k) __attribute__((always_inline)) {
-    Frags<TA, TA != TB, BK, BT, FI>::read(st[0][k], wm * 64, 0, lane, af[k]);
+  auto read_a = [&](const bf16_t* st, int k) __attribute__((always_inline)) {
+    Frags<TA, TA != TB, BK, BM, FI>::read(st + k * AT, wm * 64, 0, lane, af[k]);
   };
-  auto read_b = [&](const Stage& st, int k) __attribute__((always_inline)) {
-    Frags<TB, TA != TB, BK, BT, FJ>::read(st[1][k], wn * 32, 0, lane, bf[k]);
+  auto read_b = [&](const bf16_t* st, int k) __attribute__((always_inline)) {
+    Frags<TB, TA != TB, BK, BN, FJ>::read(st + 3 * AT + k * BT, wn * 16 * FJ, 0, lane, bf[k]);
   };
   auto multiply = [&](int ka, int kb) {
 #pragma unroll
@@ -211,52 +213,62 @@ __global__ void __launch_bounds__(512) parts_kernel(PlaneMat a, PlaneMat b, int 
 #pragma unroll
       for (int j = 0; j < FJ; ++j) acc[i][j] = mma(bf[kb][j], af[ka][i], acc[i][j]);
   };
-  // tile t lies in stage c; the one before c is free
-  auto step = [&](int t, const Stage& c, Stage& free) __attribute__((always_inline)) {
-    // tile t has landed once at most the tile issued after it is in flight
-    if (t + 1 < kt1)
+  // tile t lies in stage c; the stage `free` has been read. NS - 2 tiles stay in flight while t is waited for
+  auto step = [&](int t, const bf16_t* c, bf16_t* free) __attribute__((always_inline)) {
+    if (NS == 3 && t + 1 < kt1)
       vm_wait<PER>();
     else
       vm_drain();
     lds_barrier();     // every wave's loads of tile t are visible, and it has its fragments of t - 1
+    const int next = t + NS - 1;
     // the small part products first; the next loads between the products, so that no wave queues for all of them
-    const bool more = t + 2 < kt1;
+    const bool more = next < kt1;
     read_a(c, 2);
     read_b(c, 0);
     multiply(2, 0);
-    if (more) issue(t + 2, free, 0);
+    if (more) issue(next, free, 0);
     read_a(c, 0);
     read_b(c, 2);
     multiply(0, 2);
-    if (more) issue(t + 2, free, 1);
+    if (more) issue(next, free, 1);
     read_a(c, 1);
     read_b(c, 1);
     multiply(1, 1);
-    if (more) issue(t + 2, free, 2);
+    if (more) issue(next, free, 2);
     multiply(1, 0);
     multiply(0, 1);
     multiply(0, 0);
     lgkm_drain();
   };
-  for (int u = 0; u < 2; ++u)
-    if (kt0 + u < kt1)
+#pragma unroll
+  for (int u = 0; u < NS - 1; ++u)
+    if (kt0 + u < kt1) {
+#pragma unroll
       for (int k = 0; k < 3; ++k) issue(kt0 + u, u ? st1 : st0, k);
-  for (int kt = kt0; kt < kt1; kt += 3) {
-    step(kt, st0, st2);
-    if (kt + 1 < kt1) step(kt + 1, st1, st0);
-    if (kt + 2 < kt1) step(kt + 2, st2, st1);
+    }
+  if constexpr (NS == 3) {
+    for (int kt = kt0; kt < kt1; kt += 3) {
+      step(kt, st0, st2);
+      if (kt + 1 < kt1) step(kt + 1, st1, st0);
+      if (kt + 2 < kt1) step(kt + 2, st2, st1);
+    }
+  } else {
+    for (int kt = kt0; kt < kt1; kt += 2) {
+      step(kt, st0, st1);
+      if (kt + 1 < kt1) step(kt + 1, st1, st0);
+    }
   }
   int odd = 0;
   for (int i = threadIdx.x; i < nfa; i += 512) odd |= fa[i];
   for (int i = threadIdx.x; i < nfb; i += 512) odd |= fb[i];
   if (__syncthreads_or(odd))
-    parts_plain<TA, TB, G, FI, FJ>(a, b, m0 + wm * 64, n0 + wn * 32, (long long)kt0 * BK, (long long)kt1 * BK, lane, acc);
+    parts_plain<TA, TB, G, FI, FJ>(a, b, m0 + wm * 64, n0 + wn * 16 * FJ, (long long)kt0 * BK, (long long)kt1 * BK, lane, acc);
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
     const long long m = m0 + wm * 64 + 16 * i + (lane & 15);
 #pragma unroll
     for (int j = 0; j < FJ; j += G ? 2 : 1) {
-      const int n = (int)n0 + wn * 32 + 16 * j + 4 * (lane >> 4);
+      const int n = (int)n0 + wn * 16 * FJ + 16 * j + 4 * (lane >> 4);
       float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
       if constexpr (G) {
         float u[4] = {acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
@@ -352,7 +364,7 @@ LinearArgs rows_of(const GatedArgs& a) { return LinearArgs{a.m, a.k, 2 * a.n, a.
 
 // Whether float32 products go through planes: where both sides of a product have several tiles that share them, and
 // the forward's one product is long enough for the pass before it. us (forward, backward) by planes and without:
-// 3586 x 515 -> 2 x 1029: 66, 168 and 78, 260; 2000 x 2048 -> 2 x 2048: 195, 385 and 218, 503; 1000 x 8192 -> 2 x 600: 152, 265 and
+// 3586 x 515 -> 2 x 1029: 61, 168 and 78, 260; 2000 x 2048 -> 2 x 2048: 175, 363 and 218, 503; 1000 x 8192 -> 2 x 600: 152, 265 and
 // 178, 357; 1024 x 1024 -> 2 x 1024: 40, 84 and 38, 99; 2048 x 512 -> 2 x 1024: 38, 87 and 33, 101; 300 x 4096 -> 2 x 4096: 218,
 // 378 and 176, 436; 20000 x 256 -> 2 x 256: 56, 134 and 60, 129; 65536 x 64 -> 2 x 1024: 275, 728 and 313, 677.
 bool bwd_planes(const GatedArgs& a) {
@@ -363,16 +375,24 @@ bool bwd_planes(const GatedArgs& a) {
 bool fwd_planes(const GatedArgs& a) { return bwd_planes(a) && a.m * a.n >= (3LL << 29) / a.k; }
 size_t planes_bytes(long long rows, long long cols) { return align256(3 * sizeof(bf16_t) * (size_t)(up32(rows) * up32(cols))); }
 
-// Splits of the contraction: as many as end first, in units of 0.1 us, at 1.2 us a tile of 128 x 128 x 32 on each of 256
-// CUs, 4 us a workgroup, and the splits' sums written and read at 4 TB/s behind another launch of 4 us.
-int planes_splits(long long M, long long N, long long K, int outs) {
-  const long long tiles = (M + 127) / 128 * ((N * outs + 127) / 128), nkt = (K + 31) / 32;
-  long long best = 0, pick = 1;
-  for (long long S = 1; S <= 16 && S <= nkt; ++S) {
-    const long long t = (tiles * S + 255) / 256 * ((nkt + S - 1) / S * 12 + 40) + (S > 1 ? 40 + S * M * N * outs / 50000 : 0);
-    if (S == 1 || t < best) best = t, pick = S;
-  }
-  return (int)pick;
+// Rows of a tile and splits of the contraction.
+struct PartsPlan {
+  int BM, S;
+};
+// What ends first, in units of 0.1 us: each of 256 CUs takes 1.2 us for a tile of 128 x 128 x 32, 1.9 for 256 x 128 x 32, 4 and 6
+// for a workgroup's start and end, and the splits' sums are written and read at 4 TB/s behind another launch of 4 us.
+PartsPlan parts_plan(long long M, long long N, long long K, int outs) {
+  const long long nkt = (K + 31) / 32;
+  long long best = 0;
+  PartsPlan p{128, 1};
+  for (int BM : {128, 256})
+    for (long long S = 1; S <= 16 && S <= nkt; ++S) {
+      const long long tiles = (M + BM - 1) / BM * ((N * outs + 127) / 128);
+      const long long t = (tiles * S + 255) / 256 * ((nkt + S - 1) / S * (BM == 128 ? 12 : 19) + (BM == 128 ? 40 : 60)) +
+                          (S > 1 ? 40 + S * M * N * outs / 50000 : 0);
+      if (best == 0 || t < best) best = t, p = PartsPlan{BM, (int)S};
+    }
+  return p;
 }
 
 struct GatedBwdWs {
@@ -380,7 +400,7 @@ struct GatedBwdWs {
   size_t w, x, flags;        // planes of w and x, and the flags of w, x and dz
   int P;
   long long rpg;
-  int Sx, Sw;                // splits of dx and dw
+  PartsPlan px, pw;          // of dx and dw
 };
 GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
   GatedBwdWs L{};
@@ -400,10 +420,10 @@ GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
     L.w = put(planes_bytes(2LL * a.n, a.k));
     L.x = put(planes_bytes(a.m, a.k));
     L.flags = put(sizeof(int) * (2 * kSplitBlocks + (size_t)gx * L.P));
-    L.Sx = planes_splits(a.m, a.k, 2LL * a.n, 1);
-    L.Sw = planes_splits(2LL * a.n, a.k, a.m, 1);
+    L.px = parts_plan(a.m, a.k, 2LL * a.n, 1);
+    L.pw = parts_plan(2LL * a.n, a.k, a.m, 1);
     auto part = [](int S, long long M, long long N) { return S > 1 ? sizeof(float) * (size_t)S * M * N : 0; };
-    L.rest = put(std::max(part(L.Sx, a.m, a.k), part(L.Sw, 2LL * a.n, a.k)));
+    L.rest = put(std::max(part(L.px.S, a.m, a.k), part(L.pw.S, 2LL * a.n, a.k)));
   } else {
     L.dz = put(esz * (size_t)a.m * 2 * a.n);
     L.rest = put(linear_bwd_ws_bytes(rows_of(a)));
@@ -423,12 +443,17 @@ PlaneMat plane_mat(const void* p, long long rows, long long cols, bool column) {
 
 // C = A B^T of planes; S > 1: partial sums in part, joined by split_sum_kernel
 template <bool TA, bool TB, bool G>
-hipError_t parts_product(const PlaneMat& a, const PlaneMat& b, long long M, int N, long long K, int S, float* part, const int* fa,
+hipError_t parts_product(const PlaneMat& a, const PlaneMat& b, long long M, int N, long long K, PartsPlan p, float* part, const int* fa,
                          int nfa, const int* fb, int nfb, Epi<float> o, hipStream_t st) {
+  const int S = p.S;
   o.part = S > 1 ? part : nullptr;
-  const int nkt = (int)(up32(K) / 32), ntm = (int)((M + 127) / 128), ntn = G ? (N + 63) / 64 : (N + 127) / 128;
-  parts_kernel<TA, TB, G><<<dim3((unsigned)((long long)ntm * ntn), (unsigned)S), 512, 0, st>>>(a, b, nkt, ntm, ntn, (nkt + S - 1) / S,
-                                                                                               fa, nfa, fb, nfb, o);
+  const int nkt = (int)(up32(K) / 32), ntm = (int)((M + p.BM - 1) / p.BM), ntn = G ? (N + 63) / 64 : (N + 127) / 128;
+  const dim3 grid((unsigned)((long long)ntm * ntn), (unsigned)S);
+  const int per = (nkt + S - 1) / S;
+  if (p.BM == 256)
+    parts_kernel<TA, TB, G, 256><<<grid, 512, 0, st>>>(a, b, nkt, ntm, ntn, per, fa, nfa, fb, nfb, o);
+  else
+    parts_kernel<TA, TB, G, 128><<<grid, 512, 0, st>>>(a, b, nkt, ntm, ntn, per, fa, nfa, fb, nfb, o);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || S == 1) return e;
   o.part = nullptr;
@@ -439,18 +464,18 @@ hipError_t parts_product(const PlaneMat& a, const PlaneMat& b, long long M, int 
 
 struct GatedFwdWs {
   size_t x, w, flags, part, total;
-  int S;
+  PartsPlan p;
 };
 GatedFwdWs gated_fwd_layout(const GatedArgs& a) {
   GatedFwdWs L{};
   size_t off = 0;
   auto put = [&](size_t b) { const size_t o = off; off += align256(b); return o; };
   if (fwd_planes(a)) {
-    L.S = planes_splits(a.m, a.n, a.k, 2);
+    L.p = parts_plan(a.m, a.n, a.k, 2);
     L.x = put(planes_bytes(a.m, a.k));
     L.w = put(planes_bytes(2LL * a.n, a.k));
     L.flags = put(sizeof(int) * 2 * kSplitBlocks);
-    L.part = put(L.S > 1 ? sizeof(float) * (size_t)L.S * a.m * 2 * a.n : 0);
+    L.part = put(L.p.S > 1 ? sizeof(float) * (size_t)L.p.S * a.m * 2 * a.n : 0);
   } else if (!few_rows_ok(a.m, a.k)) {
     L.part = put(plan_bytes(fwd_plan(a), a.m, 2LL * a.n));
   }
@@ -470,7 +495,7 @@ hipError_t planes_fwd(const GatedArgs& a, const void* x, const void* w, const Ep
                                  planes_of((const float*)w, a.ldw, 2LL * a.n, a.k, ws + L.w, flags + kSplitBlocks), st);
   if (e != hipSuccess) return e;
   return parts_product<false, false, true>(plane_mat(ws + L.x, a.m, a.k, false), plane_mat(ws + L.w, 2LL * a.n, a.k, false), a.m, a.n,
-                                           a.k, L.S, (float*)(ws + L.part), flags, kSplitBlocks, flags + kSplitBlocks, kSplitBlocks,
+                                           a.k, L.p, (float*)(ws + L.part), flags, kSplitBlocks, flags + kSplitBlocks, kSplitBlocks,
                                            o, st);
 }
 
@@ -490,13 +515,13 @@ hipError_t planes_bwd(const GatedArgs& a, const GatedBwdWs& L, const void* x, co
   if (dx) {
     const Epi<float> o{a.m, a.k, (float*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
     e = parts_product<false, true, false>(plane_mat(ws + L.dz, a.m, 2LL * a.n, false), plane_mat(ws + L.w, 2LL * a.n, a.k, true), a.m,
-                                          a.k, 2LL * a.n, L.Sx, (float*)(ws + L.rest), fz, gx * L.P, fw, kSplitBlocks, o, st);
+                                          a.k, 2LL * a.n, L.px, (float*)(ws + L.rest), fz, gx * L.P, fw, kSplitBlocks, o, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
     const Epi<float> o{2LL * a.n, a.k, (float*)dw, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
     e = parts_product<true, true, false>(plane_mat(ws + L.dz, a.m, 2LL * a.n, true), plane_mat(ws + L.x, a.m, a.k, true), 2LL * a.n,
-                                         a.k, a.m, L.Sw, (float*)(ws + L.rest), fz, gx * L.P, fx, kSplitBlocks, o, st);
+                                         a.k, a.m, L.pw, (float*)(ws + L.rest), fz, gx * L.P, fx, kSplitBlocks, o, st);
   }
   return e;
 }
