@@ -355,6 +355,118 @@ __global__ void __launch_bounds__(256) gated_dz_planes_kernel(const float* __res
   }
 }
 
+// ---- gradients of few rows: the weight is read, and its gradient written, once ----
+//
+// Float32 with up to 16 rows is no work for the matrix cores: 16 multiply-adds for a value of w, or of dw, keep up
+// with memory. A lane holds 16 bytes of columns; a row's dz are the same for all lanes and come from LDS. MR: rows
+// that are computed (m of them are there). Both kernels are bound by memory: w of 10880 x 7168 and 4 rows 150 us
+// with all other launches, 4.2 TB/s for w and dw (the tiles: 305 us).
+
+constexpr int kFewChunk = 64;    // rows of w whose dz are staged at a time
+
+// zs[j][i] = dz[i][r0 + j], 0 behind the ends.
+template <int MR>
+__device__ __forceinline__ void stage_dz(float (&zs)[kFewChunk][MR], const float* dz, int m, int n2, int r0, int r1) {
+  for (int i = threadIdx.x; i < kFewChunk * MR; i += 256) {
+    const int row = i / kFewChunk, j = i % kFewChunk;
+    zs[j][row] = row < m && r0 + j < r1 ? dz[(long long)row * n2 + r0 + j] : 0.f;
+  }
+}
+
+// dx = dz w: the workgroup's columns 64 E blockIdx.x .. of the rows [r0, r1) of w that blockIdx.y takes; its waves
+// take them in turn and are joined in order.
+template <int MR>
+__global__ void __launch_bounds__(256) few_dx_kernel(const float* __restrict__ dz, const float* __restrict__ w, long long ldw, int m,
+                                                     int k, int n2, int per, Epi<float> o) {
+  constexpr int E = 4, U = 4;
+  __shared__ __attribute__((aligned(16))) float zs[kFewChunk][MR], red[4][64 * E + 4];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (blockIdx.x * 64 + lane) * E, left = k - c;
+  const int r0 = blockIdx.y * per, r1 = min(r0 + per, n2);
+  float acc[MR][E];
+#pragma unroll
+  for (int i = 0; i < MR; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[i][e] = 0.f;
+  for (int b = r0; b < r1; b += kFewChunk) {
+    __syncthreads();
+    stage_dz<MR>(zs, dz, m, n2, b, r1);
+    __syncthreads();
+    for (int j = wid; j < kFewChunk && b + j < r1; j += 4 * U) {
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {     // rows behind the last repeat its loads and are left out below
+        const float* p = w + (long long)min(b + j + 4 * u, r1 - 1) * ldw + c;
+        v[u] = left >= E ? load16u(p) : left > 0 ? load_partial(p, left) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (b + j + 4 * u < r1) {
+          float x[E];
+          unpack16<float>(v[u], x);
+#pragma unroll
+          for (int i = 0; i < MR; ++i) {
+            const float z = zs[j + 4 * u][i];
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[i][e] = fmaf(z, x[e], acc[i][e]);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[wid][lane * E + e] = acc[i][e];
+    __syncthreads();
+    if (i < m && threadIdx.x < 16 * E) {
+      const int x = 4 * threadIdx.x;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = red[0][x + e] + red[1][x + e] + red[2][x + e] + red[3][x + e];
+      epi_store4(o, i, blockIdx.x * 64 * E + x, v, blockIdx.y);
+    }
+  }
+}
+
+// dw = dz^T x: kFewChunk rows of dw by 256 columns, its waves in turn; cols workgroups share the rows.
+template <int MR>
+__global__ void __launch_bounds__(256) few_dw_kernel(const float* __restrict__ dz, const float* __restrict__ x, long long ldx, int m,
+                                                     int k, int n2, int cols, float* __restrict__ dw) {
+  constexpr int E = 4;
+  __shared__ __attribute__((aligned(16))) float zs[kFewChunk][MR];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (blockIdx.x % cols * 64 + lane) * E, left = k - c, r0 = blockIdx.x / cols * kFewChunk;
+  float xs[MR][E];
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    const float* p = x + min(i, m - 1) * ldx + c;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (i < m) v = left >= E ? load16u(p) : left > 0 ? load_partial(p, left) : v;
+    unpack16<float>(v, xs[i]);
+  }
+  stage_dz<MR>(zs, dz, m, n2, r0, n2);
+  __syncthreads();
+  if (left <= 0) return;
+  for (int j = wid; j < kFewChunk && r0 + j < n2; j += 4) {
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < MR; ++i) {
+      const float z = zs[j][i];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = fmaf(z, xs[i][e], v[e]);
+    }
+    float* const to = dw + (long long)(r0 + j) * k + c;
+    if (left >= E)
+      store16u(to, pack16<float>(v));
+    else
+      store_partial(to, pack16<float>(v), left);
+  }
+}
+
 // ---- host ----
 
 // The forward's product has 2n columns.
@@ -395,6 +507,39 @@ PartsPlan parts_plan(long long M, long long N, long long K, int outs) {
   return p;
 }
 
+// Float32 gradients by few_dx_kernel and few_dw_kernel. The products' tiles would work on three bf16 parts of mostly
+// empty rows, at a quarter of memory's rate; in bf16 they come to half of it and these kernels to no more. Splits of
+// dx are joined by threads that read all of them, which weighs when k is short. us (both gradients, 4 rows and 16) by
+// these kernels and by tiles: w of 8192 x 4096 69 and 87, 117 and 121; of 4096 x 2048 34 and 44, 46 and 48; of
+// 8192 x 1024 37 and 47, 47 and 50; of 4096 x 1024 28 and 39, 26 and 28; of 16384 x 512 54 and 60, 51 and 53.
+bool few_bwd(const GatedArgs& a) { return !a.bf16 && a.m <= 16 && a.k >= 1024 && 2LL * a.n * a.k >= 1 << 23; }
+// Splits of dx, in chunks of kFewChunk rows of w: about two workgroups to a CU.
+int few_splits(const GatedArgs& a) {
+  const int cols = (a.k + 255) / 256, chunks = (2 * a.n + kFewChunk - 1) / kFewChunk;
+  return std::max(1, std::min(std::min(512 / cols, chunks), 64));
+}
+
+template <int MR>
+hipError_t few_gradients(const GatedArgs& a, const float* x, const float* w, const float* dz, float* dx, float* dw, float* part,
+                         hipStream_t st) {
+  const int n2 = 2 * a.n, m = (int)a.m, cols = (a.k + 255) / 256, chunks = (n2 + kFewChunk - 1) / kFewChunk;
+  if (dw) {
+    few_dw_kernel<MR><<<(unsigned)((long long)cols * chunks), 256, 0, st>>>(dz, x, a.ldx, m, a.k, n2, cols, dw);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!dx) return hipSuccess;
+  const int S = few_splits(a), per = (chunks + S - 1) / S * kFewChunk;
+  Epi<float> o{a.m, a.k, dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, S > 1 ? part : nullptr};
+  few_dx_kernel<MR><<<dim3(cols, S), 256, 0, st>>>(dz, w, a.ldw, m, a.k, n2, per, o);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || S == 1) return e;
+  o.part = nullptr;
+  const long long n4 = a.m * ((a.k + 3) / 4);
+  split_sum_kernel<float, 1><<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(part, S, o);
+  return hipGetLastError();
+}
+
 struct GatedBwdWs {
   size_t dz, dbp, rest, total;
   size_t w, x, flags;        // planes of w and x, and the flags of w, x and dz
@@ -426,7 +571,7 @@ GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
     L.rest = put(std::max(part(L.px.S, a.m, a.k), part(L.pw.S, 2LL * a.n, a.k)));
   } else {
     L.dz = put(esz * (size_t)a.m * 2 * a.n);
-    L.rest = put(linear_bwd_ws_bytes(rows_of(a)));
+    L.rest = put(few_bwd(a) ? sizeof(float) * (size_t)few_splits(a) * a.m * a.k : linear_bwd_ws_bytes(rows_of(a)));
   }
   L.total = off;
   return L;
@@ -556,7 +701,12 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!planes) {    // without rows this also clears db
+  if (a.m > 0 && few_bwd(a)) {
+    const auto f = a.m <= 4 ? few_gradients<4> : a.m <= 8 ? few_gradients<8> : few_gradients<16>;
+    const hipError_t e =
+        f(a, (const float*)x, (const float*)w, (const float*)dz, (float*)dx, (float*)dw, (float*)(c + L.rest), st);
+    if (e != hipSuccess) return e;
+  } else if (!planes) {    // without rows this also clears db
     const hipError_t e = launch_linear_bwd(rows_of(a), x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
     if (e != hipSuccess) return e;
   }

@@ -377,6 +377,40 @@ def test_gated_float32_planes(m, k, n):
     check_gated(gen(m), "f32", m, k, n, "silu", True)
 
 
+@pytest.mark.parametrize("m,k,n", [(1, 1024, 4096), (4, 1027, 4099), (5, 70001, 61), (8, 2052, 2050), (9, 4097, 1031),
+                                   (16, 1100, 4000)])
+def test_gated_float32_few_rows(m, k, n):
+    """Sizes at which float32 gradients of few rows read the weight, and write its gradient, once."""
+    check_gated(gen(m), "f32", m, k, n, "silu" if m % 2 else "gelu", True)
+
+
+def test_gated_float32_few_rows_strides_parts_and_values_that_are_not_finite():
+    g, (m, k, n) = gen(6), (7, 1030, 4100)
+    x, w, dy = normal(g, m, k), normal(g, 2 * n, k, scale=0.1), normal(g, m, n)
+    x[1, k - 1], w[n, 3] = math.inf, 0.0
+    dy[3, 5], dy[4, 7] = math.nan, math.inf
+    _, pre = dense.gated_forward(x, w, act="none", save_pre=True)
+    a = dense.gated_backward(x, w, dy, pre, act="none", bias=True)
+    assert a["dx"][3].isnan().all() and not a["dx"][4].isfinite().any() and not a["dx"][1].isfinite().any()
+    rest = [0, 2, 5, 6]
+    some = dense.gated_backward(x[rest], w, dy[rest], pre[rest], act="none")["dx"]
+    assert some.isfinite().all() and torch.equal(a["dx"][rest], some)
+    assert not a["dw"].isfinite().any()      # every pre of row 1 is infinite, so its part of each dw is not finite
+    rest = [0, 2, 3, 4, 5, 6]
+    bad = ~dense.gated_backward(x[rest], w, dy[rest], pre[rest], act="none")["dw"].isfinite()
+    assert bad[[5, 7, n + 5, n + 7]].all() and not bad.index_fill(0, torch.tensor([5, 7, n + 5, n + 7], device="cuda"), False).any()
+    wide_x, wide_w, wide_dy = (torch.full((t.shape[0], t.shape[1] + 3), math.nan, device="cuda") for t in (x, w, dy))
+    for wide, t in ((wide_x, x), (wide_w, w), (wide_dy, dy)):
+        wide[:, :t.shape[1]] = t
+    b = dense.gated_backward(wide_x[:, :k], wide_w[:, :k], wide_dy[:, :n], pre, act="none", bias=True)
+    for name in a:
+        assert torch.allclose(a[name], b[name], rtol=0, atol=0, equal_nan=True)
+    for kw in (dict(need_dx=False), dict(need_dw=False), dict(need_dx=False, need_dw=False, bias=True)):
+        part = dense.gated_backward(x, w, dy, pre, act="none", **kw)
+        for name in ("dx", "dw", "db"):
+            assert part[name] is None or torch.allclose(part[name], a[name], rtol=0, atol=0, equal_nan=True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m,k,n", [(200, 136, 132), (900, 264, 520)])
 def test_gated_strides_and_parts(dtype, m, k, n):
