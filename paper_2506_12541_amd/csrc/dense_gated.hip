@@ -357,10 +357,10 @@ __global__ void __launch_bounds__(256) gated_dz_planes_kernel(const float* __res
 
 // ---- gradients of few rows: the weight is read, and its gradient written, once ----
 //
-// Float32 with up to 16 rows is no work for the matrix cores: 16 multiply-adds for a value of w, or of dw, keep up
-// with memory. A lane holds 16 bytes of columns; a row's dz are the same for all lanes and come from LDS. MR: rows
-// that are computed (m of them are there). Both kernels are bound by memory: w of 10880 x 7168 and 4 rows 150 us
-// with all other launches, 4.2 TB/s for w and dw (the tiles: 305 us).
+// Float32 with few rows is no work for the matrix cores: 16 multiply-adds for a value of w, or of dw, keep up with
+// memory. A lane holds 16 bytes of columns; a row's dz are the same for all lanes and come from LDS. MR: rows that are
+// computed (m of them are there). Both kernels are bound by memory: 2 rows and w of 10880 x 7168, which takes 60 us at
+// a copy's rate, dx 64 us and dw 58, each with the launches before and behind it.
 
 constexpr int kFewChunk = 64;    // rows of w whose dz are staged at a time
 
@@ -507,12 +507,13 @@ PartsPlan parts_plan(long long M, long long N, long long K, int outs) {
   return p;
 }
 
-// Float32 gradients by few_dx_kernel and few_dw_kernel. The products' tiles would work on three bf16 parts of mostly
-// empty rows, at a quarter of memory's rate; in bf16 they come to half of it and these kernels to no more. Splits of
-// dx are joined by threads that read all of them, which weighs when k is short. us (both gradients, 4 rows and 16) by
-// these kernels and by tiles: w of 8192 x 4096 69 and 87, 117 and 121; of 4096 x 2048 34 and 44, 46 and 48; of
-// 8192 x 1024 37 and 47, 47 and 50; of 4096 x 1024 28 and 39, 26 and 28; of 16384 x 512 54 and 60, 51 and 53.
-bool few_bwd(const GatedArgs& a) { return !a.bf16 && a.m <= 16 && a.k >= 1024 && 2LL * a.n * a.k >= 1 << 23; }
+// Whether float32 gradients of few rows go through few_dw_kernel and few_dx_kernel. The products' tiles would be mostly
+// empty rows. dw, us by the kernel and by tiles: 16 rows, w of 8192 x 4096 39 and 73, 4096 x 2048 19 and 27, 2048 x 1024
+// 18 and 17; 32 rows 64 and 78, 25 and 29, 22 and 16. dx reads all splits once more to join them, which weighs when k is
+// short: 8 rows, w of 10880 x 7168 74 and 110, 8192 x 4096 44 and 50, 4096 x 2048 23 and 22, 16384 x 512 34 and 28; 2 rows
+// 64 and 114, 40 and 52, 19 and 21, 29 and 27; 16 rows 92 and 112, 53 and 52, 30 and 23, 44 and 29.
+bool few_dw(const GatedArgs& a) { return !a.bf16 && a.m <= 16; }
+bool few_dx(const GatedArgs& a) { return !a.bf16 && a.m <= 8 && a.k >= 1024 && 2LL * a.n * a.k >= 1 << 24; }
 // Splits of dx, in chunks of kFewChunk rows of w: about two workgroups to a CU.
 int few_splits(const GatedArgs& a) {
   const int cols = (a.k + 255) / 256, chunks = (2 * a.n + kFewChunk - 1) / kFewChunk;
@@ -520,18 +521,24 @@ int few_splits(const GatedArgs& a) {
 }
 
 template <int MR>
-hipError_t few_gradients(const GatedArgs& a, const float* x, const float* w, const float* dz, float* dx, float* dw, float* part,
-                         hipStream_t st) {
-  const int n2 = 2 * a.n, m = (int)a.m, cols = (a.k + 255) / 256, chunks = (n2 + kFewChunk - 1) / kFewChunk;
-  if (dw) {
-    few_dw_kernel<MR><<<(unsigned)((long long)cols * chunks), 256, 0, st>>>(dz, x, a.ldx, m, a.k, n2, cols, dw);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (!dx) return hipSuccess;
-  const int S = few_splits(a), per = (chunks + S - 1) / S * kFewChunk;
+void few_dw_rows(const GatedArgs& a, const float* x, const float* dz, float* dw, hipStream_t st) {
+  const int cols = (a.k + 255) / 256, chunks = (2 * a.n + kFewChunk - 1) / kFewChunk;
+  few_dw_kernel<MR><<<(unsigned)((long long)cols * chunks), 256, 0, st>>>(dz, x, a.ldx, (int)a.m, a.k, 2 * a.n, cols, dw);
+}
+hipError_t few_dw_run(const GatedArgs& a, const float* x, const float* dz, float* dw, hipStream_t st) {
+  (a.m <= 4 ? few_dw_rows<4> : a.m <= 8 ? few_dw_rows<8> : few_dw_rows<16>)(a, x, dz, dw, st);
+  return hipGetLastError();
+}
+
+template <int MR>
+void few_dx_rows(const GatedArgs& a, const float* w, const float* dz, int S, const Epi<float>& o, hipStream_t st) {
+  const int cols = (a.k + 255) / 256, chunks = (2 * a.n + kFewChunk - 1) / kFewChunk, per = (chunks + S - 1) / S * kFewChunk;
+  few_dx_kernel<MR><<<dim3(cols, S), 256, 0, st>>>(dz, w, a.ldw, (int)a.m, a.k, 2 * a.n, per, o);
+}
+hipError_t few_dx_run(const GatedArgs& a, const float* w, const float* dz, float* dx, float* part, hipStream_t st) {
+  const int S = few_splits(a);
   Epi<float> o{a.m, a.k, dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, S > 1 ? part : nullptr};
-  few_dx_kernel<MR><<<dim3(cols, S), 256, 0, st>>>(dz, w, a.ldw, m, a.k, n2, per, o);
+  (a.m <= 4 ? few_dx_rows<4> : few_dx_rows<8>)(a, w, dz, S, o, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || S == 1) return e;
   o.part = nullptr;
@@ -571,7 +578,8 @@ GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
     L.rest = put(std::max(part(L.px.S, a.m, a.k), part(L.pw.S, 2LL * a.n, a.k)));
   } else {
     L.dz = put(esz * (size_t)a.m * 2 * a.n);
-    L.rest = put(few_bwd(a) ? sizeof(float) * (size_t)few_splits(a) * a.m * a.k : linear_bwd_ws_bytes(rows_of(a)));
+    const size_t own = few_dx(a) ? sizeof(float) * (size_t)few_splits(a) * a.m * a.k : 0;
+    L.rest = put(few_dx(a) && few_dw(a) ? own : std::max(own, linear_bwd_ws_bytes(rows_of(a))));
   }
   L.total = off;
   return L;
@@ -701,12 +709,19 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.m > 0 && few_bwd(a)) {
-    const auto f = a.m <= 4 ? few_gradients<4> : a.m <= 8 ? few_gradients<8> : few_gradients<16>;
-    const hipError_t e =
-        f(a, (const float*)x, (const float*)w, (const float*)dz, (float*)dx, (float*)dw, (float*)(c + L.rest), st);
-    if (e != hipSuccess) return e;
-  } else if (!planes) {    // without rows this also clears db
+  if (sizeof(T) == 4 && a.m > 0) {
+    if (dw && few_dw(a)) {
+      const hipError_t e = few_dw_run(a, (const float*)x, (const float*)dz, (float*)dw, st);
+      if (e != hipSuccess) return e;
+      dw = nullptr;
+    }
+    if (dx && few_dx(a)) {
+      const hipError_t e = few_dx_run(a, (const float*)w, (const float*)dz, (float*)dx, (float*)(c + L.rest), st);
+      if (e != hipSuccess) return e;
+      dx = nullptr;
+    }
+  }
+  if (!planes && (dx || dw || a.m == 0)) {    // without rows this also clears db
     const hipError_t e = launch_linear_bwd(rows_of(a), x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
     if (e != hipSuccess) return e;
   }

@@ -1067,10 +1067,11 @@ hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long lo
     const long long per = ((K + 31) / 32 + p.S - 1) / p.S;
     // float32: 64 x 64 tiles lie three to a CU. While they do so in one round they are faster than 128 x 64 (2816 x 512
     // -> 1024, 704 tiles: 28.0 us and 30.3; 1536 x 2048 -> 2048, 768: 90 and 95); beyond, those split a quarter less
-    // (3000 x 515 -> 1029, 799: 39.7 and 34.8; 2048 x 2048 -> 2048, 1024: 119 and 102).
+    // (3000 x 515 -> 1029, 799: 39.7 and 34.8; 2048 x 2048 -> 2048, 1024: 119 and 102), unless there is no second row of
+    // them to share with (30 rows, 3116 -> 2 x 6976: 59 and 93; 42 rows, 7138 -> 2 x 3080: 65 and 100).
     if (side == 128)
       product_kernel<T, TA, TB, 128, 128, G><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
-    else if (sizeof(T) == 2 || (long long)ntm * ntn * p.S <= 768)
+    else if (sizeof(T) == 2 || ntm == 1 || (long long)ntm * ntn * p.S <= 768)
       product_kernel<T, TA, TB, 64, 64, G><<<grid, 256, 0, st>>>(a, b, K, ntn, per, o);
     else if constexpr (sizeof(T) == 4)
       product_kernel<T, TA, TB, 128, 64, G><<<dim3((unsigned)((M + 127) / 128 * ntn), (unsigned)p.S), 256, 0, st>>>(a, b, K, ntn, per, o);

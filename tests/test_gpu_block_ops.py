@@ -378,14 +378,14 @@ def test_gated_float32_planes(m, k, n):
 
 
 @pytest.mark.parametrize("m,k,n", [(1, 1024, 4096), (4, 1027, 4099), (5, 70001, 61), (8, 2052, 2050), (9, 4097, 1031),
-                                   (16, 1100, 4000)])
+                                   (16, 1100, 4000), (1, 1024, 8192), (3, 4099, 2051), (8, 70001, 121), (6, 1501, 6001)])
 def test_gated_float32_few_rows(m, k, n):
     """Sizes at which float32 gradients of few rows read the weight, and write its gradient, once."""
     check_gated(gen(m), "f32", m, k, n, "silu" if m % 2 else "gelu", True)
 
 
 def test_gated_float32_few_rows_strides_parts_and_values_that_are_not_finite():
-    g, (m, k, n) = gen(6), (7, 1030, 4100)
+    g, (m, k, n) = gen(6), (7, 1030, 8200)
     x, w, dy = normal(g, m, k), normal(g, 2 * n, k, scale=0.1), normal(g, m, n)
     x[1, k - 1], w[n, 3] = math.inf, 0.0
     dy[3, 5], dy[4, 7] = math.nan, math.inf
