@@ -616,8 +616,17 @@ __device__ __forceinline__ void store16_stream(bf16_t* p, uint4 v) {
   __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
 }
 
+__device__ __forceinline__ void store16_past(bf16_t* p, uint4 v, bool stream) {
+  if (stream)
+    store16_stream(p, v);
+  else
+    store16u(p, v);
+}
+
 // Eight consecutive columns of both maps of a gated product. The outputs are larger than the operands and do not
 // push them out of the caches: 65536 x 512 -> 2 x 2048 with [g | u] kept 461 us, so 428; 8192 x 4096 -> 2 x 8192 965 and 897.
+// Where rows do not end with a line of 64 bytes the caches have to join the pieces: 47687 x 88 -> 2 x 3208 742 us past
+// them, through them 339; -> 2 x 3201 866 and 358; 4015 x 136 -> 2 x 6683 173 and 65.
 __device__ __forceinline__ void gated_store8(const Epi<bf16_t>& o, long long m, int n, float (&g)[8], float (&u)[8], int split) {
   if (n + 8 > o.N || o.part) {
     float g0[4] = {g[0], g[1], g[2], g[3]}, g1[4] = {g[4], g[5], g[6], g[7]};
@@ -636,13 +645,14 @@ __device__ __forceinline__ void gated_store8(const Epi<bf16_t>& o, long long m, 
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] += t[e];
   }
+  const bool lines = !((o.N | o.ldo) & 31);
   if (o.pre) {
-    store16_stream(o.pre + m * 2 * o.N + n, pack16<bf16_t>(g));
-    store16_stream(o.pre + m * 2 * o.N + o.N + n, pack16<bf16_t>(u));
+    store16_past(o.pre + m * 2 * o.N + n, pack16<bf16_t>(g), lines);
+    store16_past(o.pre + m * 2 * o.N + o.N + n, pack16<bf16_t>(u), lines);
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) u[e] *= act_fwd<bf16_t>(g[e], o.act);
-  store16_stream(o.out + m * o.ldo + n, pack16<bf16_t>(u));
+  store16_past(o.out + m * o.ldo + n, pack16<bf16_t>(u), lines);
 }
 
 // Workgroup tile BM x BN of WM x WN waves, contraction tiles of BK in a ring of NS LDS stages,
