@@ -31,6 +31,7 @@ struct LinearArgs {
   bool bf16;
   int act;
   long long ldx, ldw, ldy, ldr, lddy;
+  int readable_k = 0, readable_n = 0;   // backward: columns of x and w, and of dy, that may be read (0: k and n)
 };
 size_t linear_fwd_ws_bytes(const LinearArgs& a);
 hipError_t launch_linear_fwd(const LinearArgs& a, const void* x, const void* w, const void* bias, const void* res,

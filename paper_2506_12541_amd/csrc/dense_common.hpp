@@ -13,6 +13,19 @@ __device__ __forceinline__ uint4 load16u(const T* p) {
   __builtin_memcpy(&v, p, 16);
   return v;
 }
+// The same of eight bf16 values by whole words: a load of 16 bytes that begins inside a 4-byte word takes more than twice
+// as long. Such a load begins one value earlier, so the value in front of p has to be in bounds as well: it is in a
+// matrix that begins with a word.
+__device__ __forceinline__ uint4 load16_words(const bf16_t* p) {
+  const bool odd = (uintptr_t)p & 2;
+  uint4 v;
+  __builtin_memcpy(&v, __builtin_assume_aligned(p - (odd ? 1 : 0), 4), 16);
+  const uint32_t last = *reinterpret_cast<const uint16_t*>(p + 7);
+  if (odd)
+    v = make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                   __builtin_amdgcn_alignbit(v.w, v.z, 16), last << 16 | v.w >> 16);
+  return v;
+}
 template <typename T>
 __device__ __forceinline__ void store16u(T* p, uint4 v) {
   __builtin_memcpy(p, &v, 16);

@@ -16,7 +16,7 @@ namespace {
 template <typename T>
 __global__ void __launch_bounds__(256) gated_dz_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ pre,
                                                        int act, long long m, int n, long long rpg, T* __restrict__ dz,
-                                                       float* __restrict__ part) {
+                                                       long long lddz, float* __restrict__ part) {
   constexpr int E = 16 / (int)sizeof(T);
   __shared__ float red[8][2][32 * E + 4];
   const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(256) gated_dz_kernel(const T* __restrict__ dy,
         s[0][e] += g[e];
         s[1][e] += u[e];
       }
-      T* const p = dz + r * 2 * n + c;
+      T* const p = dz + r * lddz + c;
       if (c + E <= n) {
         store16u(p, pack16<T>(g));
         store16u(p + n, pack16<T>(u));
@@ -355,6 +355,29 @@ __global__ void __launch_bounds__(256) gated_dz_planes_kernel(const float* __res
   }
 }
 
+// ---- bf16 rows that do not begin on 16 bytes ----
+//
+// The products load 16-byte pieces straight into LDS where rows begin on 16 bytes. Others are copied so that they do,
+// zeros behind their ends.
+
+struct PadJob {
+  const bf16_t* src;
+  long long ld, rows;
+  bf16_t* dst;
+};
+
+// 32 column pieces x 8 rows at a time
+__global__ void __launch_bounds__(256) pad_rows_kernel(PadJob j0, PadJob j1, int cols, int pitch) {
+  const PadJob j = blockIdx.z ? j1 : j0;
+  const int c = 8 * (blockIdx.x * 32 + (threadIdx.x & 31));
+  if (c >= cols) return;
+  const bool words = !((uintptr_t)j.src & 2);
+  const Mat<bf16_t> m{j.src, j.ld, j.rows, cols};
+#pragma unroll 2
+  for (long long r = blockIdx.y * 8LL + (threadIdx.x >> 5); r < j.rows; r += 8LL * gridDim.y)
+    *reinterpret_cast<uint4*>(j.dst + r * pitch + c) = words && c + 8 <= cols ? load16_words(j.src + r * j.ld + c) : load_piece(m, r, c);
+}
+
 // ---- gradients of few rows: the weight is read, and its gradient written, once ----
 //
 // Float32 with few rows is no work for the matrix cores: 16 multiply-adds for a value of w, or of dw, keep up with
@@ -472,7 +495,42 @@ __global__ void __launch_bounds__(256) few_dw_kernel(const float* __restrict__ d
 // The forward's product has 2n columns.
 Plan fwd_plan(const GatedArgs& a) { return plan_product(a.bf16, a.m, 2 * a.n, a.k); }
 
-LinearArgs rows_of(const GatedArgs& a) { return LinearArgs{a.m, a.k, 2 * a.n, a.bf16, kActNone, a.ldx, a.ldw, 0, 0, 2LL * a.n}; }
+int up8(int x) { return (x + 7) / 8 * 8; }
+// dz belongs to this file: its rows begin on 16 bytes, and what lies behind them may be read.
+long long dz_pitch(const GatedArgs& a) { return a.bf16 ? up8(2 * a.n) : 2LL * a.n; }
+LinearArgs rows_of(const GatedArgs& a) {
+  return LinearArgs{a.m, a.k, 2 * a.n, a.bf16, kActNone, a.ldx, a.ldw, 0, 0, dz_pitch(a), 0, (int)dz_pitch(a)};
+}
+
+// Whether bf16 operands whose rows do not begin on 16 bytes (backward: or end inside of them) are copied first: where
+// the products are long enough for it. us (forward, backward) with copies and without: 8191 x 1023 -> 2 x 2047 105, 228
+// and 157, 290; 47687 x 84 -> 2 x 3201 376, 859 and 526, 866; 65536 x 511 -> 2 x 257 94, 322 and 139, 320; 4015 x 133 ->
+// 2 x 6683 67, 212 and 103, 245; 2048 x 2047 -> 2 x 1023 46, 92 and 41, 100; 1954 x 1331 -> 2 x 824 41, 83 and 45, 82;
+// 1000 x 707 -> 2 x 300 20, 48 and 17, 43; 64 x 8191 -> 2 x 4096 106, 181 and 40, 144.
+struct Pads {
+  bool x, w;
+  size_t x_bytes, w_bytes;
+};
+Pads pads(const GatedArgs& a, bool backward) {
+  if (!a.bf16 || a.m * a.n < (3LL << 30) / a.k || a.m < 1024) return Pads{};
+  Pads p{};
+  p.x = a.ldx % 8 || (backward && a.k % 8);
+  p.w = a.ldw % 8 || (backward && a.k % 8);
+  p.x_bytes = p.x ? align256(sizeof(bf16_t) * (size_t)a.m * up8(a.k)) : 0;
+  p.w_bytes = p.w ? align256(sizeof(bf16_t) * (size_t)2 * a.n * up8(a.k)) : 0;
+  return p;
+}
+
+// Copies of x and w behind one another at `to`, as their places in a.
+hipError_t pad(GatedArgs& a, const Pads& p, const void*& x, const void*& w, char* to, hipStream_t st) {
+  PadJob j[2]{};
+  if (p.x) j[0] = PadJob{(const bf16_t*)x, a.ldx, a.m, (bf16_t*)to}, x = to, a.ldx = up8(a.k), to += p.x_bytes;
+  if (p.w) j[1] = PadJob{(const bf16_t*)w, a.ldw, 2LL * a.n, (bf16_t*)to}, w = to, a.ldw = up8(a.k);
+  const unsigned gx = (unsigned)((a.k + 255) / 256);
+  const long long rows = std::max(j[0].rows, j[1].rows), gy = std::min<long long>((rows + 15) / 16, std::max(2048 / gx, 1u));
+  pad_rows_kernel<<<dim3(gx, (unsigned)gy, 2), 256, 0, st>>>(j[0], j[1], a.k, up8(a.k));
+  return hipGetLastError();
+}
 
 // Whether float32 products go through planes: where both sides of a product have several tiles that share them, and
 // the forward's one product is long enough for the pass before it. us (forward, backward) by planes and without:
@@ -553,6 +611,7 @@ struct GatedBwdWs {
   int P;
   long long rpg;
   PartsPlan px, pw;          // of dx and dw
+  Pads pads;                 // x and w copied, at x
 };
 GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
   GatedBwdWs L{};
@@ -577,7 +636,9 @@ GatedBwdWs gated_bwd_layout(const GatedArgs& a) {
     auto part = [](int S, long long M, long long N) { return S > 1 ? sizeof(float) * (size_t)S * M * N : 0; };
     L.rest = put(std::max(part(L.px.S, a.m, a.k), part(L.pw.S, 2LL * a.n, a.k)));
   } else {
-    L.dz = put(esz * (size_t)a.m * 2 * a.n);
+    L.dz = put(esz * (size_t)a.m * dz_pitch(a));
+    L.pads = pads(a, true);
+    L.x = put(L.pads.x_bytes + L.pads.w_bytes);
     const size_t own = few_dx(a) ? sizeof(float) * (size_t)few_splits(a) * a.m * a.k : 0;
     L.rest = put(few_dx(a) && few_dw(a) ? own : std::max(own, linear_bwd_ws_bytes(rows_of(a))));
   }
@@ -618,6 +679,7 @@ hipError_t parts_product(const PlaneMat& a, const PlaneMat& b, long long M, int 
 struct GatedFwdWs {
   size_t x, w, flags, part, total;
   PartsPlan p;
+  Pads pads;
 };
 GatedFwdWs gated_fwd_layout(const GatedArgs& a) {
   GatedFwdWs L{};
@@ -631,6 +693,8 @@ GatedFwdWs gated_fwd_layout(const GatedArgs& a) {
     L.part = put(L.p.S > 1 ? sizeof(float) * (size_t)L.p.S * a.m * 2 * a.n : 0);
   } else if (!few_rows_ok(a.m, a.k)) {
     L.part = put(plan_bytes(fwd_plan(a), a.m, 2LL * a.n));
+    L.pads = pads(a, false);
+    L.x = put(L.pads.x_bytes + L.pads.w_bytes);
   }
   L.total = off;
   return L;
@@ -680,15 +744,21 @@ hipError_t planes_bwd(const GatedArgs& a, const GatedBwdWs& L, const void* x, co
 }
 
 template <typename T>
-hipError_t gated_fwd(const GatedArgs& a, const void* x, const void* w, const void* bias, void* y, void* pre, void* ws,
+hipError_t gated_fwd(GatedArgs a, const void* x, const void* w, const void* bias, void* y, void* pre, void* ws,
                      hipStream_t st) {
   const Epi<T> o{a.m, a.n, (T*)y, a.ldy, (const T*)bias, nullptr, 0, (T*)pre, a.act, nullptr};
-  const Mat<T> mx{(const T*)x, a.ldx, a.m, a.k}, mw{(const T*)w, a.ldw, 2LL * a.n, a.k};
-  if (few_rows_ok(a.m, a.k)) return few_rows<T, 2>(mx, mw, a.m, a.n, a.k, o, st);
+  if (few_rows_ok(a.m, a.k))
+    return few_rows<T, 2>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, 2LL * a.n, a.k}, a.m, a.n, a.k, o, st);
   if constexpr (sizeof(T) == 4) {
     if (fwd_planes(a)) return planes_fwd(a, x, w, o, (char*)ws, st);
   }
-  return product<T, false, false, true>(mx, mw, a.m, a.n, a.k, fwd_plan(a), (float*)((char*)ws + gated_fwd_layout(a).part), o, st);
+  const GatedFwdWs L = gated_fwd_layout(a);
+  if (L.pads.x || L.pads.w) {
+    const hipError_t e = pad(a, L.pads, x, w, (char*)ws + L.x, st);
+    if (e != hipSuccess) return e;
+  }
+  return product<T, false, false, true>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, 2LL * a.n, a.k}, a.m, a.n,
+                                        a.k, fwd_plan(a), (float*)((char*)ws + L.part), o, st);
 }
 
 template <typename T>
@@ -705,7 +775,7 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
     if (e != hipSuccess) return e;
   } else if (a.m > 0) {
     gated_dz_kernel<T><<<dim3((a.n + 32 * E - 1) / (32 * E), L.P), 256, 0, st>>>((const T*)dy, a.lddy, (const T*)pre, a.act,
-                                                                                 a.m, a.n, L.rpg, dz, dbp);
+                                                                                 a.m, a.n, L.rpg, dz, dz_pitch(a), dbp);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -722,7 +792,14 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
     }
   }
   if (!planes && (dx || dw || a.m == 0)) {    // without rows this also clears db
-    const hipError_t e = launch_linear_bwd(rows_of(a), x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
+    LinearArgs r = rows_of(a);
+    if (a.m > 0 && (L.pads.x || L.pads.w)) {
+      GatedArgs p = a;
+      const hipError_t e = pad(p, L.pads, x, w, c + L.x, st);
+      if (e != hipSuccess) return e;
+      r.ldx = p.ldx, r.ldw = p.ldw, r.readable_k = up8(a.k);
+    }
+    const hipError_t e = launch_linear_bwd(r, x, w, nullptr, dz, dx, dw, a.m > 0 ? nullptr : db, c + L.rest, st);
     if (e != hipSuccess) return e;
   }
   if (!dbp) return hipSuccess;

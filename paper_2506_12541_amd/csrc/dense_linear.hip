@@ -126,16 +126,18 @@ hipError_t linear_bwd(const LinearArgs& a, const void* x, const void* w, const v
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const Mat<T> mz{dz ? dz : (const T*)dy, dz ? a.n : a.lddy, a.m, a.n};
+  Mat<T> mz{dz ? dz : (const T*)dy, dz ? a.n : a.lddy, a.m, a.n};
+  const int k = std::max(a.k, a.readable_k);
   if (dx) {
     Epi<T> o{a.m, a.k, (T*)dx, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
-    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, a.k}, a.m, a.k, a.n, L.dx,
+    hipError_t e = product<T, false, true>(mz, Mat<T>{(const T*)w, a.ldw, a.n, k}, a.m, a.k, a.n, L.dx,
                                              (float*)(c + L.part), o, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
     Epi<T> o{a.n, a.k, (T*)dw, a.k, nullptr, nullptr, 0, nullptr, kActNone, nullptr};
-    hipError_t e = product<T, true, true>(mz, Mat<T>{(const T*)x, a.ldx, a.m, a.k}, a.n, a.k, a.m, L.dw,
+    mz.cols = std::max(a.n, a.readable_n);
+    hipError_t e = product<T, true, true>(mz, Mat<T>{(const T*)x, a.ldx, a.m, k}, a.n, a.k, a.m, L.dw,
                                           (float*)(c + L.part), o, st);
     if (e != hipSuccess) return e;
   }

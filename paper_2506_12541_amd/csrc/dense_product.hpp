@@ -834,7 +834,9 @@ __global__ void __launch_bounds__(64 * WM * WN) product_dma_kernel(Mat<bf16_t> a
 // x comes from the caches. The waves' sums meet in LDS, added in order. Bound by the weight's
 // bytes: 4 rows, 4096 -> 8192 channels (67 MB) take 14.6 us, 4.6 TB/s; with the tiles above 24.
 // Gated: the workgroup's 16 columns of both maps (NM = 2).
-template <typename T, int MB, int NW, int NM>
+// WORDS: bf16 rows of an odd length (load16_words; 3 rows, 4263 -> 2 x 4371: 30 us, 48 without; 6 rows, 5355 -> 2 x 2311: 20
+// and 37).
+template <typename T, int MB, int NW, int NM, bool WORDS>
 __global__ void __launch_bounds__(64 * NW) few_rows_kernel(Mat<T> x, Mat<T> w, int K, Epi<T> o) {
   typedef typename Chunk<T>::type CT;
   __shared__ __attribute__((aligned(16))) float part[NW][NM][MB][256];
@@ -859,9 +861,19 @@ __global__ void __launch_bounds__(64 * NW) few_rows_kernel(Mat<T> x, Mat<T> w, i
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
 #pragma unroll
-      for (int h = 0; h < NM; ++h) wf[h][c] = load_chunk_u(wp[h] + 128 * g + 32 * c);
+      for (int h = 0; h < NM; ++h) {
+        if constexpr (WORDS)
+          wf[h][c] = __builtin_bit_cast(CT, load16_words(wp[h] + 128 * g + 32 * c));
+        else
+          wf[h][c] = load_chunk_u(wp[h] + 128 * g + 32 * c);
+      }
 #pragma unroll
-      for (int b = 0; b < MB; ++b) xf[b][c] = load_chunk_u(xp[b] + 128 * g + 32 * c);
+      for (int b = 0; b < MB; ++b) {
+        if constexpr (WORDS)
+          xf[b][c] = __builtin_bit_cast(CT, load16_words(xp[b] + 128 * g + 32 * c));
+        else
+          xf[b][c] = load_chunk_u(xp[b] + 128 * g + 32 * c);
+      }
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -1008,38 +1020,49 @@ size_t plan_bytes(const Plan& p, long long M, long long N) { return p.S > 1 ? si
 // channels: 9.2 us, split 13.0; 4096 -> 4096: 21.3 us, split 15.6, as every 16 columns read all of x.)
 bool few_rows_ok(long long m, int k) { return m <= 16 || (m <= 64 && k <= 1024); }
 
-template <typename T, int NW, int NM>
+template <typename T, int NW, int NM, bool WORDS>
 void few_rows_nw(int MB, dim3 grid, const Mat<T>& x, const Mat<T>& w, int K, const Epi<T>& o, hipStream_t st) {
   if (MB == 1)
-    few_rows_kernel<T, 1, NW, NM><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
+    few_rows_kernel<T, 1, NW, NM, WORDS><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
   else if (MB == 2)
-    few_rows_kernel<T, 2, NW, NM><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
+    few_rows_kernel<T, 2, NW, NM, WORDS><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
   else
-    few_rows_kernel<T, 4, NW, NM><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
+    few_rows_kernel<T, 4, NW, NM, WORDS><<<grid, 64 * NW, 0, st>>>(x, w, K, o);
 }
 
-// The forward of a map of N columns by few_rows_kernel (few_rows_ok).
-template <typename T, int NM>
-hipError_t few_rows(const Mat<T>& x, const Mat<T>& w, long long M, int N, int K, const Epi<T>& o, hipStream_t st) {
+template <typename T, int NM, bool WORDS>
+void few_rows_run(const Mat<T>& x, const Mat<T>& w, long long M, int N, int K, const Epi<T>& o, hipStream_t st) {
   const int MB = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   const dim3 grid((N + 15) / 16);
   // waves per workgroup: about two per SIMD of the chip, at most one per 128 indices
   const long long wg = grid.x;
   if (wg >= 512 || K <= 512)
-    few_rows_nw<T, 4, NM>(MB, grid, x, w, K, o, st);
+    few_rows_nw<T, 4, NM, WORDS>(MB, grid, x, w, K, o, st);
   else if (wg >= 256 || K <= 1024)
-    few_rows_nw<T, 8, NM>(MB, grid, x, w, K, o, st);
-  else
-    few_rows_nw<T, 16, NM>(MB, grid, x, w, K, o, st);
+    few_rows_nw<T, 8, NM, WORDS>(MB, grid, x, w, K, o, st);
+  else    // longer contractions come with up to 16 rows (few_rows_ok)
+    few_rows_kernel<T, 1, 16, NM, WORDS><<<grid, 64 * 16, 0, st>>>(x, w, K, o);
+}
+
+// The forward of a map of N columns by few_rows_kernel (few_rows_ok).
+template <typename T, int NM>
+hipError_t few_rows(const Mat<T>& x, const Mat<T>& w, long long M, int N, int K, const Epi<T>& o, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (w.ld % 2 && !(((uintptr_t)w.p | (uintptr_t)x.p) & 2)) {
+      few_rows_run<T, NM, true>(x, w, M, N, K, o, st);
+      return hipGetLastError();
+    }
+  }
+  few_rows_run<T, NM, false>(x, w, M, N, K, o, st);
   return hipGetLastError();
 }
 
-bool dma_ok(const Mat<bf16_t>& m, bool tr, long long K) {
-  const bool whole = tr ? m.cols % 8 == 0 && m.cols >= 8 : K % 8 == 0;
+bool dma_ok(const Mat<bf16_t>& m, bool tr) {
+  const bool whole = !tr || (m.cols % 8 == 0 && m.cols >= 8);    // a row's last piece is loaded as a part of one
   // a tile's byte offsets fit 32 bits: 256 rows of at most 2^22 elements
   return whole && m.ld % 8 == 0 && m.ld <= (1 << 22) && ((uintptr_t)m.p & 15) == 0;
 }
-bool dma_ok(const Mat<float>&, bool, long long) { return false; }
+bool dma_ok(const Mat<float>&, bool) { return false; }
 
 // C = A B^T with the epilogue; S > 1: partial sums in part, joined by split_sum_kernel. G: a gated product,
 // N outputs from 2 N stored rows of B.
@@ -1047,7 +1070,7 @@ template <typename T, bool TA, bool TB, bool G = false>
 hipError_t product(const Mat<T>& a, const Mat<T>& b, long long M, int N, long long K, Plan p, float* part, Epi<T> o,
                    hipStream_t st) {
   o.part = p.S > 1 ? part : nullptr;
-  const bool dma = dma_ok(a, TA, K) && dma_ok(b, TB, K);
+  const bool dma = dma_ok(a, TA) && dma_ok(b, TB);
   const int side = !dma && p.T == 256 ? 128 : p.T;
   const int cols = G ? side / 2 : side;    // outputs of a tile's row
   const int ntm = (int)((M + side - 1) / side), ntn = (N + cols - 1) / cols;

@@ -440,6 +440,47 @@ def test_gated_strides_and_parts(dtype, m, k, n):
             assert some[name] is None or torch.equal(some[name], a[name])
 
 
+@pytest.mark.parametrize("m,k,n", [(3, 515, 40), (16, 1025, 33), (1, 4097, 70), (30, 1001, 129), (64, 257, 100), (7, 129, 9)])
+def test_odd_contractions_of_few_rows(m, k, n):
+    """Rows of an odd length, that begin inside 4-byte words in turn; operands that begin inside one."""
+    check_gated(gen(m), "bf16", m, k, n, "silu", True)
+    g = gen(m + 1)
+    x, w = normal(g, m, k + 2, dtype=BF), normal(g, 2 * n, k + 2, dtype=BF, scale=0.1)
+    for a, b in ((0, 0), (0, 1), (1, 0), (1, 1), (2, 1)):
+        xs, ws = x[:, a:a + k], w[:, b:b + k]
+        y, pre = dense.gated_forward(xs, ws, save_pre=True)
+        want, want_pre = dense.gated_forward(xs.contiguous(), ws.contiguous(), save_pre=True)
+        assert torch.equal(y, want) and torch.equal(pre, want_pre)
+        want = dense_ref.linear(xs.cpu(), ws.cpu(), None, None, "none")["y"]
+        check("affine", dense.linear_forward(xs, ws)[0], *want)
+        check("affine, whole rows", dense.linear_forward(xs.contiguous(), ws.contiguous())[0], *want)
+
+
+@pytest.mark.parametrize("m,k,n", [(3000, 1031, 1100), (1100, 4100, 801), (20001, 67, 2501)])
+def test_gated_rows_that_are_copied(m, k, n):
+    """bf16 products of rows that do not begin on 16 bytes and are long enough to be copied, and of other strides."""
+    check_gated(gen(m), "bf16", m, k, n, "silu", True)
+    g = gen(9)
+    x, w, dy = normal(g, m, k, dtype=BF), normal(g, 2 * n, k, dtype=BF, scale=0.1), normal(g, m, n, dtype=BF)
+    y, pre = dense.gated_forward(x, w, act="gelu", save_pre=True)
+    a = dense.gated_backward(x, w, dy, pre, act="gelu", bias=True)
+
+    def apart(t, ld):
+        buf = torch.full((t.shape[0], ld), float("nan"), dtype=BF, device="cuda")
+        buf[:, :t.shape[1]] = t
+        return buf[:, :t.shape[1]]
+    for lx, lw in ((k + 13, k + 13), ((k + 15) // 8 * 8, (k + 15) // 8 * 8), (k + 1, (k + 15) // 8 * 8), ((k + 15) // 8 * 8, k + 3)):
+        xs, ws = apart(x, lx), apart(w, lw)
+        ys, ps = dense.gated_forward(xs, ws, act="gelu", save_pre=True)
+        b = dense.gated_backward(xs, ws, apart(dy, n + 3), ps, act="gelu", bias=True)
+        for u, v in ((y, ys), (pre, ps), *((a[name], b[name]) for name in a)):
+            assert torch.allclose(u.float(), v.float(), rtol=2 * dense_ref.HALF[BF], atol=2e-3)
+        for kw in (dict(need_dx=False), dict(need_dw=False)):
+            some = dense.gated_backward(xs, ws, dy, ps, act="gelu", **kw)
+            for name in ("dx", "dw"):
+                assert some[name] is None or torch.equal(some[name], b[name])
+
+
 def test_gated_no_rows_and_values_that_are_not_finite():
     w = torch.ones(80, 24, device="cuda", dtype=BF)
     e = torch.zeros(0, 24, device="cuda", dtype=BF)
