@@ -34,7 +34,7 @@ _HERE = contextlib.nullcontext()
 
 # Parameter records of calls whose arguments have passed the checks, by all that the checks read of them (shapes, strides,
 # types, devices, plain numbers; never addresses or values of tensors). The calls of a serving step are as short on the GPU as their
-# host path is long: with it a rotary_forward of 32 tokens takes 8 us of the host, without 14.
+# host path is long: with it a rotary_forward of 32 tokens takes 8 us of the host, without 14, a gated_forward 6.6, without 12.
 _checked = {}
 
 
@@ -254,11 +254,18 @@ def gated_forward(x, w, bias=None, act: str = "silu", save_pre: bool = False, st
     """y = act(g) u, [g | u] = x w^T + bias, for x [..., k], w [2 n, k] (the gate's n rows first), bias [2 n]. Returns
     (y [..., n], pre); pre [..., 2 n] is what gated_backward needs (save_pre; else None)."""
     lib = _lib.load()
-    p = _gated_params(x, w, act)
+    try:
+        key = ("gated_forward", _signature(x), _signature(w), _signature(bias), act)
+        record = _checked.get(key)
+    except (AttributeError, TypeError):      # no tensors: the checks say so
+        key = record = None
+    if record is None:
+        p = _gated_params(x, w, act)
+        if bias is not None:
+            _shaped(bias, "bias", (2 * p.n,), x.dtype, x.device)
+        record = _remember(key, (p, _gated_sizes(lib, p)[0]))
+    p, need = record
     dev, dt = x.device, x.dtype
-    if bias is not None:
-        _shaped(bias, "bias", (2 * p.n,), dt, dev)
-    need, _ = _gated_sizes(lib, p)
     with _on(dev, stream):
         ws = _workspace(need, dev)
         y = torch.empty((*x.shape[:-1], p.n), dtype=dt, device=dev)
@@ -273,15 +280,22 @@ def gated_backward(x, w, dy, pre, act: str = "silu", bias: bool = False, need_dx
     """Gradients of gated_forward given dy [..., n]: dict(dx, dw, db), each in x's type (None where not asked for;
     bias: form db)."""
     lib = _lib.load()
-    p = _gated_params(x, w, act)
+    try:
+        key = ("gated_backward", _signature(x), _signature(w), _signature(dy), _signature(pre), act)
+        record = _checked.get(key)
+    except (AttributeError, TypeError):
+        key = record = None
+    if record is None:
+        p = _gated_params(x, w, act)
+        _, _, p.ld_dy = _rows(dy, "dy", p.n, x.dtype, x.device, p.m)
+        if pre is None:
+            raise ValueError("pre is needed: run gated_forward with save_pre=True")
+        _rows(pre, "pre", 2 * p.n, x.dtype, x.device, p.m)
+        if not pre.is_contiguous():
+            raise ValueError("pre must be contiguous")
+        record = _remember(key, (p, _gated_sizes(lib, p)[1]))
+    p, need = record
     dev, dt = x.device, x.dtype
-    _, _, p.ld_dy = _rows(dy, "dy", p.n, dt, dev, p.m)
-    if pre is None:
-        raise ValueError("pre is needed: run gated_forward with save_pre=True")
-    _rows(pre, "pre", 2 * p.n, dt, dev, p.m)
-    if not pre.is_contiguous():
-        raise ValueError("pre must be contiguous")
-    _, need = _gated_sizes(lib, p)
     with _on(dev, stream):
         ws = _workspace(need, dev)
         dx = torch.empty(x.shape, dtype=dt, device=dev) if need_dx else None
