@@ -995,7 +995,10 @@ struct Plan {
 // - 128 x 128 where there are 256 of them (2048 x 1024 x 2048: 14.9, 64 x 64 16.8), or where a contraction of 4096 and
 //   more is split over them (1280 x 4096 x 1792: 38 and 49; 2048, no split of 64 x 64: 1024 x 2048 x 1024: 18.6 and 12.2).
 // float32: 128 x 128 where there are 512 of them (2560 x 2048 -> 3584, 560 tiles: 286 and 286; 2304 x 3200, 450
-// tiles: 213, 128 x 64 193), else 64 rows fewer or both (product()).
+// tiles: 213, 128 x 64 193), else 64 rows fewer or both (product()): also for contractions up to 1024, where more
+// workgroups to a CU write while others multiply (128 x 128 and 128 x 64; 65536 x 256 -> 512: 173 and 131, 65536 x 1024 ->
+// 1024: 897 and 886, 8192 x 1024 -> 2048: 221 and 208, dW of 4096 x 2048 with 512 rows 88 and 79, of 8192 x 4096 with 32
+// rows 76 and 59; 4096 x 2048 -> 4096: 402 and 422).
 Plan plan_product(bool bf16, long long M, int N, long long K) {
   auto tiles = [&](int T) { return ((M + T - 1) / T) * ((N + T - 1) / T); };
   auto plan = [&](int T, int want) {
@@ -1003,7 +1006,7 @@ Plan plan_product(bool bf16, long long M, int N, long long K) {
     while (tiles(T) * p.S < want && K / (2 * p.S) >= (T == 64 ? 256 : 512) && p.S < 64) p.S *= 2;
     return p;
   };
-  if (!bf16) return plan(tiles(128) >= 512 ? 128 : 64, 512);
+  if (!bf16) return plan(tiles(128) >= 512 && K > 1024 ? 128 : 64, 512);
   if (tiles(256) >= 192) return Plan{256, 1};
   if (K >= 16384 && tiles(256) >= 12) {
     const Plan p = plan(256, 192);
