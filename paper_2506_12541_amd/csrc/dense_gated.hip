@@ -534,9 +534,10 @@ hipError_t pad(GatedArgs& a, const Pads& p, const void*& x, const void*& w, char
 
 // Whether float32 products go through planes: where both sides of a product have several tiles that share them, and
 // the forward's one product is long enough for the pass before it. us (forward, backward) by planes and without:
-// 3586 x 515 -> 2 x 1029: 61, 168 and 78, 260; 2000 x 2048 -> 2 x 2048: 175, 363 and 218, 503; 1000 x 8192 -> 2 x 600: 152, 265 and
-// 178, 357; 1024 x 1024 -> 2 x 1024: 40, 84 and 38, 99; 2048 x 512 -> 2 x 1024: 38, 87 and 33, 101; 300 x 4096 -> 2 x 4096: 218,
-// 378 and 176, 436; 20000 x 256 -> 2 x 256: 56, 134 and 60, 129; 65536 x 64 -> 2 x 1024: 275, 728 and 313, 677.
+// 3586 x 515 -> 2 x 1029: 61, 156 and 76, 255; 2000 x 2048 -> 2 x 2048: 169, 352 and 200, 475; 8192 x 1024 -> 2 x 2048: 343, 693 and
+// 423, 981; 65536 x 256 -> 2 x 1024: 582, 1049 and 568, 1391; 1024 x 1024 -> 2 x 1024: 40, 89 and 42, 115; 2048 x 512 -> 2 x 1024:
+// 38, 91 and 40, 116; 800 x 256 -> 2 x 512: 12 (none), 49 and 13, 44; 20000 x 256 -> 2 x 256: 56, 134 and 52, 138; 300 x 4096 ->
+// 2 x 4096: 218, 378 and 212, 447; 65536 x 64 -> 2 x 1024: 275, 728 and 271, 707.
 bool bwd_planes(const GatedArgs& a) {
   const long long most = 1LL << 35;     // launches of fewer than 2^23 workgroups
   return !a.bf16 && a.m >= 768 && a.n >= 512 && a.k >= 256 && a.k <= (1 << 22) && a.n <= (1 << 21) && a.m * a.n <= most &&
