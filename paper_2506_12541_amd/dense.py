@@ -239,7 +239,7 @@ def _gated_params(x, w, act):
     if w.dim() != 2 or w.shape[0] % 2:
         raise ValueError("w must be [2 n, k]")
     n2, _, ldw = _rows(w, "w", k)
-    if act not in ACTIVATIONS:
+    if not isinstance(act, str) or act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
     return _lib.bsa_gated_t(m, k, n2 // 2, _CODES[x.dtype], ACTIVATIONS[act], ldx, ldw, 0, 0)
 

@@ -481,6 +481,26 @@ def test_gated_rows_that_are_copied(m, k, n):
                 assert some[name] is None or torch.equal(some[name], b[name])
 
 
+def test_gated_refusals_after_calls_that_passed():
+    """A call like one that was checked before is checked where anything differs; records keep nothing of the values."""
+    x, w, b = (torch.randn(s, device="cuda") for s in ((6, 40), (2 * 24, 40), (2 * 24,)))
+    for scale in (1.0, 2.0):                 # the same shapes again
+        y, pre = dense.gated_forward(scale * x, w, b, save_pre=True)
+        dy = torch.ones_like(y)
+        want = ref.gated((scale * x).cpu(), w.cpu(), b.cpu(), "silu", dy.cpu())
+        got = dict(y=y, **dense.gated_backward(scale * x, w, dy, pre, bias=True))
+        for name, (value, bound) in want.items():
+            check(name, got[name], value, bound)
+    for kw in (dict(act="tanh"), dict(act=["silu"]), dict(bias=b[1:]), dict(bias=b.to(BF)), dict(bias=b.cpu()), dict(w=w[1:]),
+               dict(w=w.t()), dict(x=x.to(BF)), dict(x=x[:, 1:]), dict(x=x.cpu()), dict(x=None)):
+        with pytest.raises(ValueError):
+            dense.gated_forward(**{**dict(x=x, w=w, bias=b), **kw})
+    for kw in (dict(pre=None), dict(pre=pre[1:]), dict(pre=pre.t().contiguous().t()), dict(dy=dy[:, 1:]), dict(dy=dy.to(BF)),
+               dict(dy=None), dict(act="tanh")):
+        with pytest.raises(ValueError):
+            dense.gated_backward(**{**dict(x=x, w=w, dy=dy, pre=pre), **kw})
+
+
 def test_gated_no_rows_and_values_that_are_not_finite():
     w = torch.ones(80, 24, device="cuda", dtype=BF)
     e = torch.zeros(0, 24, device="cuda", dtype=BF)
