@@ -521,14 +521,16 @@ Pads pads(const GatedArgs& a, bool backward) {
   return p;
 }
 
-// Copies of x and w behind one another at `to`, as their places in a.
+// Copies of x and w, those that p names, behind one another at `to`, as their places in a.
 hipError_t pad(GatedArgs& a, const Pads& p, const void*& x, const void*& w, char* to, hipStream_t st) {
   PadJob j[2]{};
-  if (p.x) j[0] = PadJob{(const bf16_t*)x, a.ldx, a.m, (bf16_t*)to}, x = to, a.ldx = up8(a.k), to += p.x_bytes;
-  if (p.w) j[1] = PadJob{(const bf16_t*)w, a.ldw, 2LL * a.n, (bf16_t*)to}, w = to, a.ldw = up8(a.k);
+  int n = 0;
+  if (p.x) j[n++] = PadJob{(const bf16_t*)x, a.ldx, a.m, (bf16_t*)to}, x = to, a.ldx = up8(a.k), to += p.x_bytes;
+  if (p.w) j[n++] = PadJob{(const bf16_t*)w, a.ldw, 2LL * a.n, (bf16_t*)to}, w = to, a.ldw = up8(a.k);
+  if (n == 0) return hipSuccess;
   const unsigned gx = (unsigned)((a.k + 255) / 256);
   const long long rows = std::max(j[0].rows, j[1].rows), gy = std::min<long long>((rows + 15) / 16, std::max(2048 / gx, 1u));
-  pad_rows_kernel<<<dim3(gx, (unsigned)gy, 2), 256, 0, st>>>(j[0], j[1], a.k, up8(a.k));
+  pad_rows_kernel<<<dim3(gx, (unsigned)gy, n), 256, 0, st>>>(j[0], j[1], a.k, up8(a.k));
   return hipGetLastError();
 }
 
@@ -754,10 +756,8 @@ hipError_t gated_fwd(GatedArgs a, const void* x, const void* w, const void* bias
     if (fwd_planes(a)) return planes_fwd(a, x, w, o, (char*)ws, st);
   }
   const GatedFwdWs L = gated_fwd_layout(a);
-  if (L.pads.x || L.pads.w) {
-    const hipError_t e = pad(a, L.pads, x, w, (char*)ws + L.x, st);
-    if (e != hipSuccess) return e;
-  }
+  const hipError_t e = pad(a, L.pads, x, w, (char*)ws + L.x, st);
+  if (e != hipSuccess) return e;
   return product<T, false, false, true>(Mat<T>{(const T*)x, a.ldx, a.m, a.k}, Mat<T>{(const T*)w, a.ldw, 2LL * a.n, a.k}, a.m, a.n,
                                         a.k, fwd_plan(a), (float*)((char*)ws + L.part), o, st);
 }
@@ -794,9 +794,13 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
   }
   if (!planes && (dx || dw || a.m == 0)) {    // without rows this also clears db
     LinearArgs r = rows_of(a);
-    if (a.m > 0 && (L.pads.x || L.pads.w)) {
+    // the operands of the gradients that are formed; the other one's pointer may be NULL
+    Pads pads = L.pads;
+    pads.x = pads.x && dw && a.m > 0;
+    pads.w = pads.w && dx && a.m > 0;
+    if (pads.x || pads.w) {
       GatedArgs p = a;
-      const hipError_t e = pad(p, L.pads, x, w, c + L.x, st);
+      const hipError_t e = pad(p, pads, x, w, c + L.x, st);
       if (e != hipSuccess) return e;
       r.ldx = p.ldx, r.ldw = p.ldw, r.readable_k = up8(a.k);
     }

@@ -1,5 +1,6 @@
 """Rotary positions with head norms, the gated map, and the 8-bit cache with the attention that reads it, on the GPU
 against their float64 definitions, within bounds derived from the types (tests/block_ref.py)."""
+import ctypes as C
 import math
 
 import pytest
@@ -8,7 +9,7 @@ import torch
 import block_ref as ref
 import dense_ref
 from dense_ref import check
-from paper_2506_12541_amd import dense
+from paper_2506_12541_amd import _lib, dense
 
 pytestmark = pytest.mark.gpu
 
@@ -479,6 +480,30 @@ def test_gated_rows_that_are_copied(m, k, n):
             some = dense.gated_backward(xs, ws, dy, ps, act="gelu", **kw)
             for name in ("dx", "dw"):
                 assert some[name] is None or torch.equal(some[name], b[name])
+
+
+@pytest.mark.parametrize("dtype,m,k,n", [("bf16", 3000, 1031, 1100), ("bf16", 1100, 4100, 801), ("bf16", 900, 264, 520), ("bf16", 3, 515, 40),
+                                         ("bf16", 1, 64, 64), ("f32", 800, 300, 700), ("f32", 4, 1027, 4099), ("f32", 12, 1500, 6000),
+                                         ("f32", 300, 136, 132), ("f32", 30, 70, 9)])
+def test_gated_gradients_without_the_other_operand(dtype, m, k, n):
+    """The C entry with NULL for what a gradient that is not formed would read: copied rows, tiles, planes, few rows."""
+    lib, g, dt = _lib.load(), gen(m), DT[dtype]
+    x, w = normal(g, m, k, dtype=dt), normal(g, 2 * n, k, dtype=dt, scale=1 / math.sqrt(k))
+    dy = normal(g, m, n, dtype=dt)
+    _, pre = dense.gated_forward(x, w, save_pre=True)
+    want = dense.gated_backward(x, w, dy, pre, bias=True)
+    p = _lib.bsa_gated_t(m=m, k=k, n=n, dtype=_lib.BSA_BF16 if dtype == "bf16" else _lib.BSA_F32, act=dense.ACTIVATIONS["silu"])
+    need = C.c_size_t()
+    assert lib.bsa_gated_sizes(C.byref(p), None, C.byref(need)) == 0
+    for formed in (("dx",), ("dw",), ("db",), ("dx", "db"), ("dw", "db")):
+        ws = torch.full((need.value,), 255, dtype=torch.uint8, device="cuda")       # NaN in both types
+        got = {name: torch.full_like(want[name], float("nan")) for name in formed}
+        out = [got[name].data_ptr() if name in got else None for name in ("dx", "dw", "db")]
+        assert lib.bsa_gated_backward(C.byref(p), x.data_ptr() if "dw" in got else None, w.data_ptr() if "dx" in got else None,
+                                      pre.data_ptr(), dy.data_ptr(), *out, ws.data_ptr(), need.value,
+                                      torch.cuda.current_stream().cuda_stream) == 0
+        for name in got:
+            assert torch.equal(got[name], want[name]), (formed, name)
 
 
 def test_gated_refusals_after_calls_that_passed():
