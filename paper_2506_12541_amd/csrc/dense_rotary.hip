@@ -357,6 +357,7 @@ RotPlan rot_plan(const RotaryArgs& a, bool sums) {
   // 2 rows 71.3)
   const int per_row = a.heads * p.G;
   p.R = (int)std::max<long long>(1, std::min<long long>(std::min((256 + per_row - 1) / per_row, kRotLds / p.pitch), a.rows / 2048));
+  p.R = std::min(p.R, 65535 / std::max(a.heads, a.kv_heads));    // a step's heads, of queries and of keys, are counted by Div
   const long long groups = ((a.rows + p.R - 1) / p.R + 3) / 4;
   // few rows: waves share a row's heads, two for each lane
   const long long parts = std::max<long long>(1, std::min<long long>(256 / std::max<long long>(groups, 1), a.heads * p.G / 128));

@@ -78,6 +78,50 @@ def copied_rows(b):
         assert copies(x=None, w=None, dx=None, dw=None) == {}, (m, k, n)
 
 
+class RotParts(C.Structure):        # of rotary_kernel
+    _fields_ = [(n, C.c_void_p) for n in ("x", "dy", "out", "gain")] + [
+        (n, C.c_int64) for n in ("x_row", "x_head", "dy_row", "dy_head", "out_row", "out_head")] + [("heads", C.c_int32), ("magic", C.c_uint32)]
+
+
+class RotP(C.Structure):
+    _fields_ = [("part", RotParts * 2), ("pos", C.c_void_p), ("freq", C.c_void_p), ("rows", C.c_int64)] + [
+        (n, C.c_int32) for n in ("hd", "rot", "half", "axes", "per_axis", "R", "G", "lrot", "pitch")] + [
+        ("pitch_magic", C.c_uint32), ("axis_magic", C.c_uint32)]
+
+
+def rotary_steps(b):
+    """The divisions of a wave's step (an item by the heads, an angle by the row's pitch and the axis's pairs) are exact for
+    every number that they are given."""
+    b.take = {"rotary_kernel": (RotP,)}
+
+    def exact(top, d, magic):
+        """floor(x / d) as the high half of a product for x < top: it grows with x, so the ends of its steps decide."""
+        if d == 1:
+            return True
+        return all((x * magic >> 32) == x // d for q in range((top + d - 1) // d) for x in (q * d, min(q * d + d, top) - 1))
+    many = 0
+    for heads, kv in ((1, 1), (8, 2), (32, 8), (1, 255), (1, 2049), (1, 11000), (1, 16384), (1, 20000), (1, 32769), (1, 46508),
+                      (1, 65535), (2, 65535), (3, 40000), (200, 65521), (65535, 1), (65535, 65535), (300, 7)):
+        for hd, rot, axes in ((2, 2, 1), (6, 4, 2), (32, 32, 1), (64, 48, 3), (255, 130, 1), (256, 256, 4)):
+            for rows in (1, 2047, 4096, 10000, 131072, 1 << 24):
+                for dtype in (0, 1):
+                    p = b.abi.bsa_rotary_t(rows=rows, heads=heads, kv_heads=kv, head_dim=hd, rot=rot, axes=axes, dtype=dtype, eps=1e-5,
+                                           magnitude=1.0)
+                    q, k, pos, freq, g, h, dq, dk, yq, yk, dg, dh, ws = (i * PTR for i in range(1, 14))
+                    for run in (b.call("bsa_rotary_forward", C.byref(p), q, k, pos, freq, None, None, yq, yk, None),
+                                b.call("bsa_rotary_backward", C.byref(p), q, k, pos, freq, g, h, dq, dk, yq, yk, dg, dh, ws, BIG, None)):
+                        r = run[0].args[0]
+                        # the kernel's record is the one that this file knows
+                        assert (r.rows, r.hd, r.rot, r.half, r.axes, r.part[0].heads, r.part[1].heads) == (
+                            rows, hd, rot, rot // 2, axes, heads, kv)
+                        at = heads, kv, hd, rows, dtype, r.R
+                        assert 1 <= r.R and r.R * r.pitch <= 256, at      # the angles' place
+                        assert all(exact(r.R * t.heads, t.heads, t.magic) for t in r.part), at
+                        assert exact(r.R * r.pitch, r.pitch, r.pitch_magic) and exact(r.half, r.per_axis, r.axis_magic), at
+                        many += r.R > 1
+    assert many > 100
+
+
 if __name__ == "__main__":
     globals()[sys.argv[2]](Library(sys.argv[1]))
     print("checked")

@@ -95,6 +95,28 @@ def test_rotary_many_rows():
     check_rotary(gen(8), "bf16", 9000, 40, 8, 128, 128, False, False, train=False)
 
 
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("rows,kv,d,dtype", [(4096, 46508, 2, "bf16"), (131072, 1025, 2, "f32"), (66000, 2200, 4, "bf16")])
+def test_rotary_many_more_key_heads_than_query_heads(rows, kv, d, dtype, inter):
+    """Keys beside one query head, against the same keys as queries: rows are shared out otherwise, each head's numbers
+    are the same."""
+    g, dt = torch.Generator("cuda").manual_seed(rows), DT[dtype]
+    q, k = (torch.randn(rows, h, d, generator=g, device="cuda", dtype=dt) for h in (1, kv))
+    at = torch.randint(0, 1 << 20, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    freq, _ = dense.rotary_frequencies(d)
+    gain = torch.linspace(0.5, 1.5, d, device="cuda")
+    how = dict(eps=1e-5, interleaved=inter)
+    yq, yk = dense.rotary_forward(q, k, at, freq, gain_q=gain, gain_k=gain, **how)
+    assert torch.equal(yk, dense.rotary_forward(k, None, at, freq, gain_q=gain, **how)[0])
+    assert torch.equal(yq, dense.rotary_forward(q, None, at, freq, gain_q=gain, **how)[0])
+    # some heads against the definition
+    some = torch.tensor([0, 1, kv // 2, kv - 1])
+    last = torch.arange(rows - 300, rows)
+    check("y", yk[last][:, some], *ref.rotary(k[last][:, some].cpu(), at[last].cpu(), freq.cpu(), gain.cpu(), 1e-5, inter, 1.0)["y"])
+    got = dense.rotary_backward(yq, yk, at, freq, q=q, k=k, gain_q=gain, gain_k=gain, **how)
+    assert torch.equal(got["dk"], dense.rotary_backward(yk, None, at, freq, q=k, gain_q=gain, **how)["dq"])
+
+
 # ---- gated map ----
 
 def check_gated(g, dtype, m, k, n, act, bias, train=True):
