@@ -65,7 +65,7 @@ bsa_status_t check(const bsa_linear_t* p, bsa::LinearArgs* a) {
   if (p->m < 0 || p->m > INT32_MAX) return bad("m must be in [0, 2^31)");
   if (p->k < 1 || p->n < 1) return bad("k and n must be >= 1");
   if (p->k > (1 << 24) || p->n > (1 << 24)) return set_error(BSA_ERR_UNSUPPORTED, "k and n must be <= 2^24");
-  // 256 x 256 tiles have 512 threads, 128 x 128 tiles 256 (64 x 64 tiles are used where there are few)
+  // 256 x 256 tiles have 512 threads, 128 x 128 tiles 256 (smaller ones are used where they are fewer than 2^24)
   const auto fits = [](int64_t M, int64_t N) {
     return (M + 255) / 256 * ((N + 255) / 256) < 1 << 23 && (M + 127) / 128 * ((N + 127) / 128) < 1 << 24;
   };

@@ -1006,7 +1006,9 @@ Plan plan_product(bool bf16, long long M, int N, long long K) {
     while (tiles(T) * p.S < want && K / (2 * p.S) >= (T == 64 ? 256 : 512) && p.S < 64) p.S *= 2;
     return p;
   };
-  if (!bf16) return plan(tiles(128) >= 512 && K > 1024 ? 128 : 64, 512);
+  // 128 x 64 tiles of a very long and narrow product would be more workgroups than a launch holds
+  const bool narrow = (M + 127) / 128 * ((N + 63) / 64) >= 1 << 24;
+  if (!bf16) return plan((tiles(128) >= 512 && K > 1024) || narrow ? 128 : 64, 512);
   if (tiles(256) >= 192) return Plan{256, 1};
   if (K >= 16384 && tiles(256) >= 12) {
     const Plan p = plan(256, 192);

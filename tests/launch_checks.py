@@ -3,6 +3,7 @@ launch_stub.c in the HIP runtime's place. Not for a process that has loaded torc
 import ctypes as C
 import importlib.util
 import os
+import random
 import sys
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -120,6 +121,68 @@ def rotary_steps(b):
                         assert exact(r.R * r.pitch, r.pitch, r.pitch_magic) and exact(r.half, r.per_axis, r.axis_magic), at
                         many += r.R > 1
     assert many > 100
+
+
+def launches_fit(b):
+    """Calls that are accepted, and whose tensors fit a card of 288 GB, launch fewer than 2^32 threads (x) and 2^16 workgroups
+    (y, z)."""
+    abi, rng, card = b.abi, random.Random(1), 288e9
+    p8 = [i * PTR for i in range(1, 14)]
+    seen = [0, 0]
+
+    def call(name, *args):
+        b.launches = []
+        status = getattr(b.lib, name)(*args)
+        seen[status != 0] += 1
+        assert status in (0, abi.BSA_ERR_UNSUPPORTED), (name, status, b.lib.bsa_last_error())
+        assert not (status and b.launches), name
+        for r in b.launches:
+            assert r.threads() < 1 << 32 and max(r.grid[1:]) < 1 << 16, (name, r.kernel, r.grid, r.block)
+
+    def maps(m, k, n, dtype):
+        size = 2 if dtype == abi.BSA_BF16 else 4
+        p = abi.bsa_linear_t(m=m, k=k, n=n, dtype=dtype, act=2)
+        if size * (m * k + m * n + n * k) < card:
+            call("bsa_linear_forward", C.byref(p), *p8[:6], ws, BIG, None)
+            call("bsa_linear_backward", C.byref(p), *p8[:7], ws, BIG, None)
+        p = abi.bsa_gated_t(m=m, k=k, n=n, dtype=dtype, act=3)
+        if size * (m * k + m * n + 2 * n * k) < card and n <= 1 << 23:
+            call("bsa_gated_forward", C.byref(p), *p8[:5], ws, BIG, None)
+            call("bsa_gated_backward", C.byref(p), *p8[:7], ws, BIG, None)
+    ws = 1 << 50
+    for dtype in (abi.BSA_F32, abi.BSA_BF16):
+        for m in (1 << 29, (1 << 30) - 129, 1 << 30, (1 << 31) - 256):
+            for k in (1, 3, 8):
+                for n in (1, 16, 17, 32, 33, 34, 48, 63, 64, 65, 66, 100, 128):
+                    maps(m, k, n, dtype)
+                    if n <= 66:
+                        maps(m, n, k, dtype)
+        for n in (1 << 22, 1 << 23, 1 << 24):
+            for k, m in ((1, 1), (1, 17), (1, 300), (65, 17), (300, 1), (2049, 2), (4097, 40), (1, 4097), (8, 1 << 13)):
+                maps(m, k, n, dtype)
+                maps(m, n, k, dtype)
+        for _ in range(4000):
+            maps(*(int(2 ** rng.uniform(0, top)) for top in (31, 24, 24)), dtype)
+    assert seen[0] > 5000, seen
+
+    for _ in range(3000):
+        d, dtype = 2 ** rng.randint(5, 7), rng.choice((abi.BSA_F32, abi.BSA_BF16))
+        kv, group, seqs = (int(2 ** rng.uniform(0, top)) for top in (16, 7, 24))
+        tq, tk = (int(2 ** rng.uniform(0, 30)) for _ in range(2))
+        heads = kv * group
+        if heads < 1 << 16 and tq * group <= 1 << 30 and kv < 1 << 16 and 2 * d * (2 * tq * heads + tk * kv) < card:
+            p = abi.bsa_attention_t(seqs=seqs, heads=heads, kv_heads=kv, head_dim=d, total_q=tq, total_k=tk, dtype=dtype, zero_rest=1)
+            call("bsa_cache_attention_forward", C.byref(p), *p8[:10], ws, BIG, None)
+            call("bsa_attention_forward", C.byref(p), *p8[:8], ws, BIG, None)
+            call("bsa_attention_backward", C.byref(p), *p8[:12], ws, BIG, None)
+            p = abi.bsa_cache_t(seqs=seqs, kv_heads=kv, head_dim=d, dtype=dtype, rows=tq, total_k=tk)
+            call("bsa_cache_write", C.byref(p), *p8[:9], None)
+            call("bsa_cache_read", C.byref(p), *p8[:9], None)
+            p = abi.bsa_rotary_t(rows=tq << rng.randint(0, 10), heads=heads, kv_heads=kv, head_dim=d, rot=d, axes=1, dtype=dtype, eps=1e-5,
+                                 magnitude=1.0)
+            call("bsa_rotary_forward", C.byref(p), *p8[:8], None)
+            call("bsa_rotary_backward", C.byref(p), *p8[:12], ws, BIG, None)
+    assert seen[0] > 8000, seen
 
 
 if __name__ == "__main__":

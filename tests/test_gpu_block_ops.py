@@ -155,6 +155,12 @@ def test_gated_large_tiles(dtype):
     check_gated(gen(4), dtype, 4096, 256, 2048, "gelu", False, train=False)
 
 
+@pytest.mark.parametrize("m,k,n", [(700, 1101, 5505), (5001, 1500, 301)])
+def test_gated_float32_tiles_of_long_contractions(m, k, n):
+    """128 x 128 tiles, which very long and narrow products take as well, and 128 x 64 tiles, none by planes."""
+    check_gated(gen(m), "f32", m, k, n, "silu", True)
+
+
 # ---- 8-bit cache ----
 
 def check_cache(g, dtype, lens, cap, used, kv, d, tail=0, k=None, v=None):

@@ -20,7 +20,7 @@ def stub(tmp_path_factory):
     return str(so)
 
 
-@pytest.mark.parametrize("check", ["copied_rows", "rotary_steps"])
+@pytest.mark.parametrize("check", ["copied_rows", "rotary_steps", "launches_fit"])
 def test_launches(stub, check):
     r = subprocess.run([sys.executable, os.path.join(HERE, "launch_checks.py"), stub, check], capture_output=True, text=True,
                        timeout=300)
