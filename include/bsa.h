@@ -371,7 +371,7 @@ typedef struct {
   int64_t ld_x, ld_w, ld_y, ld_dy;      /* elements between rows (0: packed)            */
 } bsa_gated_t;
 
-/* Validate p and report the workspaces (pointers may be NULL). */
+/* Validate p and report the workspaces (pointers may be NULL), which begin on 16 bytes. */
 bsa_status_t bsa_gated_sizes(const bsa_gated_t* p, size_t* ws_fwd_bytes, size_t* ws_bwd_bytes);
 
 /* bias and pre may be NULL. pre [m, 2 n] packed receives [g | u] for the backward, rounded to dtype. */

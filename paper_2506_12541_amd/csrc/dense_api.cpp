@@ -329,6 +329,7 @@ bsa_status_t bsa_gated_forward(const bsa_gated_t* p, const void* x, const void* 
     if (on_one(pre, {x, w, bias})) return bad("pre may not alias an input");
     const size_t need = bsa::gated_fwd_ws_bytes(a);
     if (need && (!ws || ws_bytes < need)) return small_ws("gated map forward", need);
+    if (need && !aligned(ws, 16)) return bad("ws must be 16-byte aligned");
     hipError_t e;
     BSA_PHASE("gated.fwd", (hipStream_t)stream, e = bsa::launch_gated_fwd(a, x, w, bias, y, pre, ws, (hipStream_t)stream));
     return launched(e, "bsa_gated_forward");
@@ -351,6 +352,7 @@ bsa_status_t bsa_gated_backward(const bsa_gated_t* p, const void* x, const void*
       if (on_one(g, {x, w, pre, dy})) return bad("a gradient may not alias an input");
     const size_t need = bsa::gated_bwd_ws_bytes(a);
     if (need && (!ws || ws_bytes < need)) return small_ws("gated map backward", need);
+    if (need && !aligned(ws, 16)) return bad("ws must be 16-byte aligned");
     hipError_t e;
     BSA_PHASE("gated.bwd", (hipStream_t)stream,
               e = bsa::launch_gated_bwd(a, x, w, pre, dy, dx, dw, db, ws, (hipStream_t)stream));

@@ -137,6 +137,20 @@ def test_gated_pointers(lib):
     assert lib.bsa_gated_forward(C.byref(gat(m=0)), *[None] * 6, 0, None) == 0
 
 
+def test_gated_workspaces_begin_on_16_bytes(lib):
+    """Pieces of 16 bytes go from the workspace straight into LDS."""
+    f, b = C.c_size_t(), C.c_size_t()
+    for kw in (dict(m=100, k=8192), dict(m=2048, k=1024, n=1024, dtype=0), dict(m=3000, k=1031, n=1100)):
+        p = gat(**kw)
+        assert lib.bsa_gated_sizes(C.byref(p), C.byref(f), C.byref(b)) == 0 and f.value > 0 and b.value > 0
+        x, w, bias, y, pre, dy, dx, dw, db = (i * PTR for i in range(1, 10))
+        for ws in (16 * PTR + 2, 16 * PTR + 4, 16 * PTR + 8):
+            assert lib.bsa_gated_forward(C.byref(p), x, w, bias, y, pre, ws, f.value, None) == INVALID
+            assert "aligned" in lib.bsa_last_error().decode()
+            assert lib.bsa_gated_backward(C.byref(p), x, w, pre, dy, dx, dw, db, ws, b.value, None) == INVALID
+            assert "aligned" in lib.bsa_last_error().decode()
+
+
 # ---- 8-bit cache ----
 
 @pytest.mark.parametrize("kw,code", [
