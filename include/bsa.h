@@ -499,7 +499,8 @@ bsa_status_t bsa_cache_read(const bsa_cache_t* p, const void* cache_k, const voi
 
 /* bsa_attention_forward with the cache for k and v: o = softmax(scale q K^T) V with the values that the bytes stand
  * for. Everything else is as there, p's k and v strides being those of the cache in bytes; there is no backward.
- * bf16 queries: probabilities are rounded to bf16 where they enter the product with V. float32 queries, and their
+ * bf16 queries: probabilities enter the product with V as two bf16 parts (within 2^-16 of themselves) in calls of few
+ * rows, such as single tokens, and rounded to bf16 in others. float32 queries, and their
  * probabilities, enter the products as three bf16 parts (within 2^-24 of themselves; a query value past the
  * largest bf16 number gives NaN). */
 bsa_status_t bsa_cache_attention_sizes(const bsa_attention_t* p, size_t* ws_bytes);

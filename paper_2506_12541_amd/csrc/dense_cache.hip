@@ -198,6 +198,11 @@ struct ByteTile {
 
 // float32 values as three bf16 parts: x1 = bf16(x), x2 = bf16(x - x1), x3 = bf16(x - x1 - x2). bf16: one.
 template <typename T> constexpr int parts_of() { return sizeof(T) == 4 ? 3 : 1; }
+// Of a probability in calls of few rows (cache_step_kernel). Beside a bf16 query two, within 2^-16 of it: the matrix cores wait for
+// memory there, so a second product costs 0 to 1.5 % (32 tokens against 64 to 8192 rows: 69.8 us, so 70.0; 16 x 1 to 4
+// rows, 4 key heads: 36.8 and 37.2), and outputs are off by their own rounding alone: 0.0017 of the norm, with one part 0.0023 to
+// 0.0026.
+template <typename T> constexpr int probability_parts() { return sizeof(T) == 4 ? 3 : 2; }
 template <int P>
 __device__ __forceinline__ void to_parts(const float* v, bf16x8 (&out)[P]) {
   float x[8];
@@ -372,8 +377,10 @@ __device__ __forceinline__ int clear_bytes(uint8_t* t, int lane) {
 // Many rows: as packed_fwd_kernel of dense_attn.hip, the tiles of keys and values converted to bf16 as they are
 // stored in LDS, once for the workgroup. Bound by the matrix cores and the exponentials beside them: two waves share a
 // SIMD (one register more than 256 leaves one: chunks of 200 to 1024 rows against 1024 to 8192, 252 us, so 173), and the one
-// that multiplies goes first (166). 4 x 1024 rows against 8192, 32 heads of 128: 586 us, 880 TFLOP/s; packed_fwd_kernel on bf16
-// caches 542.
+// that multiplies goes first (166). 4 x 1024 rows against 8192, 32 heads of 128, causal: 497 us, 1.04 PFLOP/s; packed_fwd_kernel on
+// bf16 caches 492. A quarter of its LDS cycles are bank conflicts of the stores of converted tiles. float32 queries: 1150 us, 1.34
+// PFLOP/s of their three products. bf16: probabilities enter their product as one bf16 part each, as in packed_fwd_kernel, where a
+// second would add half of the products again; the output carries 0.0023 of the norm, its own rounding alone is 0.0017.
 template <typename T, int HD, int QB>
 __global__ void __launch_bounds__((64 * kWaves), 2) cache_fwd_kernel(CacheFwdP cp) {
   constexpr int NW = kWaves, KT = 64, KB = KT / 16, NCH = HD / 32, DB = HD / 16, R = 16 * QB * NW, P = parts_of<T>();
@@ -584,7 +591,7 @@ __device__ __forceinline__ StepAt step_at(const CacheFwdP& cp) {
 // (324 MB) 65 us and 6 to join them, 2 against 65536 to 131072 (371 MB) 74 and 8; a copy would take 62 and 72.
 template <typename T, int HD, int HW>
 __global__ void __launch_bounds__(256, 2) cache_step_kernel(CacheFwdP cp) {
-  constexpr int NW = kWaves, NK = NW / HW, KT = 32, ST = NK * KT, KB = 2, DB = HD / 16, NCH = HD / 32, P = parts_of<T>();
+  constexpr int NW = kWaves, NK = NW / HW, KT = 32, ST = NK * KT, KB = 2, DB = HD / 16, NCH = HD / 32, P = parts_of<T>(), PP = probability_parts<T>();
   typedef StepTile<HD> Tile;
   constexpr int VB = KT * HD;      // bytes of a wave's value tile
   __shared__ __attribute__((aligned(1024))) uint8_t vs[2 * NW * VB];
@@ -671,13 +678,13 @@ __global__ void __launch_bounds__(256, 2) cache_step_kernel(CacheFwdP cp) {
         ls += e;
         v8[4 * kb + i] = e * __uint_as_float((kc.ev[kb] >> (8 * i) & 0xff) << 23);
       }
-    bf16x8 pf[P];
-    to_parts<P>(v8, pf);
+    bf16x8 pf[PP];
+    to_parts<PP>(v8, pf);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const bf16x8 vf = e4m3_chunk(byte_cols<HD>(vc, db, r, j), 1.f);
 #pragma unroll
-      for (int x = P - 1; x >= 0; --x) o[db] = mma(vf, pf[x], o[db]);
+      for (int x = PP - 1; x >= 0; --x) o[db] = mma(vf, pf[x], o[db]);
     }
   };
   const int k_first = k_lo + wid / HW * KT;

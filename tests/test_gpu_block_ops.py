@@ -258,6 +258,24 @@ def check_cache_attention(g, dtype, lq, cap, used, heads, kv, d, causal, tail=0,
     check("lse", lse, want["lse"][0], more * want["lse"][1])
 
 
+@pytest.mark.parametrize("heads,kv,d", [(8, 2, 128), (4, 4, 64), (5, 1, 32), (32, 8, 128)])
+def test_cache_attention_steps_round_once(heads, kv, d):
+    """bf16 outputs of few rows: rounded once. Probabilities enter their product as two bf16 parts, within 2^-16 of
+    themselves, which doubles the terms of each sum; nothing else is off by more than float32 sums are."""
+    g = gen(14)
+    for lq, cap, used in (([1] * 6, [1024] * 6, [1, 1024, 0, 700, 257, 64]), ([2, 17], [5000, 3000], [4999, 2049]), ([1], [9000], [8999])):
+        q, total = normal(g, sum(lq), heads, d, dtype=BF), sum(cap)
+        k, v = normal(g, total, kv, d), normal(g, total, kv, d) * torch.exp2(normal(g, total, kv, 1).round())
+        cache, one, cu_q, cu_k = dense.cache_alloc(total, kv, d), cu([total]), cu(lq), cu(cap)
+        dense.cache_write(cache, k, v, one, one)
+        kd, vd = dense.cache_read(cache, total, one, one, dtype=F32)
+        o, _ = dense.cache_attention_forward(q, cache, cu_q, cu_k, ints(used), causal=True)
+        want, e = dense_ref.attention(q.float(), kd, vd, cu_q, cu_k, used, True)["o"]
+        whole = dense_ref.attention(q.float(), kd, vd.abs(), cu_q, cu_k, used, True)["o"][0]      # sum of p |v|
+        e = 2 * e + 2.0 ** -16 * whole
+        check("o", o, want, e + dense_ref.HALF[BF] * (want.abs() + e))
+
+
 LENS = [1, 0, 7, 64, 65, 130, 33, 200]
 
 
