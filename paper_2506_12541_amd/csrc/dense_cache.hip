@@ -378,7 +378,7 @@ __device__ __forceinline__ int clear_bytes(uint8_t* t, int lane) {
 // stored in LDS, once for the workgroup. Bound by the matrix cores and the exponentials beside them: two waves share a
 // SIMD (one register more than 256 leaves one: chunks of 200 to 1024 rows against 1024 to 8192, 252 us, so 173), and the one
 // that multiplies goes first (166). 4 x 1024 rows against 8192, 32 heads of 128, causal: 497 us, 1.04 PFLOP/s; packed_fwd_kernel on
-// bf16 caches 492. A quarter of its LDS cycles are bank conflicts of the stores of converted tiles. float32 queries: 1150 us, 1.34
+// bf16 caches 492. A quarter of its LDS cycles are bank conflicts, which tiles loaded directly do not have. float32 queries: 1150 us, 1.34
 // PFLOP/s of their three products. bf16: probabilities enter their product as one bf16 part each, as in packed_fwd_kernel, where a
 // second would add half of the products again; the output carries 0.0023 of the norm, its own rounding alone is 0.0017.
 template <typename T, int HD, int QB>
@@ -588,7 +588,7 @@ __device__ __forceinline__ StepAt step_at(const CacheFwdP& cp) {
 // A key's scale enters as its bytes become bf16, a value's by its probability (a power of two: no rounding more).
 // Heads side by side read a packed cache's rows in long runs: 32 x 8192 keys, 8 heads of 128, 106 us (5.1 TB/s), of one
 // head a workgroup 127, as fast as in a head-major cache. Bound by the bytes of the caches: 32 tokens against 64 to 8192 rows
-// (324 MB) 65 us and 6 to join them, 2 against 65536 to 131072 (371 MB) 74 and 8; a copy would take 62 and 72.
+// (324 MB) 64 us and 6 to join them, 2 against 65536 to 131072 (371 MB) 72 and 8; a copy would take 62 and 72.
 template <typename T, int HD, int HW>
 __global__ void __launch_bounds__(256, 2) cache_step_kernel(CacheFwdP cp) {
   constexpr int NW = kWaves, NK = NW / HW, KT = 32, ST = NK * KT, KB = 2, DB = HD / 16, NCH = HD / 32, P = parts_of<T>(), PP = probability_parts<T>();

@@ -794,7 +794,8 @@ hipError_t gated_bwd(const GatedArgs& a, const void* x, const void* w, const voi
   }
   if (!planes && (dx || dw || a.m == 0)) {    // without rows this also clears db
     LinearArgs r = rows_of(a);
-    // the operands of the gradients that are formed; the other one's pointer may be NULL
+    // the operands of the gradients that are formed; the other one's pointer may be NULL (8191 x 1023 -> 2 x 2047: dw alone
+    // 154.5 us, 157 with a copy of w; dx alone 136 and 142)
     Pads pads = L.pads;
     pads.x = pads.x && dw && a.m > 0;
     pads.w = pads.w && dx && a.m > 0;

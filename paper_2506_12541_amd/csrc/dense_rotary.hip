@@ -10,8 +10,8 @@
 // few rows), forms the angles of a row once for all its heads, while its first pieces are on their way, and keeps their
 // cosines and sines in LDS; waves share nothing, so no barrier holds them together.
 // Bound by the bytes: 65536 rows of 8 + 8 heads of 64 (48 of them turn), bf16 with norms, the forward (268 MB) takes
-// 59 us, the backward (403 MB) 92 and 5 to join the gains' gradients; a copy would take 52 and 78. 16384 rows of 32 + 8
-// heads of 128 out of a fused projection (336 MB): 68 us, a copy 65.
+// 56 us, the backward (403 MB) 86 and 5 to join the gains' gradients; a copy would take 52 and 78. 16384 rows of 32 + 8
+// heads of 128 out of a fused projection (336 MB): 66 us, a copy 65.
 #include <algorithm>
 
 #include "common.hpp"
